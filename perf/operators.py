@@ -87,7 +87,7 @@ def draw(rng):
     else:
         q = 1 if what == "prefix" and rng.random() < 0.7 else _log(rng, 2, 512)
         length = q + _log(rng, 1, 8000 if what == "chunk" else 1000)
-        seqs = _log(rng, 1, max(1, min(96, 8 * 300 * 8000 // (q * length))))
+        seqs = _log(rng, 1, max(1, min(96, 8 * 300 * 8000 // (q * length), most // length)))
         case.update(seqs=seqs, q=q, len=length, prefix=_log(rng, 1, 8192 if q == 1 else 2000) if what == "prefix" else 0)
     return case
 
