@@ -63,6 +63,12 @@ enum { KT_OP_LOSS_GRAD = 0, KT_OP_CAYLEY = 1, KT_OP_FAKEQUANT = 2, KT_OP_POOLED_
        KT_OP_SENSITIVITY = 6, KT_OP_LOSS_GRAD_RECOMPUTE = 7,
        KT_OP_POOLED_LOSS_GRAD_RECOMPUTE = 8 };
 
+/* What the norm's rows are quantised to, and what a cache holds. */
+typedef int32_t kt_qformat;
+enum { KT_Q_NONE = 0, KT_Q_INT4 = 1, KT_Q_INT8 = 2, KT_Q_E4M3 = 3 };
+typedef int32_t kt_kv_format;
+enum { KT_KV_BF16 = 0, KT_KV_U8 = 1, KT_KV_U4 = 2 };
+
 /* Library version (major*10000 + minor*100 + patch). Host call. */
 int32_t kt_version(void);
 
@@ -353,6 +359,115 @@ kt_status kt_hadamard_rows(const void* X, int64_t ldx, void* Y, int64_t ldy, con
 kt_status kt_fuse_rotation(const float* W, int64_t ldw, const float* R, int64_t ldr, float* Wout,
                            int64_t ldo, int64_t k, int64_t d, int32_t side,
                            void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Serving a rotated, quantised model: the rows in front of a quantised product, the cache of rotated keys, attention over it.
+ *
+ * Residual addition, RMS norm and per-token symmetric codes of token rows, in one pass:
+ *
+ *   h = x + res;  rstd = 1 / sqrt(mean_j h_j^2 + eps);  u = h * gain;  y = u * rstd
+ *   t = (clip_ratio * max_j |u_j|) / L;   code_j = round(clamp(u_j * (1 / t), -L, L));   scale = t * rstd
+ *
+ * y_j is code_j * scale up to the code's rounding: the codes of y and of u are the same, so they do not depend on rstd, and
+ * are pinned to fp32 with one rounding an operation in the order written (h and u included).  `format`:
+ *   KT_Q_INT4  L = 7, one code per int8 byte as in kt_rotate_fakequant_int4;  KT_Q_INT8  L = 127;  both round half to even
+ *   KT_Q_E4M3  L = 448, codes are the nearest e4m3 values (half to even);  KT_Q_NONE  no codes, Y = y
+ *  X, res   [n][ldx], [n][ldres] `dtype` (KT_BF16 or KT_F32), res may be NULL (h = x).
+ *  gain     [d] gain_dtype or NULL (1: gains fused into the weights).
+ *  res_out  [n][ldro] dtype or NULL: h, rounded to dtype.  May be X or res, laid out alike (the norm goes on from the unrounded h).
+ *  Y        [n][ldy] dtype or NULL: the values that the codes stand for (code * scale), or y for KT_Q_NONE.  May be X or res, laid out alike, not res_out.
+ *  codes    [n][ldc] bytes or NULL, 8-byte aligned, ldc a multiple of 8.   scales [n] fp32 or NULL.
+ *  d        a multiple of 8 up to 32768, rows 16-byte aligned.  1 <= n < 2^31.
+ * A row whose t is below the smallest normal number has codes and scale 0.  A row with a value of h or u that is not finite, or
+ * with a sum of squares beyond fp32, has codes 0 and scale NaN.  No workspace.
+ */
+kt_status kt_add_rmsnorm_quant(const void* X, int64_t ldx, const void* res, int64_t ldres, const void* gain, int64_t n,
+                               int64_t d, kt_dtype dtype, kt_dtype gain_dtype, float eps, float clip_ratio,
+                               kt_qformat format, void* res_out, int64_t ldro, void* Y, int64_t ldy, void* codes,
+                               int64_t ldc, float* scales, void* stream);
+
+/*
+ * A paged cache of keys and values (host struct, passed by address, read during the call).
+ *  data       device, 16-byte aligned, kt_kv_cache_bytes() bytes; needs no initialisation (what no token was written to is never
+ *             read as one).  Layout [page][head][page_size / 64][block], a block being 64 tokens of one head: keys, values, then
+ *             (KT_KV_U8, KT_KV_U4) {step, minimum} fp32 of each key and of each value.  The order inside is given in
+ *             csrc/kt_kvcache.h.
+ *  page_size  tokens of a page: a power of two from 64 to 65536.   n_heads  key / value heads, at most 1024.
+ *  head_dim   64, 128 or 256.
+ *  format     KT_KV_BF16; KT_KV_U8, KT_KV_U4: asymmetric codes of 8 or 4 bits per token and head (Background, "Uniform
+ *             Quantization": b = min, s = (max - min) / (2^k - 1); Setup: KV caches).
+ * Token t of a sequence lives in slot  pages[t / page_size] * page_size + t % page_size.
+ */
+typedef struct {
+  void* data;
+  int64_t n_pages, page_size, n_heads, head_dim;
+  kt_kv_format format;
+} kt_kv_cache;
+
+/* Bytes of the cache's data (`data` is not looked at; 0 on bad sizes).  Host call. */
+size_t kt_kv_cache_bytes(const kt_kv_cache* cache);
+
+/*
+ * New tokens into the cache, with the rotations applied on the way: keys and queries are turned by their position and then, if
+ * asked, by the online Hadamard rotation R3 ("Placement of the Rotations": after the position rotation, on queries and keys
+ * alike, so that it cancels in their products); keys and values are quantised and written to their slots; queries go to Q_out.
+ *
+ *   position: for i < rot_dim / 2, with (a, b) = features (i, i + rot_dim / 2), or (2 i, 2 i + 1) if `interleaved`:
+ *             (a, b) <- (a cos - b sin, b cos + a sin),  cos = rope[pos][i], sin = rope[pos][rot_dim / 2 + i]
+ *   hadamard: y <- y H / sqrt(head_dim), H the Sylvester matrix as in kt_hadamard_rows
+ *   KT_KV_U8, KT_KV_U4: b = min_j y_j, s = (max_j y_j - b) / L, code_j = round(((y_j - b) * L) / (max - b)), L = 255 or 15;
+ *             the value held is code * s + b.  KT_KV_BF16: y rounded to nearest even.
+ *
+ * fp32, one rounding an operation in the order written (the Hadamard rotation: butterflies by distances 1, 2, 4, ..., then one
+ * multiplication), rounding half to even.
+ *  Q [n][ldq], Q_out [n][ldqo]: n_q_heads heads of head_dim, both NULL with n_q_heads = 0 to leave queries out.  Q_out may be Q, laid out alike.
+ *  K [n][ldk], V [n][ldv]: the cache's heads.  All `dtype` (KT_BF16, KT_F32), rows 16-byte aligned, so that parts of one
+ *            projection's rows can be handed in.
+ *  slots     [n] int64: where each token goes.  A token whose slot is negative or outside the cache is passed over (its Q_out row
+ *            is left as it was); so is one whose position is outside the table.  Slots must differ from each other; two equal ones
+ *            leave an unspecified mix of both tokens in that slot.
+ *  positions [n] int32, rope [n_pos][rot_dim] fp32 16-byte aligned, rot_dim a multiple of 16 up to head_dim; rope NULL: no
+ *            position rotation.
+ * A key or value row with a value that is not finite (or whose width times L is beyond fp32) is held as NaN in KT_KV_U8 and KT_KV_U4; one
+ * whose s is below the smallest normal number as its minimum.  No workspace.
+ */
+kt_status kt_kv_append(const kt_kv_cache* cache, const void* Q, int64_t ldq, const void* K, int64_t ldk, const void* V,
+                       int64_t ldv, int64_t n, int64_t n_q_heads, kt_dtype dtype, const int64_t* slots,
+                       const int32_t* positions, const float* rope, int64_t n_pos, int64_t rot_dim, int32_t interleaved,
+                       int32_t hadamard, void* Q_out, int64_t ldqo, void* stream);
+
+/*
+ * The keys and values that the cache holds in `slots` [n], as values: K [n][ldk], V [n][ldv] of `dtype` (one of them may be
+ * NULL); to move a sequence elsewhere, or to see what quantisation has made of it.  Rows of slots outside the cache are left
+ * as they were; slots may repeat.
+ */
+kt_status kt_kv_gather(const kt_kv_cache* cache, const int64_t* slots, int64_t n, void* K, int64_t ldk, void* V, int64_t ldv,
+                       kt_dtype dtype, void* stream);
+
+/*
+ * Attention of new tokens over the cache:  o = sum_j p_j v_j,  p = softmax_j(scale * q . k_j), for every query head (head h reads
+ * key / value head h / (n_q_heads / n_heads)), j running over
+ *   - the first prefix_len tokens of prefix_pages: a prefix that all sequences share, read once for all of them; and
+ *   - the sequence's own tokens up to the query's: sequence i has lens[i] tokens in the pages of row i of `pages`, the last of them being
+ *     those of its queries (q_starts[i] .. q_starts[i + 1] - 1), which therefore are appended first.
+ *  Q, O     [n_tokens][ldq], [n_tokens][ldo] bf16 (dtype must be KT_BF16), rows of Q 16-byte, of O 8-byte aligned.
+ *  q_starts [n_seq + 1] int32, not descending, at most n_tokens; NULL: one query a sequence (n_tokens = n_seq, max_q = 1).  Rows in front
+ *           of the first and behind the last sequence are left as they were.  max_q: a bound on the queries of a sequence.
+ *  lens     [n_seq] int32, at most ldp * page_size (what is above counts as that).   pages [n_seq][ldp] int32; entries behind a
+ *           sequence's last page are not read, tokens of a page that is outside the cache count as not there.
+ *  lse      [n_tokens][n_q_heads] fp32 or NULL: log sum_j exp(scale * q . k_j).
+ * A query that sees nothing gives 0, and -inf in lse.  Scores, statistics and sums are fp32, the p_j are rounded to bf16 in front of
+ * their product with the values.  All index arrays are on the device: the call can be captured and replayed with other
+ * lengths and pages.  n_seq <= 4096, ldp * page_size < 2^31, scale > 0.
+ * Workspace: kt_paged_attention_bytes(n_tokens, n_q_heads, head_dim, prefix_len).
+ */
+kt_status kt_paged_attention(const kt_kv_cache* cache, const void* Q, int64_t ldq, kt_dtype dtype, const int32_t* q_starts,
+                             const int32_t* lens, const int32_t* pages, int64_t ldp, int64_t n_seq, int64_t n_tokens,
+                             int64_t max_q, int64_t n_q_heads, const int32_t* prefix_pages, int64_t prefix_len, float scale,
+                             void* O, int64_t ldo, float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Scratch bytes of kt_paged_attention (0 on bad sizes).  Host call. */
+size_t kt_paged_attention_bytes(int64_t n_tokens, int64_t n_q_heads, int64_t head_dim, int64_t prefix_len);
 
 /*
  * Measurement aid (not part of the method; off by default).  When enabled, the

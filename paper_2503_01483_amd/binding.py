@@ -11,10 +11,19 @@ _lib = None
 KT_F32, KT_BF16 = 0, 1
 KT_OP_LOSS_GRAD, KT_OP_CAYLEY, KT_OP_FAKEQUANT, KT_OP_POOLED_LOSS_GRAD, KT_OP_QUANT_METRICS = 0, 1, 2, 3, 4
 KT_OP_FUSE_ROTATION, KT_OP_SENSITIVITY, KT_OP_LOSS_GRAD_RECOMPUTE, KT_OP_POOLED_LOSS_GRAD_RECOMPUTE = 5, 6, 7, 8
+KT_Q_NONE, KT_Q_INT4, KT_Q_INT8, KT_Q_E4M3 = 0, 1, 2, 3
+KT_KV_BF16, KT_KV_U8, KT_KV_U4 = 0, 1, 2
 
 EXPORTS = ("kt_version", "kt_last_error", "kt_workspace_bytes", "kt_kurtosis_loss_grad",
            "kt_pooled_kurtosis_loss_grad", "kt_cayley_step", "kt_cayley_adam_step", "kt_rotate_fakequant_int4", "kt_rotate_quant_metrics", "kt_hadamard_rows", "kt_fuse_rotation", "kt_quant_sensitivity", "kt_profile_enable", "kt_profile_read",
-           "kt_profile_reset", "kt_cayley_step_static", "kt_build_id")
+           "kt_profile_reset", "kt_cayley_step_static", "kt_build_id", "kt_add_rmsnorm_quant", "kt_kv_cache_bytes", "kt_kv_append",
+           "kt_kv_gather", "kt_paged_attention", "kt_paged_attention_bytes")
+
+
+class _CacheDesc(ctypes.Structure):
+    """kt_kv_cache"""
+    _fields_ = [("data", ctypes.c_void_p), ("n_pages", ctypes.c_int64), ("page_size", ctypes.c_int64),
+                ("n_heads", ctypes.c_int64), ("head_dim", ctypes.c_int64), ("format", ctypes.c_int32)]
 
 
 class KtError(RuntimeError):
@@ -88,6 +97,19 @@ def lib():
     L.kt_rotate_fakequant_int4.restype = i32
     L.kt_rotate_fakequant_int4.argtypes = [vp, i64, vp, i64, i64, i64, i64, i32, i32, f32,
                                            vp, vp, vp, vp, vp, sz, vp]
+    cache = ctypes.POINTER(_CacheDesc)
+    L.kt_add_rmsnorm_quant.restype = i32
+    L.kt_add_rmsnorm_quant.argtypes = [vp, i64, vp, i64, vp, i64, i64, i32, i32, f32, f32, i32, vp, i64, vp, i64, vp, i64, vp, vp]
+    L.kt_kv_cache_bytes.restype = sz
+    L.kt_kv_cache_bytes.argtypes = [cache]
+    L.kt_kv_append.restype = i32
+    L.kt_kv_append.argtypes = [cache, vp, i64, vp, i64, vp, i64, i64, i64, i32, vp, vp, vp, i64, i64, i32, i32, vp, i64, vp]
+    L.kt_kv_gather.restype = i32
+    L.kt_kv_gather.argtypes = [cache, vp, i64, vp, i64, vp, i64, i32, vp]
+    L.kt_paged_attention_bytes.restype = sz
+    L.kt_paged_attention_bytes.argtypes = [i64, i64, i64, i64]
+    L.kt_paged_attention.restype = i32
+    L.kt_paged_attention.argtypes = [cache, vp, i64, i32, vp, vp, vp, i64, i64, i64, i64, i64, vp, i64, f32, vp, i64, vp, vp, sz, vp]
     L.kt_profile_enable.restype = i32
     L.kt_profile_enable.argtypes = [i32]
     L.kt_profile_read.restype = i32
@@ -297,6 +319,167 @@ def kt_quant_sensitivity(Y, alphas, *, bits=4, workspace=None, stream=None):
     _check(lib().kt_quant_sensitivity(_ptr(Y), Y.numel(), int(bits), _ptr(alphas), alphas.numel(), _ptr(out),
                                       _ptr(gamma), _ptr(ws), ws.numel(), _stream(stream)))
     return out, gamma
+
+
+def _operands(device, **tensors):
+    """All given tensors have to live on one device, the current one (a kernel is launched there)."""
+    for name, t in tensors.items():
+        if t is not None and (not t.is_cuda or t.get_device() != device):
+            raise ValueError(f"{name} is on {t.device}: operands have to be on the current device, cuda:{device}")
+
+
+def _device(t, name):
+    if not t.is_cuda:
+        raise ValueError(f"{name} is on {t.device}: a GPU tensor is needed")
+    return torch.cuda.current_device()
+
+
+def _index(t, name, dtype, shape):
+    if t.dtype != dtype or t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{name}: contiguous {dtype} of shape {tuple(shape)} needed, got {t.dtype} {tuple(t.shape)}")
+
+
+def _rows(t, name, shape=None, dtype=None):
+    """Leading dimension of a [n][width] tensor whose rows are contiguous; checks against `shape`, `dtype` where given."""
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1) or (shape is not None and t.shape != shape) or \
+            (dtype is not None and t.dtype != dtype):
+        raise ValueError(f"{name}: {dtype or 'a tensor'} of shape {tuple(shape) if shape else '[n, width]'} with contiguous rows "
+                         f"needed, got {t.dtype} {tuple(t.shape)}, strides {t.stride()}")
+    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+
+
+def _heads(t, name, n, heads, head_dim, dtype=None):
+    """Leading dimension of [n][heads][head_dim] (or [n][heads * head_dim]) rows with their heads next to each other."""
+    if t.dim() == 3:
+        if t.shape != (n, heads, head_dim) or t.stride(2) != 1 or (heads > 1 and t.stride(1) != head_dim):
+            raise ValueError(f"{name}: [{n}, {heads}, {head_dim}] with contiguous rows of heads needed, got {tuple(t.shape)}, "
+                             f"strides {t.stride()}")
+        if dtype is not None and t.dtype != dtype:
+            raise ValueError(f"{name}: {dtype} needed, got {t.dtype}")
+        return t.stride(0) if n > 1 else max(t.stride(0), heads * head_dim)
+    return _rows(t, name, (n, heads * head_dim), dtype)
+
+
+_CODE_TYPES = {KT_Q_INT4: (torch.int8,), KT_Q_INT8: (torch.int8,), KT_Q_E4M3: (torch.float8_e4m3fn, torch.uint8)}
+
+
+def kt_add_rmsnorm_quant(X, *, res=None, gain=None, eps=1e-6, clip_ratio=1.0, format=KT_Q_INT8, res_out=None, Y=None,
+                         codes=None, scales=None, stream=None):
+    """Norm of the rows of X (+ res) [n][d] and their codes.  Writes the outputs that are given; returns (codes, scales)."""
+    dev = _device(X, "X")
+    _operands(dev, X=X, res=res, gain=gain, res_out=res_out, Y=Y, codes=codes, scales=scales)
+    xdt, ldx = _dtype_code(X), _rows(X, "X")
+    n, d = X.shape
+    ld = [0 if t is None else _rows(t, name, X.shape, X.dtype) for name, t in (("res", res), ("res_out", res_out), ("Y", Y))]
+    if gain is not None and (gain.shape != (d,) or not gain.is_contiguous()):
+        raise ValueError(f"gain: [{d}], contiguous, needed, got {tuple(gain.shape)}")
+    if codes is not None:
+        if codes.dtype not in _CODE_TYPES.get(format, ()):
+            raise TypeError(f"codes of type {codes.dtype} do not fit format {format}")
+        ldc = _rows(codes, "codes", X.shape)
+    if scales is not None:
+        _index(scales, "scales", torch.float32, (n,))
+    _check(lib().kt_add_rmsnorm_quant(_ptr(X), ldx, _ptr(res), ld[0], _ptr(gain), n, d, xdt, xdt if gain is None else _dtype_code(gain),
+                                      eps, clip_ratio, format, _ptr(res_out), ld[1], _ptr(Y), ld[2], _ptr(codes),
+                                      0 if codes is None else ldc, _ptr(scales), _stream(stream)))
+    return codes, scales
+
+
+class KVCache:
+    """A paged key / value cache: its shape, and `data`, a uint8 tensor of as many bytes (allocated here unless given)."""
+
+    def __init__(self, n_pages, page_size, n_heads, head_dim, format, *, data=None, device="cuda"):
+        self.n_pages, self.page_size, self.n_heads, self.head_dim, self.format = n_pages, page_size, n_heads, head_dim, format
+        self.desc = _CacheDesc(None, n_pages, page_size, n_heads, head_dim, format)
+        nbytes = lib().kt_kv_cache_bytes(ctypes.byref(self.desc))
+        if nbytes == 0:
+            raise KtError(2, kt_last_error() or "bad cache sizes")
+        if data is None:
+            data = torch.empty(nbytes, dtype=torch.uint8, device=device)
+        if data.dtype != torch.uint8 or not data.is_contiguous() or data.numel() != nbytes:
+            raise ValueError(f"data: {nbytes} contiguous bytes (uint8) needed, got {data.dtype} {tuple(data.shape)}")
+        self.data = data
+        self.desc.data = data.data_ptr()
+        self.ref = ctypes.byref(self.desc)
+
+
+def kt_kv_append(cache, K, V, slots, *, Q=None, positions=None, rope=None, interleaved=False, hadamard=False, Q_out=None,
+                 stream=None):
+    """Rotated, quantised K and V [n][heads][head_dim] into `slots` [n] of the cache; returns the rotated queries (Q_out or new)."""
+    dev = _device(K, "K")
+    if Q is not None and Q_out is None:
+        Q_out = torch.empty(Q.shape, dtype=Q.dtype, device=Q.device)
+    _operands(dev, cache=cache.data, K=K, V=V, slots=slots, Q=Q, positions=positions, rope=rope, Q_out=Q_out)
+    n, hd, dt = K.shape[0], cache.head_dim, _dtype_code(K)
+    ldk, ldv = _heads(K, "K", n, cache.n_heads, hd), _heads(V, "V", n, cache.n_heads, hd, K.dtype)
+    _index(slots, "slots", torch.int64, (n,))
+    hq = ldq = ldqo = 0
+    if Q is not None:
+        hq = Q.numel() // (n * hd) if n else 0
+        ldq, ldqo = _heads(Q, "Q", n, hq, hd, K.dtype), _heads(Q_out, "Q_out", n, hq, hd, K.dtype)
+    elif Q_out is not None:
+        raise ValueError("Q_out without Q")
+    n_pos = rot = 0
+    if rope is not None:
+        if positions is None:
+            raise ValueError("positions are needed with rope")
+        _index(positions, "positions", torch.int32, (n,))
+        if rope.dim() != 2:
+            raise ValueError("rope: [n_pos, rot_dim] needed")
+        _index(rope, "rope", torch.float32, rope.shape)
+        n_pos, rot = rope.shape
+    _check(lib().kt_kv_append(cache.ref, _ptr(Q), ldq, _ptr(K), ldk, _ptr(V), ldv, n, hq, dt, _ptr(slots),
+                              _ptr(positions) if rope is not None else None, _ptr(rope), n_pos, rot, bool(interleaved),
+                              bool(hadamard), _ptr(Q_out), ldqo, _stream(stream)))
+    return Q_out
+
+
+def kt_kv_gather(cache, slots, *, K=None, V=None, dtype=torch.bfloat16, stream=None):
+    """The values held in `slots` [n]: (K, V) [n][heads][head_dim], those given or, if neither is, new ones of `dtype`."""
+    dev = _device(slots, "slots")
+    n = slots.shape[0]
+    if K is None and V is None:
+        K, V = (torch.zeros(n, cache.n_heads, cache.head_dim, dtype=dtype, device=slots.device) for _ in range(2))
+    _operands(dev, cache=cache.data, slots=slots, K=K, V=V)
+    _index(slots, "slots", torch.int64, (n,))
+    first = K if K is not None else V
+    ld = [0 if t is None else _heads(t, name, n, cache.n_heads, cache.head_dim, first.dtype) for name, t in (("K", K), ("V", V))]
+    _check(lib().kt_kv_gather(cache.ref, _ptr(slots), n, _ptr(K), ld[0], _ptr(V), ld[1], _dtype_code(first), _stream(stream)))
+    return K, V
+
+
+def kt_paged_attention(Q, cache, pages, lens, *, q_starts=None, max_q=1, prefix_pages=None, prefix_len=0, scale=None, out=None,
+                       lse=None, workspace=None, stream=None):
+    """Attention of Q [n_tokens][heads][head_dim] over the cache; returns out (given or new).  scale: 1 / sqrt(head_dim)."""
+    dev = _device(Q, "Q")
+    if Q.dim() != 3:
+        raise ValueError(f"Q: [n_tokens, heads, head_dim] needed, got {tuple(Q.shape)}")
+    n, hq, hd = Q.shape
+    if out is None:
+        out = (torch.empty if q_starts is None else torch.zeros)(n, hq, hd, dtype=Q.dtype, device=Q.device)
+    ws = workspace if workspace is not None else Workspace(Q.device)
+    _operands(dev, Q=Q, cache=cache.data, pages=pages, lens=lens, q_starts=q_starts, prefix_pages=prefix_pages, out=out, lse=lse)
+    n_seq = lens.shape[0]
+    ldq, ldo = _heads(Q, "Q", n, hq, cache.head_dim), _heads(out, "out", n, hq, cache.head_dim, Q.dtype)
+    _index(lens, "lens", torch.int32, (n_seq,))
+    if pages.dim() != 2 or pages.shape[0] != n_seq:
+        raise ValueError(f"pages: [{n_seq}, pages of a sequence] needed, got {tuple(pages.shape)}")
+    _index(pages, "pages", torch.int32, pages.shape)
+    if q_starts is not None:
+        _index(q_starts, "q_starts", torch.int32, (n_seq + 1,))
+    if prefix_len:
+        if prefix_pages is None or prefix_pages.dim() != 1 or prefix_pages.shape[0] * cache.page_size < prefix_len:
+            raise ValueError("prefix_pages: one dimension of pages for prefix_len tokens needed")
+        _index(prefix_pages, "prefix_pages", torch.int32, prefix_pages.shape)
+    if lse is not None:
+        _index(lse, "lse", torch.float32, (n, hq))
+    need = lib().kt_paged_attention_bytes(n, hq, cache.head_dim, prefix_len)
+    buf = ws.get(need)
+    _check(lib().kt_paged_attention(cache.ref, _ptr(Q), ldq, _dtype_code(Q), _ptr(q_starts), _ptr(lens), _ptr(pages), pages.shape[1], n_seq, n,
+                                    max_q, hq, _ptr(prefix_pages) if prefix_len else None, prefix_len,
+                                    cache.head_dim ** -0.5 if scale is None else scale, _ptr(out), ldo, _ptr(lse), _ptr(buf), buf.numel(),
+                                    _stream(stream)))
+    return out
 
 
 def kt_profile_enable(max_records):

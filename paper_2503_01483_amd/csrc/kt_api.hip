@@ -15,6 +15,7 @@
 #include "kt_cayley_d128.h"
 #include "kt_fused_d128.h"
 #include "kt_hadamard.h"
+#include "kt_host.h"
 #include "kt_rows.h"
 #include "kt_rowsync.h"
 #include "kt_skinny.h"
@@ -24,15 +25,15 @@ namespace kt {
 // ------------------------------------------------------------------ errors --------
 static thread_local char g_err[512] = "";
 
-static kt_status fail(kt_status code, const char* fmt, ...) {
+void clear_error() { g_err[0] = 0; }
+
+kt_status fail(kt_status code, const char* fmt, ...) {
   va_list ap;
   va_start(ap, fmt);
   vsnprintf(g_err, sizeof(g_err), fmt, ap);
   va_end(ap);
   return code;
 }
-
-static bool launch_ok() { return hipGetLastError() == hipSuccess; }
 
 // Kernels that use more than 64 KiB of dynamic LDS need the limit raised once per kernel AND per
 // device (the attribute belongs to the device's copy of the code).  Remembers what has been set;
@@ -125,11 +126,6 @@ using TH_BIG = Tile<_Float16, 256, 256, 2, 2>;  // retraction, d >= 1024 (split3
 using TH_128 = Tile<_Float16, 128, 128, 2, 2>;
 using TH_64 = Tile<_Float16, 64, 64, 2, 2>;
 using TF_64 = Tile<float, 64, 64, 2, 2>;     // fp32 path, d x d outputs of few tiles
-
-static inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
-static inline int64_t round_up(int64_t a, int64_t b) { return ceil_div(a, b) * b; }
-
-constexpr int kNumCUs = 256;
 
 // fp32 products: 64 x 64 tiles when `tiles` 128 x 128 ones would leave CUs idle, in all of the launch or in its last
 // round.  A 128 x 128 tile takes a CU about 4100 cycles per 32 of K, a 64 x 64 one a little over a quarter of that, four
@@ -1560,11 +1556,6 @@ static kt_status run_hadamard(const void* X, int64_t ldx, void* Y, int64_t ldy, 
 extern "C" {
 
 int32_t kt_version(void) { return 100; }
-
-#ifndef KT_BUILD_ID
-#define KT_BUILD_ID "unknown"
-#endif
-const char* kt_build_id(void) { return KT_BUILD_ID; }
 
 const char* kt_last_error(void) { return g_err; }
 

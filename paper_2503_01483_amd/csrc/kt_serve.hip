@@ -1,0 +1,278 @@
+// kt_serve.hip -- host side of the serving operators: argument checks, workspace layout, launches, and their part of the extern "C"
+// boundary of include/kt.h.
+#include "kt_attention.h"
+#include "kt_host.h"
+#include "kt_norm.h"
+
+namespace kt {
+
+static bool misaligned(const void* p, uintptr_t to) { return reinterpret_cast<uintptr_t>(p) & (to - 1); }
+
+// rows of `width` values of `dtype`: leading dimension and 16-byte alignment
+static bool rows_ok(const void* p, int64_t ld, int64_t width, kt_dtype dtype) {
+  return ld >= width && ld <= ((int64_t)1 << 24) && ld % (dtype == KT_F32 ? 4 : 8) == 0 && !misaligned(p, 16);
+}
+
+// ------------------------------------------------------------------ norm ----------
+template <typename T, typename TG, int FORMAT>
+static kt_status launch_norm(const NormArgs& a, hipStream_t st) {
+  const int64_t chunks = ceil_div(a.d, 8);
+  auto go = [&](auto tpr, auto ch) {
+    constexpr int TPR = decltype(tpr)::value, CH = decltype(ch)::value, ROWS = TPR >= 256 ? 1 : 256 / TPR;
+    add_rmsnorm_quant_kernel<T, TG, FORMAT, TPR, CH><<<dim3((unsigned)ceil_div(a.n, ROWS)), TPR > 256 ? TPR : 256, 0, st>>>(a);
+  };
+  using std::integral_constant;
+  if (chunks <= 64) go(integral_constant<int, 64>{}, integral_constant<int, 1>{});
+  else if (chunks <= 256) go(integral_constant<int, 256>{}, integral_constant<int, 1>{});
+  else if (chunks <= 512) go(integral_constant<int, 256>{}, integral_constant<int, 2>{});
+  else if (chunks <= 1024) go(integral_constant<int, 256>{}, integral_constant<int, 4>{});
+  else if (chunks <= 2048) go(integral_constant<int, 1024>{}, integral_constant<int, 2>{});
+  else go(integral_constant<int, 1024>{}, integral_constant<int, 4>{});
+  return launch_ok() ? KT_OK : fail(KT_ERR_DEVICE, "norm kernel launch failed");
+}
+template <typename T, typename TG>
+static kt_status dispatch_norm(const NormArgs& a, int format, hipStream_t st) {
+  switch (format) {
+    case KT_Q_NONE: return launch_norm<T, TG, kFormatNone>(a, st);
+    case KT_Q_INT4: return launch_norm<T, TG, kFormatInt4>(a, st);
+    case KT_Q_INT8: return launch_norm<T, TG, kFormatInt8>(a, st);
+    default: return launch_norm<T, TG, kFormatE4M3>(a, st);
+  }
+}
+
+// ------------------------------------------------------------------ cache ---------
+static int log2_of(int64_t v) {
+  int b = 0;
+  while (((int64_t)1 << b) < v) ++b;
+  return b;
+}
+
+// f(integral_constant<KV>, integral_constant<HD>)
+template <class F>
+static auto with_cache(const kt_kv_cache* c, F f) {
+  using std::integral_constant;
+  auto hd = [&](auto kv) {
+    if (c->head_dim == 64) return f(kv, integral_constant<int, 64>{});
+    if (c->head_dim == 128) return f(kv, integral_constant<int, 128>{});
+    return f(kv, integral_constant<int, 256>{});
+  };
+  if (c->format == KT_KV_BF16) return hd(integral_constant<int, kKvBf16>{});
+  if (c->format == KT_KV_U8) return hd(integral_constant<int, kKvU8>{});
+  return hd(integral_constant<int, kKvU4>{});
+}
+
+static kt_status check_cache_shape(const kt_kv_cache* c) {
+  if (!c) return fail(KT_ERR_INVALID_ARG, "cache must not be null");
+  if (c->format != KT_KV_BF16 && c->format != KT_KV_U8 && c->format != KT_KV_U4)
+    return fail(KT_ERR_BAD_DTYPE, "cache format must be KT_KV_BF16, KT_KV_U8 or KT_KV_U4");
+  if (c->head_dim != 64 && c->head_dim != 128 && c->head_dim != 256)
+    return fail(KT_ERR_NOT_SUPPORTED, "head_dim = %lld: heads of 64, 128 or 256 features", (long long)c->head_dim);
+  if (c->n_pages < 1 || c->n_pages > ((int64_t)1 << 31) - 1) return fail(KT_ERR_BAD_SHAPE, "n_pages must be in [1, 2^31)");
+  if (c->n_heads < 1 || c->n_heads > 1024) return fail(KT_ERR_BAD_SHAPE, "n_heads must be in [1, 1024]");
+  if (c->page_size < 64 || c->page_size > 65536 || (c->page_size & (c->page_size - 1)))
+    return fail(KT_ERR_BAD_SHAPE, "page_size = %lld: a power of two from 64 to 65536", (long long)c->page_size);
+  return KT_OK;
+}
+static kt_status check_cache(const kt_kv_cache* c) {
+  if (kt_status s = check_cache_shape(c)) return s;
+  if (!c->data) return fail(KT_ERR_INVALID_ARG, "cache data must not be null");
+  if (misaligned(c->data, 16)) return fail(KT_ERR_BAD_SHAPE, "cache data must be 16-byte aligned");
+  return KT_OK;
+}
+static KvCache device_cache(const kt_kv_cache* c) {
+  return KvCache{static_cast<char*>(c->data), c->n_pages, (int)c->n_heads, log2_of(c->page_size)};
+}
+
+// ------------------------------------------------------------------ attention -----
+// Waves that share the key tiles of a call: two workgroups of four a CU.
+constexpr int64_t kWorkers = (int64_t)kNumCUs * 8;
+constexpr int64_t kMaxSequences = 4096;  // their tile counts are listed in LDS
+
+static size_t part_bytes(int64_t hd) { return (size_t)(2 * kWorkers * kRows * (hd + 2) * 4); }
+static size_t whole_bytes(int64_t n_tokens, int64_t hq, int64_t hd) { return (size_t)round_up(n_tokens * hq * (hd + 2) * 4, 256); }
+
+}  // namespace kt
+
+using namespace kt;
+
+extern "C" {
+
+kt_status kt_add_rmsnorm_quant(const void* X, int64_t ldx, const void* res, int64_t ldres, const void* gain, int64_t n, int64_t d,
+                               kt_dtype dtype, kt_dtype gain_dtype, float eps, float clip_ratio, kt_qformat format, void* res_out,
+                               int64_t ldro, void* Y, int64_t ldy, void* codes, int64_t ldc, float* scales, void* stream) {
+  clear_error();
+  if (!X) return fail(KT_ERR_INVALID_ARG, "X must not be null");
+  if (!res_out && !Y && !codes && !scales) return fail(KT_ERR_INVALID_ARG, "no output requested");
+  if (n < 1 || n > ((int64_t)1 << 31) - 1) return fail(KT_ERR_INVALID_ARG, "n must be in [1, 2^31)");
+  if (d < 8 || d > 32768 || d % 8) return fail(KT_ERR_BAD_SHAPE, "d = %lld: a multiple of 8 up to 32768", (long long)d);
+  if (dtype != KT_F32 && dtype != KT_BF16) return fail(KT_ERR_BAD_DTYPE, "dtype must be KT_F32 or KT_BF16");
+  if (gain && gain_dtype != KT_F32 && gain_dtype != KT_BF16) return fail(KT_ERR_BAD_DTYPE, "gain_dtype must be KT_F32 or KT_BF16");
+  if (format != KT_Q_NONE && format != KT_Q_INT4 && format != KT_Q_INT8 && format != KT_Q_E4M3)
+    return fail(KT_ERR_BAD_DTYPE, "format must be KT_Q_NONE, KT_Q_INT4, KT_Q_INT8 or KT_Q_E4M3");
+  if (format == KT_Q_NONE && (codes || scales)) return fail(KT_ERR_INVALID_ARG, "KT_Q_NONE has neither codes nor scales");
+  if (!(eps >= 0.f) || !(eps <= kHuge)) return fail(KT_ERR_INVALID_ARG, "eps must be finite and not negative");
+  if (!(clip_ratio > 0.f) || !(clip_ratio <= 1.f)) return fail(KT_ERR_INVALID_ARG, "clip_ratio must be in (0, 1]");
+  if (!rows_ok(X, ldx, d, dtype) || (res && !rows_ok(res, ldres, d, dtype)) || (res_out && !rows_ok(res_out, ldro, d, dtype)) ||
+      (Y && !rows_ok(Y, ldy, d, dtype)))
+    return fail(KT_ERR_BAD_SHAPE, "leading dimensions must be in [d, 2^24] and keep rows 16-byte aligned");
+  if (gain && misaligned(gain, 16)) return fail(KT_ERR_BAD_SHAPE, "gain must be 16-byte aligned");
+  if (codes && (ldc < d || ldc > ((int64_t)1 << 24) || ldc % 8 || misaligned(codes, 8)))
+    return fail(KT_ERR_BAD_SHAPE, "ldc must be a multiple of 8 in [d, 2^24], codes 8-byte aligned");
+  NormArgs a{X, res, gain, res_out, Y, static_cast<uint8_t*>(codes), scales, ldx, ldres, ldro, ldy, ldc, (int)n, (int)d, eps, clip_ratio,
+             format == KT_Q_INT4 ? 7.f : format == KT_Q_INT8 ? 127.f : 448.f};
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  if (dtype == KT_F32) return gain && gain_dtype == KT_BF16 ? dispatch_norm<float, bf16>(a, format, st) : dispatch_norm<float, float>(a, format, st);
+  return gain && gain_dtype == KT_F32 ? dispatch_norm<bf16, float>(a, format, st) : dispatch_norm<bf16, bf16>(a, format, st);
+}
+
+size_t kt_kv_cache_bytes(const kt_kv_cache* cache) {
+  if (check_cache_shape(cache) != KT_OK) return 0;
+  return with_cache(cache, [&](auto kv, auto hd) {
+    const size_t block = kv_block_bytes<decltype(kv)::value, decltype(hd)::value>(), blocks = (size_t)cache->n_heads * (cache->page_size / 64);
+    // sizes that no address space holds count as bad
+    return (size_t)cache->n_pages > (((size_t)1 << 47) / block) / blocks ? (size_t)0 : (size_t)cache->n_pages * blocks * block;
+  });
+}
+
+kt_status kt_kv_append(const kt_kv_cache* cache, const void* Q, int64_t ldq, const void* K, int64_t ldk, const void* V, int64_t ldv,
+                       int64_t n, int64_t n_q_heads, kt_dtype dtype, const int64_t* slots, const int32_t* positions, const float* rope,
+                       int64_t n_pos, int64_t rot_dim, int32_t interleaved, int32_t hadamard, void* Q_out, int64_t ldqo, void* stream) {
+  clear_error();
+  if (kt_status s = check_cache(cache)) return s;
+  if (!K || !V || !slots) return fail(KT_ERR_INVALID_ARG, "K, V and slots must not be null");
+  if (n < 1 || n > ((int64_t)1 << 31) - 1) return fail(KT_ERR_INVALID_ARG, "n must be in [1, 2^31)");
+  if (dtype != KT_F32 && dtype != KT_BF16) return fail(KT_ERR_BAD_DTYPE, "dtype must be KT_F32 or KT_BF16");
+  if (!Q != !Q_out) return fail(KT_ERR_INVALID_ARG, "Q and Q_out go together");
+  if (Q ? n_q_heads < 1 || n_q_heads > 65536 : n_q_heads != 0) return fail(KT_ERR_BAD_SHAPE, "n_q_heads must be in [1, 65536], or 0 without Q");
+  const int64_t hd = cache->head_dim;
+  if ((Q && (!rows_ok(Q, ldq, n_q_heads * hd, dtype) || !rows_ok(Q_out, ldqo, n_q_heads * hd, dtype))) ||
+      !rows_ok(K, ldk, cache->n_heads * hd, dtype) || !rows_ok(V, ldv, cache->n_heads * hd, dtype))
+    return fail(KT_ERR_BAD_SHAPE, "leading dimensions must be in [heads * head_dim, 2^24] and keep rows 16-byte aligned");
+  if (rope) {
+    if (!positions) return fail(KT_ERR_INVALID_ARG, "positions must not be null with a rope table");
+    if (rot_dim < 16 || rot_dim > hd || rot_dim % 16) return fail(KT_ERR_BAD_SHAPE, "rot_dim = %lld: a multiple of 16 up to head_dim", (long long)rot_dim);
+    if (n_pos < 1) return fail(KT_ERR_INVALID_ARG, "n_pos must be positive");
+    if (misaligned(rope, 16)) return fail(KT_ERR_BAD_SHAPE, "rope must be 16-byte aligned");
+  }
+  if (misaligned(slots, 8) || misaligned(positions, 4)) return fail(KT_ERR_BAD_SHAPE, "slots and positions must be aligned to their type");
+  AppendArgs a{device_cache(cache), Q, K, V, Q_out, ldq, ldk, ldv, ldqo, slots, positions, rope, n_pos, (int)n, (int)n_q_heads,
+               rope ? (int)rot_dim : 0, interleaved != 0, hadamard != 0};
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  const int64_t wgs = ceil_div(n * (n_q_heads + 2 * cache->n_heads), 256 / (hd / 8));
+  if (wgs > INT32_MAX) return fail(KT_ERR_NOT_SUPPORTED, "too many rows for one call");
+  with_cache(cache, [&](auto kv, auto h) {
+    constexpr int KV = decltype(kv)::value, HD = decltype(h)::value;
+    if (dtype == KT_F32) kv_append_kernel<float, KV, HD><<<dim3((unsigned)wgs), 256, 0, st>>>(a);
+    else kv_append_kernel<bf16, KV, HD><<<dim3((unsigned)wgs), 256, 0, st>>>(a);
+  });
+  return launch_ok() ? KT_OK : fail(KT_ERR_DEVICE, "append kernel launch failed");
+}
+
+kt_status kt_kv_gather(const kt_kv_cache* cache, const int64_t* slots, int64_t n, void* K, int64_t ldk, void* V, int64_t ldv, kt_dtype dtype,
+                       void* stream) {
+  clear_error();
+  if (kt_status s = check_cache(cache)) return s;
+  if (!slots || (!K && !V)) return fail(KT_ERR_INVALID_ARG, "slots and one of K, V must not be null");
+  if (n < 1 || n > ((int64_t)1 << 31) - 1) return fail(KT_ERR_INVALID_ARG, "n must be in [1, 2^31)");
+  if (dtype != KT_F32 && dtype != KT_BF16) return fail(KT_ERR_BAD_DTYPE, "dtype must be KT_F32 or KT_BF16");
+  const int64_t hd = cache->head_dim;
+  if ((K && !rows_ok(K, ldk, cache->n_heads * hd, dtype)) || (V && !rows_ok(V, ldv, cache->n_heads * hd, dtype)))
+    return fail(KT_ERR_BAD_SHAPE, "leading dimensions must be in [heads * head_dim, 2^24] and keep rows 16-byte aligned");
+  if (misaligned(slots, 8)) return fail(KT_ERR_BAD_SHAPE, "slots must be aligned to their type");
+  GatherArgs a{device_cache(cache), slots, K, V, ldk, ldv, (int)n};
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  const int64_t wgs = ceil_div(n * 2 * cache->n_heads, 256 / (hd / 8));
+  if (wgs > INT32_MAX) return fail(KT_ERR_NOT_SUPPORTED, "too many rows for one call");
+  with_cache(cache, [&](auto kv, auto h) {
+    constexpr int KV = decltype(kv)::value, HD = decltype(h)::value;
+    if (dtype == KT_F32) kv_gather_kernel<float, KV, HD><<<dim3((unsigned)wgs), 256, 0, st>>>(a);
+    else kv_gather_kernel<bf16, KV, HD><<<dim3((unsigned)wgs), 256, 0, st>>>(a);
+  });
+  return launch_ok() ? KT_OK : fail(KT_ERR_DEVICE, "gather kernel launch failed");
+}
+
+size_t kt_paged_attention_bytes(int64_t n_tokens, int64_t n_q_heads, int64_t head_dim, int64_t prefix_len) {
+  if (n_tokens < 1 || n_tokens > INT32_MAX || n_q_heads < 1 || n_q_heads > 65535 || (head_dim != 64 && head_dim != 128 && head_dim != 256) ||
+      prefix_len < 0)
+    return 0;
+  const size_t one = part_bytes(head_dim);
+  return prefix_len ? 2 * (one + whole_bytes(n_tokens, n_q_heads, head_dim)) : one;
+}
+
+kt_status kt_paged_attention(const kt_kv_cache* cache, const void* Q, int64_t ldq, kt_dtype dtype, const int32_t* q_starts, const int32_t* lens,
+                             const int32_t* pages, int64_t ldp, int64_t n_seq, int64_t n_tokens, int64_t max_q, int64_t n_q_heads,
+                             const int32_t* prefix_pages, int64_t prefix_len, float scale, void* O, int64_t ldo, float* lse,
+                             void* workspace, size_t workspace_bytes, void* stream) {
+  clear_error();
+  if (kt_status s = check_cache(cache)) return s;
+  if (!Q || !lens || !pages || !O) return fail(KT_ERR_INVALID_ARG, "Q, lens, pages and O must not be null");
+  if (dtype != KT_BF16) return fail(KT_ERR_BAD_DTYPE, "dtype must be KT_BF16");
+  if (n_seq < 1 || n_tokens < 1 || n_tokens > INT32_MAX || max_q < 1) return fail(KT_ERR_INVALID_ARG, "n_seq, n_tokens and max_q must be positive");
+  if (n_seq > kMaxSequences) return fail(KT_ERR_NOT_SUPPORTED, "n_seq = %lld: at most %lld sequences a call", (long long)n_seq, (long long)kMaxSequences);
+  if (!q_starts && (n_tokens != n_seq || max_q != 1)) return fail(KT_ERR_INVALID_ARG, "without q_starts every sequence has one query");
+  const int64_t hd = cache->head_dim;
+  if (n_q_heads < 1 || n_q_heads > 65535 || n_q_heads % cache->n_heads)
+    return fail(KT_ERR_BAD_SHAPE, "n_q_heads must be a multiple of the cache's heads, at most 65535");
+  if (!rows_ok(Q, ldq, n_q_heads * hd, dtype) || ldo < n_q_heads * hd || ldo > ((int64_t)1 << 24) || ldo % 4 || misaligned(O, 8))
+    return fail(KT_ERR_BAD_SHAPE, "leading dimensions must be in [heads * head_dim, 2^24], rows of Q 16-byte and of O 8-byte aligned");
+  if (ldp < 1 || ldp * cache->page_size > INT32_MAX) return fail(KT_ERR_BAD_SHAPE, "ldp must be positive, ldp * page_size below 2^31");
+  if (prefix_len < 0 || prefix_len > INT32_MAX || (prefix_len && !prefix_pages))
+    return fail(KT_ERR_INVALID_ARG, "prefix_len must be in [0, 2^31), with prefix_pages");
+  if (!(scale > 0.f) || !(scale <= kHuge)) return fail(KT_ERR_INVALID_ARG, "scale must be positive and finite");
+  const size_t need = kt_paged_attention_bytes(n_tokens, n_q_heads, hd, prefix_len);
+  if (!workspace || workspace_bytes < need)
+    return fail(KT_ERR_WORKSPACE_TOO_SMALL, "workspace of %zu bytes needed, %zu given", need, workspace ? workspace_bytes : (size_t)0);
+  if (misaligned(workspace, 256)) return fail(KT_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
+  if (misaligned(q_starts, 4) || misaligned(lens, 4) || misaligned(pages, 4) || misaligned(prefix_pages, 4) || misaligned(lse, 4))
+    return fail(KT_ERR_BAD_SHAPE, "index arrays and lse must be aligned to their type");
+
+  char* ws = static_cast<char*>(workspace);
+  auto take = [&](size_t bytes) {
+    float* p = reinterpret_cast<float*>(ws);
+    ws += bytes;
+    return p;
+  };
+  AttendArgs own{};
+  own.cache = device_cache(cache);
+  own.q = static_cast<const bf16*>(Q);
+  own.q_starts = q_starts;
+  own.lens = lens;
+  own.pages = pages;
+  own.ldq = ldq;
+  own.ldp = ldp;
+  own.n_seq = (int)n_seq;
+  own.n_tokens = (int)n_tokens;
+  own.hq = (int)n_q_heads;
+  own.group = (int)(n_q_heads / cache->n_heads);
+  own.workers = (int)kWorkers;
+  own.scale = scale;
+  own.out = static_cast<bf16*>(O);
+  own.ldo = ldo;
+  own.lse = lse;
+  own.part = take(part_bytes(hd));
+  own.whole = prefix_len ? take(whole_bytes(n_tokens, n_q_heads, hd)) : nullptr;
+  own.causal = true;
+  JoinArgs join{own, AttendArgs{}};
+  if (prefix_len) {
+    AttendArgs& p = join.prefix = own;
+    p.q_starts = p.lens = nullptr;
+    p.pages = prefix_pages;
+    p.ldp = ceil_div(prefix_len, cache->page_size);
+    p.fixed_len = prefix_len;
+    p.n_seq = 1;
+    p.part = take(part_bytes(hd));
+    p.whole = take(whole_bytes(n_tokens, n_q_heads, hd));
+    p.causal = false;
+  }
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  const size_t lds = (size_t)(n_seq + 1) * 8;
+  with_cache(cache, [&](auto kv, auto h) {
+    constexpr int KV = decltype(kv)::value, HD = decltype(h)::value;
+    if (prefix_len) attend_rows_kernel<KV, HD><<<dim3(kWorkers / 4), 256, 16, st>>>(join.prefix);
+    attend_rows_kernel<KV, HD><<<dim3(kWorkers / 4), 256, lds, st>>>(own);
+    attend_join_kernel<HD><<<dim3((unsigned)n_tokens, (unsigned)n_q_heads), 256, lds, st>>>(join);
+  });
+  return launch_ok() ? KT_OK : fail(KT_ERR_DEVICE, "attention kernel launch failed");
+}
+
+}  // extern "C"
