@@ -458,7 +458,7 @@ kt_status kt_kv_gather(const kt_kv_cache* cache, const int64_t* slots, int64_t n
  *  lse      [n_tokens][n_q_heads] fp32 or NULL: log sum_j exp(scale * q . k_j).
  * A query that sees nothing gives 0, and -inf in lse.  Scores, statistics and sums are fp32, the p_j are rounded to bf16 in front of
  * their product with the values.  All index arrays are on the device: the call can be captured and replayed with other
- * lengths and pages.  n_seq <= 4096, ldp * page_size < 2^31, scale > 0.
+ * lengths and pages.  n_seq <= 4096, ldp * page_size and prefix_len <= 2^30, scale > 0.
  * Workspace: kt_paged_attention_bytes(n_tokens, n_q_heads, head_dim, prefix_len).
  */
 kt_status kt_paged_attention(const kt_kv_cache* cache, const void* Q, int64_t ldq, kt_dtype dtype, const int32_t* q_starts,

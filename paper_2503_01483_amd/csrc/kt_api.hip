@@ -38,7 +38,7 @@ kt_status fail(kt_status code, const char* fmt, ...) {
 // Kernels that use more than 64 KiB of dynamic LDS need the limit raised once per kernel AND per
 // device (the attribute belongs to the device's copy of the code).  Remembers what has been set;
 // safe to call from several host threads.
-static bool ensure_dynamic_lds(const void* kernel, size_t bytes) {
+bool ensure_dynamic_lds(const void* kernel, size_t bytes) {
   struct Entry { const void* kernel; int device; size_t bytes; };
   static std::mutex mu;
   static std::vector<Entry> done;

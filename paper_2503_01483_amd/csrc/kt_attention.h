@@ -8,13 +8,13 @@
 // holds the scores of one row and of 16 keys that lie next to each other in its column of V^T: after the exponentials the scores ARE
 // the operand of O^T = V^T P^T.  Nothing goes through LDS but the quantisers' parameters, no wave waits for another.
 // All key tiles of all segments form one list, and every wave takes an equal piece of it, whatever the lengths: a segment that is
-// cut leaves {O, max, sum} of each piece in the workspace, and attend_join_kernel puts them together.
+// cut leaves {O, max, sum} of each piece in the workspace, and a second launch puts them together.
 //
 // Quantised rows are never expanded: k = s c + b gives q . k = s (q . c) + b sum(q), and v = s c + b gives p v = (p s) c + p b, so that the
-// codes themselves, exact in bf16, are the operands.  A 4-bit code becomes 128 + c by OR (0x4300 | c), two at a time; what the 128
-// adds is taken off again with the same rounded p s (a row of ones in V^T), so that it costs no accuracy, and with 8 more the codes
-// are centred, which keeps the rounding of p s to bf16 as small as that of p would be against plain values.
-// Held in fp32: scores, running maximum, sum of p, O.  Rounded to bf16: p (or p s), 2^-9 of a term each, in both signs.
+// codes themselves, exact in bf16, are the operands.  A 4-bit code becomes 128 + c by OR (0x4300 | c), two at a time; a product of
+// the same rounded p s with a constant takes 136 (u8: 128) off again within the tile, which leaves the codes centred and costs no accuracy.
+// Held in fp32: scores, running maximum, sum of p, O.  Rounded to bf16: p, 2^-8 of a term, in both signs; p s goes in as the sum of two bf16
+// (2^-16): the product has room for it beside the memory.
 #pragma once
 #include "kt_kvcache.h"
 
@@ -25,78 +25,69 @@ constexpr int kRows = 16;  // rows of a segment
 struct AttendArgs {
   KvCache cache;
   const bf16* q;
-  const int *q_starts, *lens, *pages;  // q_starts null: token i is the only query of sequence i; lens null: `fixed_len` for all
-  int64_t ldq, ldp, fixed_len;
+  const int *q_starts, *lens, *pages;  // q_starts null: token i is the only query of sequence i
+  int64_t ldq, ldp;
   int n_seq, n_tokens, hq, group;
-  int workers;  // waves that take pieces
   float scale;
   bf16* out;
   int64_t ldo;
   float* lse;
+  // workspace
+  int workers;   // waves that take pieces of the list
+  int* tiles;    // [n_seq + 1] key tiles of one head in front of each sequence
+  int4* cuts;    // [workers] the segment whose first piece a worker has while others have the rest: {first token, rows, head, pieces or 0}
   float* part;   // pieces of cut segments: O [2 workers][kRows][HD], then {max in bits, sum} [2 workers][kRows]
   float* whole;  // null: whole segments go to out.  Else something is to be joined: O [n_tokens][hq][HD], then {max, sum} [n_tokens][hq]
-  bool causal;
 };
 
 // First token and number of a sequence's queries, and its tokens in the cache.
 struct Sequence {
-  int first, count;
-  int64_t len;
+  int first, count, len;
 };
 __device__ __forceinline__ Sequence sequence_of(const AttendArgs& a, int s) {
-  Sequence q;
+  Sequence q{s, 1, 0};
   if (a.q_starts) {
-    const int b = a.q_starts[s], e = a.q_starts[s + 1];
-    q.first = min(max(b, 0), a.n_tokens);
-    q.count = min(max(e - q.first, 0), a.n_tokens - q.first);
-  } else if (a.lens) {
-    q.first = s;
-    q.count = 1;
-  } else {
-    q.first = 0;
-    q.count = a.n_tokens;
+    q.first = min(max(a.q_starts[s], 0), a.n_tokens);
+    q.count = min(max(a.q_starts[s + 1] - q.first, 0), a.n_tokens - q.first);
   }
-  const int64_t room = a.ldp << a.cache.log2_page;
-  q.len = a.lens ? min((int64_t)max(a.lens[s], 0), room) : a.fixed_len;
+  q.len = min(max(a.lens[s], 0), (int)(a.ldp << a.cache.log2_page));
   return q;
 }
-__device__ __forceinline__ int64_t key_tiles(const Sequence& q) { return max((int64_t)1, (q.len + 63) >> 6); }
-__device__ __forceinline__ int row_tiles(const AttendArgs& a, const Sequence& q) {
-  return (int)(((int64_t)q.count * a.group + kRows - 1) / kRows);
-}
+__device__ __forceinline__ int key_tiles(const Sequence& q) { return max(1, (int)(((unsigned)q.len + 63) >> 6)); }
 
-// Key tiles of the sequences in front of each, into `cum` [n_seq + 1] (LDS), by a workgroup of 256.
-__device__ __forceinline__ void list_tiles(const AttendArgs& a, int64_t* cum) {
-  __shared__ int64_t wave_sum[4];
+// Key tiles of one head in front of each sequence, `cum` [n_seq + 1] (LDS), by a workgroup of 256.  A sequence of more than kRows rows
+// breaks the caller's bound: its first kRows are computed.
+__device__ __forceinline__ void list_tiles(const AttendArgs& a, int* cum) {
+  __shared__ int wave_sum[4];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  int64_t carry = 0;
+  int carry = 0;
   for (int base = 0; base < a.n_seq; base += 256) {
     const int s = base + threadIdx.x;
-    int64_t mine = 0;
+    int mine = 0;
     if (s < a.n_seq) {
       const Sequence q = sequence_of(a, s);
-      mine = key_tiles(q) * row_tiles(a, q) * a.cache.n_heads;
+      mine = q.count ? key_tiles(q) : 0;
     }
-    int64_t upto = mine;
+    int upto = mine;
 #pragma unroll
     for (int o = 1; o < 64; o *= 2) {
-      const int64_t t = __shfl_up(upto, o);
+      const int t = __shfl_up(upto, o);
       if (lane >= o) upto += t;
     }
     if (lane == 63) wave_sum[wave] = upto;
     __syncthreads();
-    int64_t before = carry;
+    int before = carry;
     for (int w = 0; w < wave; ++w) before += wave_sum[w];
     if (s < a.n_seq) cum[s] = before + upto - mine;
     carry += wave_sum[0] + wave_sum[1] + wave_sum[2] + wave_sum[3];
-    __syncthreads();
+    if (base + 256 < a.n_seq) __syncthreads();
   }
   if (threadIdx.x == 0) cum[a.n_seq] = carry;
   __syncthreads();
 }
 
-// The sequence that tile u of the list belongs to.
-__device__ __forceinline__ int sequence_at(const int64_t* cum, int n_seq, int64_t u) {
+// The last sequence that starts at or before place u of the list.
+__device__ __forceinline__ int sequence_at(const int* cum, int n_seq, int u) {
   int lo = 0, hi = n_seq - 1;
   while (lo < hi) {
     const int mid = (lo + hi + 1) >> 1;
@@ -105,11 +96,9 @@ __device__ __forceinline__ int sequence_at(const int64_t* cum, int n_seq, int64_
   }
   return lo;
 }
-
-__device__ __forceinline__ int64_t uniform64(int64_t v) {
-  return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)v) |
-                   (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32);
-}
+// Tiles of a worker's piece of a list of `total` (worker w has [w n, (w + 1) n)).
+__device__ __forceinline__ int piece_length(int total, int workers) { return max(1, (int)(((unsigned)total + workers - 1) / (unsigned)workers)); }
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
 // 8 codes of 4 bits as bf16 128 + c: elements 2 i, 2 i + 1 in dword i.
 __device__ __forceinline__ bf16x8 spread_nibbles(uint32_t x) {
@@ -204,63 +193,76 @@ struct Tile64 {
   }
 };
 
+// What has to be added to O where a value that not all rows of a tile see is not finite: products take such values as 0.  Feature `at` of
+// values `v` [feature][64].
+__device__ __forceinline__ float unfinite(const bf16* v, int at, int seen) {
+  float sum = 0.f;
+  for (int j = 0; j < seen; ++j) {
+    const float x = (float)v[at * kBlockTokens + j];
+    if (!(fabsf(x) <= kHuge)) sum += x;
+  }
+  return sum;
+}
+
+// The list's order: sequences, in each its heads, in each its tiles.
 template <int KV, int HD>
 __global__ __launch_bounds__(256) void attend_rows_kernel(AttendArgs a) {
-  extern __shared__ int64_t cum[];
+  extern __shared__ int cum[];
   __shared__ float4 params[4][64];
   constexpr int TD = HD / 16;
   constexpr float kOffset = KV == kKvU4 ? 136.f : 128.f, kCentre = KV == kKvU4 ? 8.f : 128.f;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, g = lane >> 4;
-  list_tiles(a, cum);
-  const int64_t total = cum[a.n_seq], workers = min((int64_t)a.workers, total);
-  const int64_t me = (int64_t)blockIdx.x * 4 + wave;
-  if (me >= workers) return;
-  int64_t u = uniform64(me * total / workers);
-  const int64_t end = uniform64((me + 1) * total / workers), begin = u;
-  const float c = a.scale * 1.44269504f;
   constexpr float kNone = -__builtin_inff();
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, g = lane >> 4, heads = a.cache.n_heads;
+  list_tiles(a, cum);
+  if (blockIdx.x == 0 && a.whole)
+    for (int s = threadIdx.x; s <= a.n_seq; s += 256) a.tiles[s] = cum[s];
+  const int total = cum[a.n_seq] * heads, per = uniform(piece_length(total, a.workers));
+  const int me = uniform(blockIdx.x * 4 + wave), begin = me * per, end = min(begin + per, total);
+  const float c = a.scale * 1.44269504f;
+  const int page_blocks = a.cache.log2_page - 6;
+  int4 cut = {0, 0, 0, 0};
 
-  while (u < end) {
+  for (int u = begin; u < end;) {
     // the segment that tile u belongs to, and this wave's tiles of it
-    const int s = __builtin_amdgcn_readfirstlane(sequence_at(cum, a.n_seq, u));
+    const int s = uniform(sequence_at(cum, a.n_seq, (int)((unsigned)u / (unsigned)heads)));
     const Sequence q = sequence_of(a, s);
-    const int64_t tiles = uniform64(key_tiles(q)), rel = u - cum[s];
-    const int64_t segment = uniform64(rel / tiles), start = cum[s] + segment * tiles;
-    const int row_tile = (int)(segment / a.cache.n_heads), head = (int)(segment - (int64_t)row_tile * a.cache.n_heads);
-    int64_t tile = uniform64(u - start);
-    const int64_t last = uniform64(min(tiles, end - start)), first = tile;
+    const int tiles = uniform(key_tiles(q)), rel = u - uniform(cum[s]) * heads;
+    const int head = uniform((int)((unsigned)rel / (unsigned)tiles)), start = u - (rel - head * tiles);
+    const int first = u - start, last = min(tiles, end - start);
 
     // this lane's row
-    const int64_t row = (int64_t)row_tile * kRows + r;
-    const int in_seq = (int)(row / a.group), qh = head * a.group + (int)(row - (int64_t)in_seq * a.group);
+    const int in_seq = r / a.group, qh = head * a.group + (r - in_seq * a.group);
     const bool live = in_seq < q.count;
     const int64_t token = q.first + (live ? in_seq : 0);
-    const int64_t sees = a.causal ? min(max(q.len - q.count + in_seq + 1, (int64_t)0), q.len) : q.len;
-    const int64_t all_see = a.causal ? q.len - q.count + (int64_t)row_tile * kRows / a.group + 1 : q.len;  // what every row of the tile sees
+    const int sees = min(max(q.len - q.count + in_seq + 1, 0), q.len), all_see = q.len - q.count + 1;
     bf16x8 qf[HD / 32];
     float qsum = 0.f;
 #pragma unroll
     for (int w = 0; w < HD / 32; ++w) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) qf[w][e] = (bf16)0.f;
-      if (live) qf[w] = *reinterpret_cast<const bf16x8*>(a.q + token * a.ldq + (int64_t)qh * HD + 32 * w + 8 * g);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) qsum += (float)qf[w][e];
+      if (live) qf[w] = *reinterpret_cast<const bf16x8*>(a.q + token * a.ldq + qh * HD + 32 * w + 8 * g);
     }
-    qsum = quarters_sum(qsum);
+    if constexpr (KV != kKvBf16) {
+#pragma unroll
+      for (int w = 0; w < HD / 32; ++w)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) qsum += (float)qf[w][e];
+      qsum = quarters_sum(qsum);
+    }
 
-    f32x4 o[TD], ones_acc = {0.f, 0.f, 0.f, 0.f};
+    f32x4 o[TD];
 #pragma unroll
     for (int i = 0; i < TD; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
     float m = kNone, l = 0.f, low = 0.f;
-    const int* pages = a.pages + (a.lens ? s * a.ldp : 0);
+    const int* pages = a.pages + s * a.ldp;
     Tile64<KV, HD> t64;
 
-    for (; tile < last; ++tile) {
+    for (int tile = first; tile < last; ++tile) {
       if (tile * 64 >= q.len) break;
-      const int64_t page = pages[tile >> (a.cache.log2_page - 6)];
+      const int64_t page = pages[tile >> page_blocks];
       if (page < 0 || page >= a.cache.n_pages) continue;  // a page outside the cache holds nothing to see
-      const char* block = a.cache.data + kv_block_offset<KV, HD>(a.cache, page, head, (int)(tile & ((1 << (a.cache.log2_page - 6)) - 1)));
+      const char* block = a.cache.data + kv_block_offset<KV, HD>(a.cache, page, head, tile & ((1 << page_blocks) - 1));
       t64.load_keys(block, lane);
       t64.load_values(block, lane);
 
@@ -292,7 +294,7 @@ __global__ __launch_bounds__(256) void attend_rows_kernel(AttendArgs a) {
         __builtin_amdgcn_wave_barrier();
       }
       const bool masked = tile * 64 + 64 > all_see;
-      const int seen = (int)min(max(sees - tile * 64, (int64_t)0), (int64_t)64);
+      const int seen = min(max(sees - tile * 64, 0), 64);
       if (masked) {
 #pragma unroll
         for (int t = 0; t < 4; ++t)
@@ -300,36 +302,43 @@ __global__ __launch_bounds__(256) void attend_rows_kernel(AttendArgs a) {
           for (int i = 0; i < 4; ++i)
             if (Tile64<KV, HD>::token(t, 4 * g + i) >= seen) x[t][i] = kNone;
       }
-      float most = fmaxf(fmaxf(fmaxf(x[0][0], x[0][1]), fmaxf(x[0][2], x[0][3])), fmaxf(fmaxf(x[1][0], x[1][1]), fmaxf(x[1][2], x[1][3])));
-      most = fmaxf(most, fmaxf(fmaxf(fmaxf(x[2][0], x[2][1]), fmaxf(x[2][2], x[2][3])), fmaxf(fmaxf(x[3][0], x[3][1]), fmaxf(x[3][2], x[3][3]))));
-      most = fmaxf(m, quarters_max(most));
-      const float mc = most == kNone ? 0.f : most * c;
-      const float shrink = __builtin_amdgcn_exp2f(fmaf(m, c, -mc));
-      m = most;
-      l *= shrink;
-      low *= shrink;
-      ones_acc *= shrink;
+      float most = m;
 #pragma unroll
-      for (int i = 0; i < TD; ++i) o[i] *= shrink;
+      for (int t = 0; t < 4; ++t) most = fmaxf(most, fmaxf(fmaxf(x[t][0], x[t][1]), fmaxf(x[t][2], x[t][3])));
+      most = quarters_max(most);
+      const float mc = most == kNone ? 0.f : most * c;
+      if (__any(most > m)) {
+        const float shrink = __builtin_amdgcn_exp2f(fmaf(m, c, -mc));
+        l *= shrink;
+        low *= shrink;
+#pragma unroll
+        for (int i = 0; i < TD; ++i) o[i] *= shrink;
+        m = most;
+      }
       bf16x8 pf[2];
+      [[maybe_unused]] bf16x8 rest[2];  // what rounding p s leaves
+      float sum[4] = {0.f, 0.f, 0.f, 0.f};  // (of a tile first: fewer roundings at the size of the whole)
 #pragma unroll
       for (int t = 0; t < 4; ++t)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           float p = __builtin_amdgcn_exp2f(fmaf(x[t][i], c, -mc));
-          l += p;
+          sum[i] += p;
+          const int e = 4 * (t & 1) + i, at = KV == kKvU4 ? (e & 4) | (e & 1) << 1 | (e & 2) >> 1 : e;
           if constexpr (KV != kKvBf16) {
             const float vs = vp[t][i >> 1][2 * (i & 1)], vb = vp[t][i >> 1][2 * (i & 1) + 1];
             const bool off = masked && Tile64<KV, HD>::token(t, 4 * g + i) >= seen;  // parameters of keys that are not seen may be anything
             low = off ? low : fmaf(p, fmaf(kCentre, vs, vb), low);
             p = off ? 0.f : p * vs;
+            rest[t >> 1][at] = (bf16)(p - (float)(bf16)p);
           }
-          const int e = 4 * (t & 1) + i;
-          pf[t >> 1][KV == kKvU4 ? (e & 4) | (e & 1) << 1 | (e & 2) >> 1 : e] = (bf16)p;
+          pf[t >> 1][at] = (bf16)p;
         }
+      l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
       if constexpr (KV == kKvBf16) {
-        if (tile * 64 + 64 > q.len) {  // what lies behind the last token may be anything, and 0 NaN = NaN
-          const int there = (int)(q.len - tile * 64);
+        if (masked) {  // what a row does not see may be anything, and 0 NaN = NaN
+          const int there = q.len - tile * 64;
+          bool odd = false;
 #pragma unroll
           for (int i = 0; i < TD; ++i)
 #pragma unroll
@@ -339,24 +348,48 @@ __global__ __launch_bounds__(256) void attend_rows_kernel(AttendArgs a) {
                 const int at = 32 * j + 8 * g + 2 * w;
                 uint32_t& d = t64.v[i][4 * j + w];
                 d = at >= there ? 0u : at + 1 >= there ? d & 0xffffu : d;
+                if ((d & 0x7f80u) == 0x7f80u) odd = true, d &= 0xffff0000u;
+                if ((d & 0x7f800000u) == 0x7f800000u) odd = true, d &= 0xffffu;
               }
+          if (__any(odd)) {
+            const bf16* v = reinterpret_cast<const bf16*>(block + kv_half_bytes<KV, HD>());
+#pragma unroll
+            for (int i = 0; i < TD; ++i)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) o[i][e] += unfinite(v, 16 * i + 4 * g + e, seen);
+          }
         }
+#pragma unroll
+        for (int i = 0; i < TD; ++i)
+#pragma unroll
+          for (int j = 0; j < 2; ++j) o[i] = mfma16(t64.value(i, j), pf[j], o[i]);
       } else {
-        bf16x8 one;
+        bf16x8 off;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) one[e] = (bf16)1.f;
+        for (int e = 0; e < 8; ++e) off[e] = (bf16)-kOffset;
+        f32x4 shift = {0.f, 0.f, 0.f, 0.f};  // the same in all its rows
 #pragma unroll
-        for (int j = 0; j < 2; ++j) ones_acc = mfma16(one, pf[j], ones_acc);
+        for (int j = 0; j < 2; ++j) {
+          shift = mfma16(off, pf[j], shift);
+          shift = mfma16(off, rest[j], shift);
+        }
+#pragma unroll
+        for (int i = 0; i < TD; ++i) {
+          f32x4 t = shift;
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const bf16x8 v = t64.value(i, j);
+            t = mfma16(v, pf[j], t);
+            t = mfma16(v, rest[j], t);
+          }
+          o[i] += t;
+        }
       }
-#pragma unroll
-      for (int i = 0; i < TD; ++i)
-#pragma unroll
-        for (int j = 0; j < 2; ++j) o[i] = mfma16(t64.value(i, j), pf[j], o[i]);
     }
 
     l = quarters_sum(l);
     if constexpr (KV != kKvBf16) {
-      const float add = quarters_sum(low) - kOffset * ones_acc[0];
+      const float add = quarters_sum(low);
 #pragma unroll
       for (int i = 0; i < TD; ++i) o[i] += add;
     }
@@ -364,7 +397,7 @@ __global__ __launch_bounds__(256) void attend_rows_kernel(AttendArgs a) {
     if (whole && !a.whole) {
       if (live) {
         const float inv = l > 0.f ? 1.f / l : l;  // (NaN stays)
-        bf16* to = a.out + token * a.ldo + (int64_t)qh * HD + 4 * g;
+        bf16* to = a.out + token * a.ldo + qh * HD + 4 * g;
 #pragma unroll
         for (int i = 0; i < TD; ++i) {
           bf16 t[4];
@@ -372,128 +405,77 @@ __global__ __launch_bounds__(256) void attend_rows_kernel(AttendArgs a) {
           for (int e = 0; e < 4; ++e) t[e] = (bf16)(l == 0.f ? 0.f : o[i][e] * inv);
           *reinterpret_cast<u32x2*>(to + 16 * i) = __builtin_bit_cast(u32x2, t);
         }
-        if (a.lse && g == 0) a.lse[token * a.hq + qh] = l == 0.f ? kNone : fmaf(m, a.scale, __logf(l));
+        if (a.lse && g == 0) a.lse[token * a.hq + qh] = l == 0.f ? kNone : (m * c + __log2f(l)) * 0.693147181f;
       }
-    } else if (live) {
-      const int64_t slot = whole ? token * a.hq + qh : (2 * me + (start < begin ? 0 : 1)) * kRows + r;
-      float* base = whole ? a.whole : a.part;
-      float* to = base + slot * HD + 4 * g;
+    } else {
+      if (live) {
+        const int64_t slot = whole ? token * a.hq + qh : (int64_t)(2 * me + (first ? 0 : 1)) * kRows + r;
+        float* base = whole ? a.whole : a.part;
+        float* to = base + slot * HD + 4 * g;
 #pragma unroll
-      for (int i = 0; i < TD; ++i) *reinterpret_cast<f32x4*>(to + 16 * i) = o[i];
-      if (g == 0)
-        reinterpret_cast<float2*>(base + (whole ? (int64_t)a.n_tokens * a.hq : (int64_t)2 * a.workers * kRows) * HD)[slot] =
-            make_float2(l == 0.f ? kNone : m * c, l);
+        for (int i = 0; i < TD; ++i) *reinterpret_cast<f32x4*>(to + 16 * i) = o[i];
+        if (g == 0)
+          reinterpret_cast<float2*>(base + (whole ? (int64_t)a.n_tokens * a.hq : (int64_t)2 * a.workers * kRows) * HD)[slot] =
+              make_float2(l == 0.f ? kNone : m * c, l);
+      }
+      if (first == 0 && !whole)
+        cut = int4{q.first, min(q.count * a.group, kRows), head, (int)((unsigned)(start + tiles - 1) / (unsigned)per) - me + 1};
     }
     u = start + last;
   }
+  if (lane == 0) a.cuts[me] = cut;
 }
 
-struct JoinArgs {
-  AttendArgs own, prefix;  // prefix.workers = 0: none
-};
-
-// Where the pieces of a row lie: workers [begin, end) have one each.
-struct Pieces {
-  const float* o;
-  const float2* ml;
-  int64_t begin, end, start, total, workers, row;  // row: in the segment; of a whole segment (workers = 0): its place in `whole`
-  __device__ __forceinline__ int64_t slot(int64_t w) const {
-    return workers ? (2 * w + (start < w * total / workers ? 0 : 1)) * kRows + row : row;
-  }
-};
+// The pieces of cut segments put together: one segment a workgroup of 256, HD / 4 threads a piece of a row.
 template <int HD>
-__device__ __forceinline__ Pieces pieces_of(const AttendArgs& a, int64_t total, int64_t start, int64_t tiles, int64_t row, int64_t out_row) {
-  Pieces p;
-  p.total = total;
-  p.workers = min((int64_t)a.workers, total);
-  p.start = start;
-  p.row = row;
-  p.begin = ((start + 1) * p.workers - 1) / total;
-  p.end = ((start + tiles) * p.workers - 1) / total + 1;
-  p.o = a.part;
-  p.ml = reinterpret_cast<const float2*>(a.part + (int64_t)2 * a.workers * kRows * HD);
-  if (p.end - p.begin == 1 && a.whole) {
-    p.workers = 0;
-    p.row = out_row;
-    p.o = a.whole;
-    p.ml = reinterpret_cast<const float2*>(a.whole + (int64_t)a.n_tokens * a.hq * HD);
-  }
-  return p;
-}
-
-// One output row a workgroup of 256: HD / 4 threads hold a row, 1024 / HD pieces at a time.
-template <int HD>
-__global__ __launch_bounds__(256) void attend_join_kernel(JoinArgs a) {
-  extern __shared__ int64_t cum[];
+__global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
   constexpr int TR = HD / 4, AT = 256 / TR;
-  __shared__ float sh_m[4];
-  __shared__ f32x4 sh_o[AT][TR];
-  const AttendArgs& own = a.own;
-  list_tiles(own, cum);
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t token = blockIdx.x;
-  const int qh = blockIdx.y, head = qh / own.group;
-  // the token's sequence
-  int s = (int)token;
-  if (own.q_starts) {
-    int lo = 0, hi = own.n_seq - 1;
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
-      if (own.q_starts[mid] <= token) lo = mid;
-      else hi = mid - 1;
-    }
-    s = lo;
-  }
-  const Sequence q = sequence_of(own, s);
-  if (token < q.first || token >= q.first + q.count) return;
-  const int64_t row = (token - q.first) * own.group + (qh - head * own.group), tiles = key_tiles(q);
-  const int64_t out_row = token * own.hq + qh;
-  Pieces p[2];
-  p[0] = pieces_of<HD>(own, cum[own.n_seq], cum[s] + (row / kRows * own.cache.n_heads + head) * tiles, tiles, row % kRows, out_row);
-  int sides = 1;
-  if (a.prefix.workers) {
-    sides = 2;
-    const Sequence z = sequence_of(a.prefix, 0);
-    const int64_t prow = token * own.group + (qh - head * own.group), ptiles = key_tiles(z);
-    p[1] = pieces_of<HD>(a.prefix, ptiles * row_tiles(a.prefix, z) * own.cache.n_heads, (prow / kRows * own.cache.n_heads + head) * ptiles, ptiles,
-                         prow % kRows, out_row);
-  } else if (p[0].end - p[0].begin == 1) {
-    return;  // a whole segment: written already
-  }
   constexpr float kNone = -__builtin_inff();
-  // the largest maximum, then the sum
-  float m = kNone;
-  for (int k = 0; k < sides; ++k)
-    for (int64_t w = p[k].begin + threadIdx.x; w < p[k].end; w += 256) m = fmaxf(m, p[k].ml[p[k].slot(w)].x);
-#pragma unroll
-  for (int o = 1; o < 64; o *= 2) m = fmaxf(m, __shfl_xor(m, o));
-  if (lane == 0) sh_m[wave] = m;
-  __syncthreads();
-  m = fmaxf(fmaxf(sh_m[0], sh_m[1]), fmaxf(sh_m[2], sh_m[3]));
-  const float base = m == kNone ? 0.f : m;
+  __shared__ f32x4 sh_o[AT][TR];
+  __shared__ float2 sh_ml[AT];
+  const int4 cut = a.cuts[blockIdx.x];
+  if (cut.w == 0) return;
+  const float2* ml = reinterpret_cast<const float2*>(a.part + (int64_t)2 * a.workers * kRows * HD);
   const int t = threadIdx.x % TR, at = threadIdx.x / TR;
-  float l = 0.f;
-  f32x4 o = {0.f, 0.f, 0.f, 0.f};
-  for (int k = 0; k < sides; ++k)
-    for (int64_t w = p[k].begin + at; w < p[k].end; w += AT) {
-      const int64_t slot = p[k].slot(w);
-      const float2 d = p[k].ml[slot];
-      const float f = __builtin_amdgcn_exp2f(d.x - base);
-      l = fmaf(d.y, f, l);
-      o += *reinterpret_cast<const f32x4*>(p[k].o + slot * HD + 4 * t) * f;
+  for (int r = blockIdx.y; r < cut.y; r += gridDim.y) {
+    float m = kNone, l = 0.f;
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    for (int k = at; k < cut.w; k += AT) {
+      const int64_t slot = (2 * ((int64_t)blockIdx.x + k) + (k ? 0 : 1)) * kRows + r;
+      const float2 d = ml[slot];
+      const f32x4 v = *reinterpret_cast<const f32x4*>(a.part + slot * HD + 4 * t);
+      const float most = fmaxf(m, d.x), base = most == kNone ? 0.f : most;
+      const float f = __builtin_amdgcn_exp2f(d.x - base), h = __builtin_amdgcn_exp2f(m - base);
+      l = fmaf(d.y, f, l * h);
+      o = v * f + o * h;
+      m = most;
     }
-  sh_o[at][t] = o;
-  __shared__ float sh_s[AT];
-  if (t == 0) sh_s[at] = l;
-  __syncthreads();
-  if (at != 0) return;
-  for (int i = 1; i < AT; ++i) o += sh_o[i][t], l += sh_s[i];
-  const float inv = l == 0.f ? 0.f : 1.f / l;
-  bf16 v[4];
+    __syncthreads();
+    sh_o[at][t] = o;
+    if (t == 0) sh_ml[at] = make_float2(m, l);
+    __syncthreads();
+    if (at == 0) {
+      float most = kNone;
 #pragma unroll
-  for (int e = 0; e < 4; ++e) v[e] = (bf16)(l == 0.f ? 0.f : o[e] * inv);
-  *reinterpret_cast<u32x2*>(own.out + token * own.ldo + (int64_t)qh * HD + 4 * t) = __builtin_bit_cast(u32x2, v);
-  if (own.lse && t == 0) own.lse[token * own.hq + qh] = l == 0.f ? kNone : (base + __log2f(l)) * 0.693147181f;
+      for (int i = 0; i < AT; ++i) most = fmaxf(most, sh_ml[i].x);
+      const float base = most == kNone ? 0.f : most;
+      l = 0.f;
+      o = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int i = 0; i < AT; ++i) {
+        const float f = __builtin_amdgcn_exp2f(sh_ml[i].x - base);
+        l = fmaf(sh_ml[i].y, f, l);
+        o += sh_o[i][t] * f;
+      }
+      const int64_t token = cut.x + r / a.group, qh = cut.z * a.group + r % a.group;
+      const float inv = l == 0.f ? 0.f : 1.f / l;
+      bf16 v[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = (bf16)(l == 0.f ? 0.f : o[e] * inv);
+      *reinterpret_cast<u32x2*>(a.out + token * a.ldo + qh * HD + 4 * t) = __builtin_bit_cast(u32x2, v);
+      if (a.lse && t == 0) a.lse[token * a.hq + qh] = l == 0.f ? kNone : (base + __log2f(l)) * 0.693147181f;
+    }
+  }
 }
 
 }  // namespace kt

@@ -1,8 +1,12 @@
 // kt_serve.hip -- host side of the serving operators: argument checks, workspace layout, launches, and their part of the extern "C"
 // boundary of include/kt.h.
 #include "kt_attention.h"
+#include "kt_attention_tiles.h"
 #include "kt_host.h"
 #include "kt_norm.h"
+
+#include <algorithm>
+#include <type_traits>
 
 namespace kt {
 
@@ -84,12 +88,57 @@ static KvCache device_cache(const kt_kv_cache* c) {
 }
 
 // ------------------------------------------------------------------ attention -----
-// Waves that share the key tiles of a call: two workgroups of four a CU.
-constexpr int64_t kWorkers = (int64_t)kNumCUs * 8;
-constexpr int64_t kMaxSequences = 4096;  // their tile counts are listed in LDS
+constexpr int64_t kWaveWorkers = (int64_t)kNumCUs * 8;  // waves that share the key tiles of single tokens: two workgroups of four a CU
+constexpr int64_t kMaxTokens = (int64_t)1 << 30;         // of a sequence's pages, of a prefix
+constexpr int64_t kMaxSequences = 4096;                 // their tile counts are listed in LDS
+constexpr int kTileWaves = 4, kTileRows = 32 * kTileWaves;
+static int64_t tile_workers(int64_t hd) { return hd == 256 ? kNumCUs : 2 * kNumCUs; }  // as many as are resident (LDS)
 
-static size_t part_bytes(int64_t hd) { return (size_t)(2 * kWorkers * kRows * (hd + 2) * 4); }
-static size_t whole_bytes(int64_t n_tokens, int64_t hq, int64_t hd) { return (size_t)round_up(n_tokens * hq * (hd + 2) * 4, 256); }
+// Single tokens (and few: up to 16 rows a head) take kt_attention.h, which reads each key for its own sequence only; what has more rows
+// takes kt_attention_tiles.h, whose tiles of 128 rows are wasted on fewer.
+static bool few_rows(int64_t max_q, int64_t group) { return max_q * group <= kRows; }
+
+// Tiles of a prefix that single tokens share are split until the launch fills the card.
+static int64_t prefix_splits(int64_t n_tokens, int64_t hq, int64_t n_heads, int64_t hd, int64_t prefix_len) {
+  const int64_t items = ceil_div(n_tokens * (hq / n_heads), kTileRows) * n_heads;
+  return std::max<int64_t>(1, std::min(tile_workers(hd) / items, ceil_div(prefix_len, 64)));
+}
+
+struct AttendPlan {
+  size_t tiles, cuts, part, whole, prefix, seq, row, bytes;
+};
+// Offsets in the workspace; sized for either kernel (hq rows a token, at most kMaxSequences).
+static AttendPlan plan_attention(int64_t n_tokens, int64_t hq, int64_t hd, int64_t prefix_len) {
+  AttendPlan p{};
+  size_t at = 0;
+  auto take = [&](int64_t bytes) {
+    const size_t o = at;
+    at += (size_t)round_up(bytes, 256);
+    return o;
+  };
+  const int64_t entries = n_tokens * hq / kTileRows + kMaxSequences + 1, row = (hd + 2) * 4;
+  p.tiles = take(4 * std::max(entries, kMaxSequences + 1));
+  p.seq = take(4 * entries);
+  p.row = take(4 * entries);
+  p.cuts = take(16 * kWaveWorkers);
+  p.part = take(2 * std::max(kWaveWorkers * kRows, tile_workers(hd) * kTileRows) * row);
+  if (prefix_len) {
+    p.whole = take(n_tokens * hq * row);
+    // splits x rows: at most all rows once, or as many as fill the card
+    p.prefix = take(std::max(n_tokens * hq, tile_workers(hd) * kTileRows) * row);
+  }
+  p.bytes = at;
+  return p;
+}
+
+template <int KV, int HD, bool PREFIX>
+static bool launch_tiles(const TileArgs& t, int64_t wgs, hipStream_t st) {
+  constexpr size_t lds = sizeof(TileShared<KV, HD, kTileWaves>);
+  auto kernel = attend_tiles_kernel<KV, HD, kTileWaves, PREFIX>;
+  if (!ensure_dynamic_lds(reinterpret_cast<const void*>(kernel), lds)) return false;
+  kernel<<<dim3((unsigned)wgs), 64 * kTileWaves, lds, st>>>(t);
+  return true;
+}
 
 }  // namespace kt
 
@@ -193,10 +242,9 @@ kt_status kt_kv_gather(const kt_kv_cache* cache, const int64_t* slots, int64_t n
 
 size_t kt_paged_attention_bytes(int64_t n_tokens, int64_t n_q_heads, int64_t head_dim, int64_t prefix_len) {
   if (n_tokens < 1 || n_tokens > INT32_MAX || n_q_heads < 1 || n_q_heads > 65535 || (head_dim != 64 && head_dim != 128 && head_dim != 256) ||
-      prefix_len < 0)
+      prefix_len < 0 || prefix_len > kMaxTokens)
     return 0;
-  const size_t one = part_bytes(head_dim);
-  return prefix_len ? 2 * (one + whole_bytes(n_tokens, n_q_heads, head_dim)) : one;
+  return plan_attention(n_tokens, n_q_heads, head_dim, prefix_len).bytes;
 }
 
 kt_status kt_paged_attention(const kt_kv_cache* cache, const void* Q, int64_t ldq, kt_dtype dtype, const int32_t* q_starts, const int32_t* lens,
@@ -215,9 +263,9 @@ kt_status kt_paged_attention(const kt_kv_cache* cache, const void* Q, int64_t ld
     return fail(KT_ERR_BAD_SHAPE, "n_q_heads must be a multiple of the cache's heads, at most 65535");
   if (!rows_ok(Q, ldq, n_q_heads * hd, dtype) || ldo < n_q_heads * hd || ldo > ((int64_t)1 << 24) || ldo % 4 || misaligned(O, 8))
     return fail(KT_ERR_BAD_SHAPE, "leading dimensions must be in [heads * head_dim, 2^24], rows of Q 16-byte and of O 8-byte aligned");
-  if (ldp < 1 || ldp * cache->page_size > INT32_MAX) return fail(KT_ERR_BAD_SHAPE, "ldp must be positive, ldp * page_size below 2^31");
-  if (prefix_len < 0 || prefix_len > INT32_MAX || (prefix_len && !prefix_pages))
-    return fail(KT_ERR_INVALID_ARG, "prefix_len must be in [0, 2^31), with prefix_pages");
+  if (ldp < 1 || ldp > kMaxTokens / cache->page_size) return fail(KT_ERR_BAD_SHAPE, "ldp must be positive, ldp * page_size at most 2^30");
+  if (prefix_len < 0 || prefix_len > kMaxTokens || (prefix_len && !prefix_pages))
+    return fail(KT_ERR_INVALID_ARG, "prefix_len must be in [0, 2^30], with prefix_pages");
   if (!(scale > 0.f) || !(scale <= kHuge)) return fail(KT_ERR_INVALID_ARG, "scale must be positive and finite");
   const size_t need = kt_paged_attention_bytes(n_tokens, n_q_heads, hd, prefix_len);
   if (!workspace || workspace_bytes < need)
@@ -226,52 +274,62 @@ kt_status kt_paged_attention(const kt_kv_cache* cache, const void* Q, int64_t ld
   if (misaligned(q_starts, 4) || misaligned(lens, 4) || misaligned(pages, 4) || misaligned(prefix_pages, 4) || misaligned(lse, 4))
     return fail(KT_ERR_BAD_SHAPE, "index arrays and lse must be aligned to their type");
 
+  const int64_t group = n_q_heads / cache->n_heads;
+  const bool few = few_rows(max_q, group);
+  const int64_t entries = few ? n_seq : n_tokens * group / kTileRows + n_seq;
+  if (entries > INT32_MAX / cache->n_heads / (ceil_div(ldp * cache->page_size, 64) + (few ? 0 : ceil_div(prefix_len, 64))))
+    return fail(KT_ERR_NOT_SUPPORTED, "too many tiles of 64 keys for one call: hand in a narrower page table or fewer tokens");
+
+  const AttendPlan p = plan_attention(n_tokens, n_q_heads, hd, prefix_len);
   char* ws = static_cast<char*>(workspace);
-  auto take = [&](size_t bytes) {
-    float* p = reinterpret_cast<float*>(ws);
-    ws += bytes;
-    return p;
-  };
-  AttendArgs own{};
-  own.cache = device_cache(cache);
-  own.q = static_cast<const bf16*>(Q);
-  own.q_starts = q_starts;
-  own.lens = lens;
-  own.pages = pages;
-  own.ldq = ldq;
-  own.ldp = ldp;
-  own.n_seq = (int)n_seq;
-  own.n_tokens = (int)n_tokens;
-  own.hq = (int)n_q_heads;
-  own.group = (int)(n_q_heads / cache->n_heads);
-  own.workers = (int)kWorkers;
-  own.scale = scale;
-  own.out = static_cast<bf16*>(O);
-  own.ldo = ldo;
-  own.lse = lse;
-  own.part = take(part_bytes(hd));
-  own.whole = prefix_len ? take(whole_bytes(n_tokens, n_q_heads, hd)) : nullptr;
-  own.causal = true;
-  JoinArgs join{own, AttendArgs{}};
-  if (prefix_len) {
-    AttendArgs& p = join.prefix = own;
-    p.q_starts = p.lens = nullptr;
-    p.pages = prefix_pages;
-    p.ldp = ceil_div(prefix_len, cache->page_size);
-    p.fixed_len = prefix_len;
-    p.n_seq = 1;
-    p.part = take(part_bytes(hd));
-    p.whole = take(whole_bytes(n_tokens, n_q_heads, hd));
-    p.causal = false;
-  }
+  auto floats = [&](size_t at) { return reinterpret_cast<float*>(ws + at); };
+  auto ints = [&](size_t at) { return reinterpret_cast<int*>(ws + at); };
+  TileArgs t{};
+  AttendArgs& a = t.a;
+  a.cache = device_cache(cache);
+  a.q = static_cast<const bf16*>(Q);
+  a.q_starts = q_starts;
+  a.lens = lens;
+  a.pages = pages;
+  a.ldq = ldq;
+  a.ldp = ldp;
+  a.n_seq = (int)n_seq;
+  a.n_tokens = (int)n_tokens;
+  a.hq = (int)n_q_heads;
+  a.group = (int)group;
+  a.scale = scale;
+  a.out = static_cast<bf16*>(O);
+  a.ldo = ldo;
+  a.lse = lse;
+  a.workers = (int)kWaveWorkers;
+  a.tiles = t.cum = ints(p.tiles);
+  a.cuts = t.cuts = reinterpret_cast<int4*>(ws + p.cuts);
+  a.part = t.part = floats(p.part);
+  a.whole = prefix_len ? floats(p.whole) : nullptr;
+  t.prefix_pages = prefix_pages;
+  t.prefix_len = (int)prefix_len;
+  t.workers = (int)tile_workers(hd);
+  t.entries = (int)entries;
+  t.seq = ints(p.seq);
+  t.row = ints(p.row);
+  t.prefix_part = prefix_len ? floats(p.prefix) : nullptr;
+  t.splits = prefix_len ? (int)prefix_splits(n_tokens, n_q_heads, cache->n_heads, hd, prefix_len) : 0;
   hipStream_t st = static_cast<hipStream_t>(stream);
-  const size_t lds = (size_t)(n_seq + 1) * 8;
-  with_cache(cache, [&](auto kv, auto h) {
-    constexpr int KV = decltype(kv)::value, HD = decltype(h)::value;
-    if (prefix_len) attend_rows_kernel<KV, HD><<<dim3(kWorkers / 4), 256, 16, st>>>(join.prefix);
-    attend_rows_kernel<KV, HD><<<dim3(kWorkers / 4), 256, lds, st>>>(own);
-    attend_join_kernel<HD><<<dim3((unsigned)n_tokens, (unsigned)n_q_heads), 256, lds, st>>>(join);
+  const bool ok = with_cache(cache, [&](auto kv, auto h) {
+    constexpr int KV = decltype(kv)::value, HD = decltype(h)::value, kRowsOf = 1024 / HD;  // rows of a workgroup that joins
+    if (!few) {
+      plan_tiles_kernel<kTileRows><<<1, 1024, 0, st>>>(t);
+      if (!launch_tiles<KV, HD, false>(t, t.workers, st)) return false;
+      join_tiles_kernel<HD, kTileRows><<<dim3((unsigned)t.workers, kTileRows / kRowsOf), 256, 0, st>>>(t);
+      return true;
+    }
+    if (prefix_len && !launch_tiles<KV, HD, true>(t, ceil_div(n_tokens * group, kTileRows) * cache->n_heads * t.splits, st)) return false;
+    attend_rows_kernel<KV, HD><<<dim3(kWaveWorkers / 4), 256, (size_t)(n_seq + 1) * 4, st>>>(a);
+    if (prefix_len) join_prefix_kernel<HD><<<dim3((unsigned)ceil_div(n_tokens * n_q_heads, kRowsOf)), 256, 0, st>>>(t);
+    else attend_join_kernel<HD><<<dim3(kWaveWorkers, 4), 256, 0, st>>>(a);
+    return true;
   });
+  if (!ok) return fail(KT_ERR_DEVICE, "attention kernel needs more LDS than the device gives");
   return launch_ok() ? KT_OK : fail(KT_ERR_DEVICE, "attention kernel launch failed");
 }
 
