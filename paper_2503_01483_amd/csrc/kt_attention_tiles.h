@@ -191,10 +191,7 @@ struct TileLoader {
       const bool bad = !(most <= kHuge) || vs != vs;
       info.odd = __ballot(bad);
       if (bad) vs = vb = most = 0.f;
-      int e = (int)(__float_as_uint(most) >> 23);
-#pragma unroll
-      for (int o = 1; o < 64; o *= 2) e = max(e, __shfl_xor(e, o));
-      info.v_exp = uniform(max(min(e, 252), v_run - 60));
+      info.v_exp = max(min(wave_max((int)(__float_as_uint(most) >> 23)), 252), v_run - 60);
       const float vf = __uint_as_float((unsigned)(253 - info.v_exp) << 23);
       sh.par[wave][0][lane] = (_Float16)(vs * vf);
       sh.par[wave][1][lane] = (_Float16)(vb * vf);
@@ -244,9 +241,26 @@ struct TileLoader {
   }
 };
 
+// N products in order, `product(n, operand)`, each with an operand from LDS, `read(n)`, that is asked for kAhead products earlier: left to itself
+// the compiler waits for every read in front of its product.
+template <int N, class Read, class Product>
+__device__ __forceinline__ void pipelined(Read read, Product product) {
+  constexpr int kAhead = 4;
+  decltype(read(0)) ring[kAhead];
+#pragma unroll
+  for (int n = 0; n < kAhead; ++n) ring[n] = read(n);
+  __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    product(n, ring[n % kAhead]);
+    if (n + kAhead < N) ring[n % kAhead] = read(n + kAhead);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+}
+
 // PREFIX: the rows of all tokens over the prefix alone, split over its tiles, to prefix_part; else the list.
 template <int KV, int HD, int WAVES, bool PREFIX>
-__global__ __launch_bounds__(64 * WAVES, HD == 256 ? 1 : 2) void attend_tiles_kernel(TileArgs t) {
+__global__ __launch_bounds__(64 * WAVES, HD == 256 && WAVES == 4 ? 1 : 2) void attend_tiles_kernel(TileArgs t) {
   constexpr int R = 32 * WAVES, TD = HD / 32, KS = HD / 16;
   constexpr bool Q16 = KV != kKvBf16;  // quantised: p and the values in fp16
   using frag = std::conditional_t<Q16, f16x8, bf16x8>;
@@ -320,6 +334,9 @@ __global__ __launch_bounds__(64 * WAVES, HD == 256 ? 1 : 2) void attend_tiles_ke
       }
     }
     if constexpr (Q16) qsum += __shfl_xor(qsum, 32);
+    // arrived before the loop: a wait for them in it would wait for the tiles that are on their way to LDS as well
+#pragma unroll
+    for (int w = 0; w < KS; ++w) asm volatile("" : "+v"(qf[w]));
 
     f32x16 o[TD];
 #pragma unroll
@@ -329,15 +346,20 @@ __global__ __launch_bounds__(64 * WAVES, HD == 256 ? 1 : 2) void attend_tiles_ke
     float m = kNone, l = 0.f;  // m: in bits (times c)
     int v_run = 0;             // exponent of O
     Loader ld;
-    TileInfo info[2] = {{0, 0ull}, {0, 0ull}};
+    TileInfo info = {0, 0ull}, info_next = {0, 0ull};
 
+    PageWindow window;
+    const int* window_of = nullptr;
     // the block of tile `tile` and how many of its tokens exist; null: none that can be seen
     auto block_of = [&](int tile, int& there) -> const char* {
       const bool own = tile >= prefix_tiles;
       const int k = own ? tile - prefix_tiles : tile, len = own ? q.len : t.prefix_len;
       there = min(len - k * 64, 64);
       if (there <= 0) return nullptr;
-      const int64_t page = (own ? pages : t.prefix_pages)[k >> page_blocks];
+      const int* table = own ? pages : t.prefix_pages;
+      if (window_of != table) window.count = 0;
+      window_of = table;
+      const int64_t page = window.get(table, k >> page_blocks, (len + 63 >> 6) + (1 << page_blocks) - 1 >> page_blocks);
       if (page < 0 || page >= a.cache.n_pages) return nullptr;
       return uniform_ptr(a.cache.data + kv_block_offset<KV, HD>(a.cache, page, head, k & ((1 << page_blocks) - 1)));
     };
@@ -347,7 +369,7 @@ __global__ __launch_bounds__(64 * WAVES, HD == 256 ? 1 : 2) void attend_tiles_ke
     __syncthreads();  // the buffers are free (the last segment's tile was read)
     if (block) {
       ld.begin(block, sh.data[0]);
-      ld.finish(sh, 0, there, c, v_run, info[0]);
+      ld.finish(sh, 0, there, c, v_run, info);
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
@@ -365,7 +387,7 @@ __global__ __launch_bounds__(64 * WAVES, HD == 256 ? 1 : 2) void attend_tiles_ke
       const int seen = own ? min(max(sees - base, 0), there) : there;
       if (block) {
         char* kb = sh.data[buf];
-        unsigned long long odd = info[buf].odd;
+        unsigned long long odd = info.odd;
         if constexpr (!Q16) {
           if (masked) {  // what a row does not see may be anything, and 0 NaN = NaN
             if (threadIdx.x < 2) sh.odd[threadIdx.x] = 0u;
@@ -392,22 +414,28 @@ __global__ __launch_bounds__(64 * WAVES, HD == 256 ? 1 : 2) void attend_tiles_ke
         }
         f32x16 x[2];
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
+        for (int k = 0; k < 2; ++k)
 #pragma unroll
           for (int e = 0; e < 16; ++e) x[k][e] = KV == kKvU4 ? -128.f * qsum : 0.f;  // (codes of 4 bits enter as 128 + c)
-          const int key = 32 * k + ((r & 0x13) | (r & 4) << 1 | (r & 8) >> 1);
+        {
+          // (keys 32 further on have the same low bits)
+          const int key = (r & 0x13) | (r & 4) << 1 | (r & 8) >> 1;
           const char* from = kb + key * Loader::ROWB;
+          pipelined<2 * KS>(
+              [&](int n) {
+                return *reinterpret_cast<const bf16x8*>(from + (n & 1) * (32 * Loader::ROWB) + (((2 * (n >> 1) + h) ^ (key & Loader::KMASK)) << 4));
+              },
+              [&](int n, bf16x8 f) { x[n & 1] = mfma32(f, qf[n >> 1], x[n & 1]); });
+        }
+        if constexpr (Q16) {
 #pragma unroll
-          for (int w = 0; w < KS; ++w)
-            x[k] = mfma32(*reinterpret_cast<const bf16x8*>(from + (((2 * w + h) ^ (key & Loader::KMASK)) << 4)), qf[w], x[k]);
-          if constexpr (Q16) {
+          for (int k = 0; k < 2; ++k)
 #pragma unroll
             for (int e = 0; e < 16; e += 2) {
               const float4 kp = *reinterpret_cast<const float4*>(&sh.keys[buf][32 * k + 16 * (e >> 3) + 8 * h + (e & 7)]);
               x[k][e] = fmaf(x[k][e], kp.x, kp.y * qsum);
               x[k][e + 1] = fmaf(x[k][e + 1], kp.z, kp.w * qsum);
             }
-          }
         }
         if (masked) {
 #pragma unroll
@@ -418,13 +446,13 @@ __global__ __launch_bounds__(64 * WAVES, HD == 256 ? 1 : 2) void attend_tiles_ke
         }
         int shift = 0;
         if constexpr (Q16) {
-          if (info[buf].v_exp > v_run) {
-            const float f = v_run - info[buf].v_exp > -126 ? __uint_as_float((unsigned)(127 + v_run - info[buf].v_exp) << 23) : 0.f;
+          if (info.v_exp > v_run) {
+            const float f = v_run - info.v_exp > -126 ? __uint_as_float((unsigned)(127 + v_run - info.v_exp) << 23) : 0.f;
 #pragma unroll
             for (int i = 0; i < TD; ++i) o[i] *= f;
-            v_run = info[buf].v_exp;
+            v_run = info.v_exp;
           }
-          shift = info[buf].v_exp - v_run;  // at least -60
+          shift = info.v_exp - v_run;  // at least -60
         }
         float most = fmaxf(x[0][0], x[1][0]);
 #pragma unroll
@@ -451,12 +479,10 @@ __global__ __launch_bounds__(64 * WAVES, HD == 256 ? 1 : 2) void attend_tiles_ke
           }
         const float all = (sum[0] + sum[1]) + (sum[2] + sum[3]);
         l += Q16 ? all * __uint_as_float((unsigned)(127 - shift) << 23) : all;
-#pragma unroll
-        for (int i = 0; i < TD; ++i) {
-          const int f = 32 * i + r;
-          const char* from = kb + Shared::kKeys + f * 128;
-#pragma unroll
-          for (int j = 0; j < 4; ++j) o[i] = mfma32(*reinterpret_cast<const frag*>(from + (((2 * j + h) ^ (f & 7)) << 4)), pf[j], o[i]);
+        {
+          const char* from = kb + Shared::kKeys + r * 128;  // (features 32 further on have the same low bits)
+          pipelined<4 * TD>([&](int n) { return *reinterpret_cast<const frag*>(from + n % TD * (32 * 128) + (((2 * (n / TD) + h) ^ (r & 7)) << 4)); },
+                            [&](int n, frag f) { o[n % TD] = mfma32(f, pf[n / TD], o[n % TD]); });
         }
         if (odd) {
           const unsigned long long mine = seen >= 64 ? ~0ull : (1ull << seen) - 1;
@@ -465,18 +491,26 @@ __global__ __launch_bounds__(64 * WAVES, HD == 256 ? 1 : 2) void attend_tiles_ke
 #pragma unroll
             for (int i = 0; i < TD; ++i) o[i] += add;
           } else {
-            const bf16* v = reinterpret_cast<const bf16*>(block + Loader::kHalf);
+            const bf16* v = reinterpret_cast<const bf16*>(block + Loader::kHalf) + 4 * h * kBlockTokens;
+#pragma unroll 1
+            for (unsigned long long left = odd; left; left &= left - 1) {
+              const int j = __builtin_ctzll(left);
 #pragma unroll
-            for (int i = 0; i < TD; ++i)
+              for (int i = 0; i < TD; ++i)
 #pragma unroll
-              for (int e = 0; e < 16; ++e) o[i][e] += unfinite(v, 32 * i + (e & 3) + 8 * (e >> 2) + 4 * h, seen);
+                for (int e = 0; e < 16; ++e) {
+                  const float y = (float)v[(32 * i + (e & 3) + 8 * (e >> 2)) * kBlockTokens + j];
+                  if (j < seen && !(fabsf(y) <= kHuge)) o[i][e] += y;
+                }
+            }
           }
         }
       }
-      if (next) ld.finish(sh, buf ^ 1, there_next, c, v_run, info[buf ^ 1]);
+      if (next) ld.finish(sh, buf ^ 1, there_next, c, v_run, info_next);
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
       __syncthreads();
       block = next;
+      info = info_next;
       there = there_next;
     }
 

@@ -91,8 +91,8 @@ static KvCache device_cache(const kt_kv_cache* c) {
 constexpr int64_t kWaveWorkers = (int64_t)kNumCUs * 8;  // waves that share the key tiles of single tokens: two workgroups of four a CU
 constexpr int64_t kMaxTokens = (int64_t)1 << 30;         // of a sequence's pages, of a prefix
 constexpr int64_t kMaxSequences = 4096;                 // their tile counts are listed in LDS
-constexpr int kTileWaves = 4, kTileRows = 32 * kTileWaves;
-static int64_t tile_workers(int64_t hd) { return hd == 256 ? kNumCUs : 2 * kNumCUs; }  // as many as are resident (LDS)
+constexpr int kTileWaves = 8, kTileRows = 32 * kTileWaves;
+static int64_t tile_workers(int64_t hd) { return kNumCUs; }  // as many as are resident (LDS)
 
 // Single tokens (and few: up to 16 rows a head) take kt_attention.h, which reads each key for its own sequence only; what has more rows
 // takes kt_attention_tiles.h, whose tiles of 128 rows are wasted on fewer.
