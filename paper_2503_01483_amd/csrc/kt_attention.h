@@ -125,21 +125,6 @@ __device__ __forceinline__ bf16x8 spread_bytes(uint32_t x, uint32_t y) {
 
 __device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 
-// Pages of consecutive tiles, 64 at a time in a lane each: asked for one by one, each would stand in front of its tile's loads.
-struct PageWindow {
-  int page, from = 0, count = 0;
-  // the table's entry `at` (uniform, below `size`)
-  __device__ __forceinline__ int get(const int* table, int at, int size) {
-    if ((unsigned)(at - from) >= (unsigned)count) {
-      const int lane = threadIdx.x & 63;
-      from = at;
-      count = min(64, size - at);
-      page = lane < count ? table[at + lane] : -1;
-    }
-    return __builtin_amdgcn_readlane(page, at - from);
-  }
-};
-
 // Maximum over the lanes of a wave, by row shifts and broadcasts; uniform.
 __device__ __forceinline__ int wave_max(int v) {
   v = max(v, __builtin_amdgcn_update_dpp(v, v, 0x111, 0xf, 0xf, false));  // row_shr 1, 2, 4, 8

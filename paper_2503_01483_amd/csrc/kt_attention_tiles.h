@@ -5,8 +5,8 @@
 // keys' rows are read with bits 2 and 3 of the key's number exchanged, which makes the eight scores that a lane holds of each
 // sixteen keys neighbours.
 //
-// Bound by the matrix cores and the vector ALU side by side: a wave's tile takes 1024 cycles of products and about 900 of
-// exponentials and the like (HD = 128), and 32 KiB of LDS reads, 256 cycles of the CU's.
+// A wave's tile takes the matrix cores 1024 cycles (HD = 128) and the vector ALU about as long, most of it exponentials: three quarters of them are
+// worked out beside the products of the values that need the others, the rest beside the other wave of the SIMD.
 //
 // bf16 caches go straight from memory to LDS.  Of quantised ones the keys' codes do, as exact bf16 values, and a score becomes s (q . c) + b sum(q)
 // in fp32 as in kt_attention.h; the values are expanded on the way, in fp16: a row s c + b is scaled by a power of two per
@@ -29,7 +29,7 @@ struct TileArgs {
   int prefix_len;
   int workers;           // workgroups; a multiple of 8
   int entries;           // row tiles of one head, gaps among them
-  int *cum, *seq, *row;  // [entries + 1] key tiles in front of each, its sequence and row tile
+  int4* list;            // [entries + 1] {tiles of the keys (and cost) in front, sequence, row tile, tiles and cost}
   int4* cuts;            // [workers] {entry, head, pieces or 0}
   float* part;           // pieces of cut segments: O [2 workers][R][HD], then {max in bits, sum}
   int splits;            // of a prefix of its own (kt_attention.h takes the rest)
@@ -57,6 +57,9 @@ __device__ __forceinline__ int64_t first_entry(const AttendArgs& a, int s, int R
   return (int64_t)min(max(a.q_starts ? a.q_starts[s] : s, 0), a.n_tokens) * a.group / R + s;
 }
 
+// What a segment costs beside its tiles, in tiles: its queries, the first tiles' way to LDS, its output.  Counted in the list, in front of them.
+constexpr int kSegmentCost = 2;
+
 // The list of row tiles.  One workgroup of 1024.
 template <int R>
 __global__ __launch_bounds__(1024) void plan_tiles_kernel(TileArgs t) {
@@ -82,7 +85,7 @@ __global__ __launch_bounds__(1024) void plan_tiles_kernel(TileArgs t) {
       if (rt >= 0 && rt * R < rows) {
         const int last = (int)((min(rows, (rt + 1) * R) - 1) / a.group);
         const int sees = min(max(q.len - q.count + last + 1, 0), q.len);
-        mine = max(1, prefix_tiles + (int)(((unsigned)sees + 63) >> 6));
+        mine = kSegmentCost + max(1, prefix_tiles + (int)(((unsigned)sees + 63) >> 6));
       }
     }
     int upto = mine;
@@ -99,153 +102,149 @@ __global__ __launch_bounds__(1024) void plan_tiles_kernel(TileArgs t) {
       carry += wave_sum[w];
     }
     if (e < t.entries) {
-      t.cum[e] = before + upto - mine;
-      t.seq[e] = s;
-      t.row[e] = (int)rt;
+      t.list[e] = int4{before + upto - mine, s, (int)rt, mine};
     }
     __syncthreads();
   }
-  if (threadIdx.x == 0) t.cum[t.entries] = carry;
+  if (threadIdx.x == 0) t.list[t.entries] = int4{carry, 0, 0, 0};
 }
 
 template <int KV, int HD, int WAVES>
 struct TileShared {
-  static constexpr int kKeys = kBlockTokens * HD * 2, kBuffer = 2 * kKeys;
-  char data[2][kBuffer];           // keys [64][HD], values [HD][64], 16-byte chunks exchanged within a row (swizzled)
-  float2 keys[2][64];              // {step, minimum} of the keys, times the factor of the exponentials
-  _Float16 par[WAVES][2][64];      // of the tile that is being expanded: its values' steps and minima
-  unsigned odd[2];                 // tokens of a tile with values that are not finite (bf16)
+  static constexpr int kTile = kBlockTokens * HD * 2;
+  // 16-byte chunks exchanged within a row (swizzled)
+  char keys[2][kTile];          // [64][HD]
+  char values[2][kTile];        // [HD][64]
+  float2 par[2][64];            // {step, minimum} of the keys, times the factor of the exponentials
+  _Float16 expand[WAVES][2][64];  // steps and minima of the values that are being expanded
+  unsigned long long odd[2][WAVES];  // bf16: tokens of a masked tile with values that are not finite, those in the pieces of each wave
 };
 
-// The state of a workgroup's current tile of keys.
-struct TileInfo {
-  int v_exp;                 // exponent (biased by 126) that the values were scaled down by
-  unsigned long long odd;    // tokens whose values are not finite (as 0 in LDS)
-};
-
+// Moves tiles of keys and of values into LDS.
 template <int KV, int HD, int WAVES>
 struct TileLoader {
   using Shared = TileShared<KV, HD, WAVES>;
   static constexpr int THREADS = 64 * WAVES, kHalf = kv_half_bytes<KV, HD>(), ROWB = HD * 2;
   static constexpr int KMASK = HD >= 128 ? 15 : 7;
-  // quantised: 16-byte (HD = 64, u4: 8-byte) pieces of a thread
+  static constexpr int STEPS = Shared::kTile / 1024 / WAVES;                      // bf16: KiB of a wave, keys and values each
+  // quantised: pieces of a thread
   static constexpr int KW = KV == kKvU4 ? HD / 32 : HD / 16;                      // dwords of a (token, quarter)
-  static constexpr int KP = 256 / THREADS > 0 ? 256 / THREADS : 1;                // (token, quarter)s of a thread
   static constexpr int VROWS = KV == kKvU4 ? HD / 2 : HD;
   static constexpr int VP = (VROWS * 4 + THREADS - 1) / THREADS;                  // (row, 16 tokens)s of a thread
-  uint32_t k[KV == kKvBf16 ? 1 : KP][KV == kKvBf16 ? 1 : KW];
+  // (where keys and values are 256 pieces each, of 512 threads half take the ones, half the others)
+  __device__ __forceinline__ static int piece(int tid, int i) { return (VROWS * 4 == 256 && THREADS == 512 ? tid ^ 256 : tid) + i * THREADS; }
+  // the thread's number, and with it every address, worked out anew: kept over the loop they would push others out to memory
+  __device__ __forceinline__ static int thread() {
+    int tid = threadIdx.x;
+    asm volatile("" : "+v"(tid));
+    return tid;
+  }
+  static_assert(THREADS >= 256);                                                  // (256 (token, quarter)s: at most one a thread)
+  uint32_t k[KV == kKvBf16 ? 1 : KW];
   u32x4 v[KV == kKvBf16 ? 1 : VP];
   float2 kp, vp;
 
-  // Begins loading a block: bf16 into `buf`, else into registers.
-  __device__ __forceinline__ void begin(const char* block, char* buf) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    if constexpr (KV == kKvBf16) {
-      const unsigned at = (unsigned)(uintptr_t)buf;  // (LDS addresses are the low 32 bits)
-      constexpr int STEPS = Shared::kKeys / 1024 / WAVES;
+  // bf16: where in a block lane and wave of the first of STEPS pieces of keys, of values, begin to read
+  __device__ __forceinline__ static int key_source() {
+    const int tid = thread(), byte = (tid >> 6) * (STEPS * 1024) + (tid & 63) * 16, row = byte / ROWB;
+    return row * ROWB + ((byte % ROWB / 16 ^ (row & KMASK)) << 4);
+  }
+  __device__ __forceinline__ static int value_source() {
+    const int tid = thread(), byte = (tid >> 6) * (STEPS * 1024) + (tid & 63) * 16, row = byte / 128;
+    return kHalf + row * 128 + ((byte % 128 / 16 ^ (row & 7)) << 4);
+  }
+  // what the exchange adds to the source of the i-th piece of keys: a KiB further on the row's number has other bits, without a carry
+  __device__ __forceinline__ static constexpr int key_turn(int i) { return (1024 / ROWB * i & KMASK) << 4; }
+  // quantised: asks for keys and for values
+  __device__ __forceinline__ void ask_keys(const char* block) {
+    const int tid = thread();
+    const char* from = block + tid * (KW * 4);
+    if (tid < 256) {
+      if constexpr (KW % 4 == 0) {
 #pragma unroll
-      for (int i = 0; i < STEPS; ++i) {
-        const int kb = (wave * STEPS + i) * 1024, byte = kb + lane * 16;
-        const int row = byte / ROWB, chunk = byte % ROWB / 16;
-        to_lds_16(row * ROWB + ((chunk ^ (row & KMASK)) << 4), block, __builtin_amdgcn_readfirstlane(at + kb));
+        for (int j = 0; j < KW; j += 4) *reinterpret_cast<u32x4*>(&k[j]) = *reinterpret_cast<const u32x4*>(from + 4 * j);
+      } else {
+        *reinterpret_cast<u32x2*>(&k[0]) = *reinterpret_cast<const u32x2*>(from);
       }
-#pragma unroll
-      for (int i = 0; i < STEPS; ++i) {
-        const int kb = (wave * STEPS + i) * 1024, byte = kb + lane * 16;
-        const int row = byte / 128, chunk = byte % 128 / 16;
-        to_lds_16(kHalf + row * 128 + ((chunk ^ (row & 7)) << 4), block, __builtin_amdgcn_readfirstlane(at + Shared::kKeys + kb));
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < KP; ++i) {
-        const char* from = block + (threadIdx.x + i * THREADS) * (KW * 4);
-        if (KP * THREADS > 256 && threadIdx.x >= 256) break;
-        if constexpr (KW % 4 == 0) {
-#pragma unroll
-          for (int j = 0; j < KW; j += 4) *reinterpret_cast<u32x4*>(&k[i][j]) = *reinterpret_cast<const u32x4*>(from + 4 * j);
-        } else {
-          *reinterpret_cast<u32x2*>(&k[i][0]) = *reinterpret_cast<const u32x2*>(from);
-        }
-      }
-#pragma unroll
-      for (int i = 0; i < VP; ++i) {
-        const int piece = threadIdx.x + i * THREADS;
-        if (piece < VROWS * 4) v[i] = *reinterpret_cast<const u32x4*>(block + kHalf + piece * 16);
-      }
-      kp = reinterpret_cast<const float2*>(block + 2 * kHalf)[lane];
-      vp = reinterpret_cast<const float2*>(block + 2 * kHalf)[kBlockTokens + lane];
     }
+    kp = reinterpret_cast<const float2*>(block + 2 * kHalf)[tid & 63];
+  }
+  __device__ __forceinline__ void ask_values(const char* block) {
+    const int tid = thread();
+#pragma unroll
+    for (int i = 0; i < VP; ++i) {
+      if (piece(tid, i) < VROWS * 4) v[i] = *reinterpret_cast<const u32x4*>(block + kHalf + piece(tid, i) * 16);
+    }
+    vp = reinterpret_cast<const float2*>(block + 2 * kHalf)[kBlockTokens + (tid & 63)];
   }
 
-  // Finishes it: expanded into buffer `at`.  `there`: tokens of the block that exist; c: factor of the exponentials; v_run: exponent of O so far,
-  // for a floor.
-  __device__ __forceinline__ void finish(Shared& sh, int at, int there, float c, int v_run, TileInfo& info) {
-    if constexpr (KV != kKvBf16) {
-      const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-      constexpr float top = KV == kKvU4 ? 15.f : 255.f;
-      char* buf = sh.data[at];
-      const bool is = lane < there;
-      if (wave == 0) sh.keys[at][lane] = is ? make_float2(kp.x * c, kp.y * c) : make_float2(0.f, 0.f);
-      float vs = is ? vp.x : 0.f, vb = is ? vp.y : 0.f;
-      float most = fmaxf(fabsf(vb), fabsf(fmaf(top, vs, vb)));
-      const bool bad = !(most <= kHuge) || vs != vs;
-      info.odd = __ballot(bad);
-      if (bad) vs = vb = most = 0.f;
-      info.v_exp = max(min(wave_max((int)(__float_as_uint(most) >> 23)), 252), v_run - 60);
-      const float vf = __uint_as_float((unsigned)(253 - info.v_exp) << 23);
-      sh.par[wave][0][lane] = (_Float16)(vs * vf);
-      sh.par[wave][1][lane] = (_Float16)(vb * vf);
-      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-      __builtin_amdgcn_wave_barrier();
-      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-      const f16x2 bias = {(_Float16)-1024.f, (_Float16)-1024.f};
-      auto half2 = [](uint32_t x) { return __builtin_bit_cast(f16x2, x); };
+  // Keys into buffer `at`.  `there`: tokens of the block that exist; c: factor of the exponentials.
+  __device__ __forceinline__ void put_keys(Shared& sh, int at, int there, float c) const {
+    const int tid = thread(), token = tid >> 2, g = tid & 3;
+    if (tid < 64) sh.par[at][tid] = tid < there ? make_float2(kp.x * c, kp.y * c) : make_float2(0.f, 0.f);
+    if (tid < 256) {
 #pragma unroll
-      for (int i = 0; i < KP; ++i) {
-        const int unit = threadIdx.x + i * THREADS, token = unit >> 2, g = unit & 3;
-        if (KP * THREADS > 256 && threadIdx.x >= 256) break;
-#pragma unroll
-        for (int w = 0; w < HD / 32; ++w) {
-          bf16x8 out;
-          if constexpr (KV == kKvU4) out = spread_nibbles(k[i][w]);
-          else out = spread_bytes(k[i][2 * w], k[i][2 * w + 1]);
-          *reinterpret_cast<bf16x8*>(buf + token * ROWB + (((4 * w + g) ^ (token & KMASK)) << 4)) = out;
-        }
+      for (int w = 0; w < HD / 32; ++w) {
+        bf16x8 out;
+        if constexpr (KV == kKvU4) out = spread_nibbles(k[w]);
+        else out = spread_bytes(k[2 * w], k[2 * w + 1]);
+        *reinterpret_cast<bf16x8*>(sh.keys[at] + token * ROWB + (((4 * w + g) ^ (token & KMASK)) << 4)) = out;
       }
-#pragma unroll
-      for (int i = 0; i < VP; ++i) {
-        const int piece = threadIdx.x + i * THREADS, row = piece >> 2, g = piece & 3;
-        if (piece >= VROWS * 4) break;
-        const u32x4* vs4 = reinterpret_cast<const u32x4*>(&sh.par[wave][0][16 * g]);
-        const u32x4* vb4 = reinterpret_cast<const u32x4*>(&sh.par[wave][1][16 * g]);
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {  // 8 tokens
-          const u32x4 s8 = vs4[h], b8 = vb4[h];
-#pragma unroll
-          for (int n = 0; n < (KV == kKvU4 ? 2 : 1); ++n) {
-            u32x4 out;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              uint32_t x = v[i][2 * h + (j >> 1)];
-              if constexpr (KV == kKvU4) x = (n ? x >> 4 : x) & 0x0f0f0f0fu;
-              x = __builtin_amdgcn_perm(0x64646464u, x, j & 1 ? 0x07030702u : 0x07010700u);
-              out[j] = __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(half2(x) + bias, half2(s8[j]), half2(b8[j])));
-            }
-            const int f = KV == kKvU4 ? (row >> 4) * 32 + 16 * n + (row & 15) : row;
-            *reinterpret_cast<u32x4*>(buf + Shared::kKeys + f * 128 + (((2 * g + h) ^ (f & 7)) << 4)) = out;
-          }
-        }
-      }
-      __builtin_amdgcn_wave_barrier();
     }
+  }
+  // Values, expanded, into buffer `at`; returns the exponent (biased by 126) that they are scaled down by, and the tokens whose values are
+  // not finite (as 0).  v_run: exponent of O so far, for a floor.
+  __device__ __forceinline__ int put_values(Shared& sh, int at, int there, int v_run, unsigned long long& odd) const {
+    const int tid = thread(), lane = tid & 63, wave = uniform(tid >> 6);
+    constexpr float top = KV == kKvU4 ? 15.f : 255.f;
+    float vs = lane < there ? vp.x : 0.f, vb = lane < there ? vp.y : 0.f;
+    float most = fmaxf(fabsf(vb), fabsf(fmaf(top, vs, vb)));
+    const bool bad = !(most <= kHuge) || vs != vs;
+    odd = __ballot(bad);
+    if (bad) vs = vb = most = 0.f;
+    const int v_exp = max(min(wave_max((int)(__float_as_uint(most) >> 23)), 252), v_run - 60);
+    const float f = __uint_as_float((unsigned)(253 - v_exp) << 23);
+    sh.expand[wave][0][lane] = (_Float16)(vs * f);
+    sh.expand[wave][1][lane] = (_Float16)(vb * f);
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    const f16x2 bias = {(_Float16)-1024.f, (_Float16)-1024.f};
+    auto half2 = [](uint32_t x) { return __builtin_bit_cast(f16x2, x); };
+#pragma unroll
+    for (int i = 0; i < VP; ++i) {
+      const int row = piece(tid, i) >> 2, g = piece(tid, i) & 3;
+      if (piece(tid, i) >= VROWS * 4) break;
+      const u32x4* s4 = reinterpret_cast<const u32x4*>(&sh.expand[wave][0][16 * g]);
+      const u32x4* b4 = reinterpret_cast<const u32x4*>(&sh.expand[wave][1][16 * g]);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {  // 8 tokens
+        const u32x4 s8 = s4[h], b8 = b4[h];
+#pragma unroll
+        for (int n = 0; n < (KV == kKvU4 ? 2 : 1); ++n) {
+          u32x4 out;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            uint32_t x = v[i][2 * h + (j >> 1)];
+            if constexpr (KV == kKvU4) x = (n ? x >> 4 : x) & 0x0f0f0f0fu;
+            x = __builtin_amdgcn_perm(0x64646464u, x, j & 1 ? 0x07030702u : 0x07010700u);  // two bytes as fp16 1024 + c
+            out[j] = __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(half2(x) + bias, half2(s8[j]), half2(b8[j])));
+          }
+          const int f = KV == kKvU4 ? (row >> 4) * 32 + 16 * n + (row & 15) : row;
+          *reinterpret_cast<u32x4*>(sh.values[at] + f * 128 + (((2 * g + h) ^ (f & 7)) << 4)) = out;
+        }
+      }
+    }
+    __builtin_amdgcn_wave_barrier();
+    return v_exp;
   }
 };
 
 // N products in order, `product(n, operand)`, each with an operand from LDS, `read(n)`, that is asked for kAhead products earlier: left to itself
-// the compiler waits for every read in front of its product.
-template <int N, class Read, class Product>
-__device__ __forceinline__ void pipelined(Read read, Product product) {
-  constexpr int kAhead = 4;
+// the compiler waits for every read in front of its product.  beside(n): other work, done while the matrix cores are at it.
+template <int N, class Read, class Product, class Beside>
+__device__ __forceinline__ void pipelined(Read read, Product product, Beside beside) {
+  constexpr int kAhead = 3;
   decltype(read(0)) ring[kAhead];
 #pragma unroll
   for (int n = 0; n < kAhead; ++n) ring[n] = read(n);
@@ -254,9 +253,25 @@ __device__ __forceinline__ void pipelined(Read read, Product product) {
   for (int n = 0; n < N; ++n) {
     product(n, ring[n % kAhead]);
     if (n + kAhead < N) ring[n % kAhead] = read(n + kAhead);
+    beside(n);
     __builtin_amdgcn_sched_barrier(0);
   }
 }
+
+// Two neighbours of p in fp16, cut off (2^-10 of each at most; rounding to nearest would take three instructions for one).
+__device__ __forceinline__ void put_pair(f16x8& f, int at, float a, float b) {
+  const auto both = __builtin_bit_cast(f16x2, __builtin_amdgcn_cvt_pkrtz(a, b));
+  f[at] = both[0];
+  f[at + 1] = both[1];
+}
+__device__ __forceinline__ void put_pair(bf16x8&, int, float, float) {}
+
+// A workgroup's tile of keys.
+struct TileState {
+  int64_t block;  // offset of its block in the cache; some block where there is none
+  int there;      // tokens of it that exist
+  int base;       // the sequence's first token in it; negative: of the prefix
+};
 
 // PREFIX: the rows of all tokens over the prefix alone, split over its tiles, to prefix_part; else the list.
 template <int KV, int HD, int WAVES, bool PREFIX>
@@ -264,14 +279,13 @@ __global__ __launch_bounds__(64 * WAVES, HD == 256 && WAVES == 4 ? 1 : 2) void a
   constexpr int R = 32 * WAVES, TD = HD / 32, KS = HD / 16;
   constexpr bool Q16 = KV != kKvBf16;  // quantised: p and the values in fp16
   using frag = std::conditional_t<Q16, f16x8, bf16x8>;
-  using elem = std::conditional_t<Q16, _Float16, bf16>;
   using Loader = TileLoader<KV, HD, WAVES>;
   using Shared = typename Loader::Shared;
   extern __shared__ __align__(16) char lds[];
   Shared& sh = *reinterpret_cast<Shared*>(lds);
   constexpr float kNone = -__builtin_inff();
   const AttendArgs& a = t.a;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 31, h = lane >> 5, heads = a.cache.n_heads;
+  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), r = lane & 31, h = lane >> 5, heads = a.cache.n_heads;
   const int page_blocks = a.cache.log2_page - 6, prefix_tiles = (int)(((unsigned)t.prefix_len + 63) >> 6);
   const float c = a.scale * 1.44269504f;
 
@@ -282,15 +296,16 @@ __global__ __launch_bounds__(64 * WAVES, HD == 256 && WAVES == 4 ? 1 : 2) void a
     end = 1;
   } else {
     me = (blockIdx.x & 7) * (t.workers >> 3) + (blockIdx.x >> 3);
-    one = t.cum[t.entries];
+    one = t.list[t.entries].x;
     per = piece_length(one * heads, t.workers);
     begin = me * per;
     end = min(begin + per, one * heads);
   }
   int4 cut = {0, 0, 0, 0};
+  int entry = -1;
 
   for (int u = begin; u < end;) {
-    int head, entry = 0, tiles, first, last, row_tile, split = 0;
+    int head, tiles, first, last, row_tile, split = 0, units = 0, in = 0;
     Sequence q;
     const int* pages = nullptr;
     if constexpr (PREFIX) {
@@ -305,16 +320,33 @@ __global__ __launch_bounds__(64 * WAVES, HD == 256 && WAVES == 4 ? 1 : 2) void a
       last = (int)((int64_t)tiles * (split + 1) / t.splits);
     } else {
       head = (int)((unsigned)u / (unsigned)one);
-      const int in = u - head * one;
-      entry = uniform(sequence_at(t.cum, t.entries, in));
-      const int s = uniform(t.seq[entry]);
-      row_tile = uniform(t.row[entry]);
+      in = u - head * one;
+      // the entry that place `in` of a head's list is in: looked for once, then the next ones in turn
+      if (entry < 0) {
+        int lo = 0, hi = t.entries - 1;
+        while (lo < hi) {
+          const int mid = (lo + hi + 1) >> 1;
+          if (t.list[mid].x <= in) lo = mid;
+          else hi = mid - 1;
+        }
+        entry = uniform(lo);
+      }
+      int4 item = t.list[entry];
+      while (item.x + item.w <= in) item = t.list[++entry];
+      entry = uniform(entry);
+      const int s = uniform(item.y), at = uniform(item.x), all = uniform(item.w);
+      row_tile = uniform(item.z);
       q = sequence_of(a, s);
       pages = a.pages + s * a.ldp;
-      const int at = uniform(t.cum[entry]);
-      tiles = uniform(t.cum[entry + 1]) - at;
-      first = in - at;
-      last = min(tiles, first + (end - u));
+      tiles = all - kSegmentCost;
+      units = min(all - (in - at), end - u);
+      first = max(0, in - at - kSegmentCost);
+      last = max(0, in - at + units - kSegmentCost);
+      if (first >= last) {  // nothing but the cost
+        u += units;
+        if (in + units == one) entry = 0;
+        continue;
+      }
     }
     // this lane's row
     const int64_t row = (int64_t)row_tile * R + 32 * wave + r;
@@ -334,9 +366,6 @@ __global__ __launch_bounds__(64 * WAVES, HD == 256 && WAVES == 4 ? 1 : 2) void a
       }
     }
     if constexpr (Q16) qsum += __shfl_xor(qsum, 32);
-    // arrived before the loop: a wait for them in it would wait for the tiles that are on their way to LDS as well
-#pragma unroll
-    for (int w = 0; w < KS; ++w) asm volatile("" : "+v"(qf[w]));
 
     f32x16 o[TD];
 #pragma unroll
@@ -344,174 +373,245 @@ __global__ __launch_bounds__(64 * WAVES, HD == 256 && WAVES == 4 ? 1 : 2) void a
 #pragma unroll
       for (int e = 0; e < 16; ++e) o[i][e] = 0.f;
     float m = kNone, l = 0.f;  // m: in bits (times c)
-    int v_run = 0;             // exponent of O
+    int v_run = 0, v_exp = 0;  // exponents of O, of the values at hand
+    unsigned long long odd = 0ull;
     Loader ld;
-    TileInfo info = {0, 0ull}, info_next = {0, 0ull};
 
-    PageWindow window;
-    const int* window_of = nullptr;
-    // the block of tile `tile` and how many of its tokens exist; null: none that can be seen
-    auto block_of = [&](int tile, int& there) -> const char* {
-      const bool own = tile >= prefix_tiles;
-      const int k = own ? tile - prefix_tiles : tile, len = own ? q.len : t.prefix_len;
-      there = min(len - k * 64, 64);
-      if (there <= 0) return nullptr;
-      const int* table = own ? pages : t.prefix_pages;
-      if (window_of != table) window.count = 0;
-      window_of = table;
-      const int64_t page = window.get(table, k >> page_blocks, (len + 63 >> 6) + (1 << page_blocks) - 1 >> page_blocks);
-      if (page < 0 || page >= a.cache.n_pages) return nullptr;
-      return uniform_ptr(a.cache.data + kv_block_offset<KV, HD>(a.cache, page, head, k & ((1 << page_blocks) - 1)));
+    // Offsets of 64 tiles' blocks, one a lane, looked up together; those of tiles without a block are negative.
+    int64_t window = -1;
+    int window_from = first, window_end = first;
+    const int64_t head_at = kv_block_offset<KV, HD>(a.cache, 0, head, 0), page_bytes = kv_block_offset<KV, HD>(a.cache, 1, 0, 0);
+    auto state_of = [&](int tile) {
+      if (tile >= window_end) {
+        window_from = tile;
+        window_end = tile + 64;
+        const int at = tile + lane;
+        const bool own = at >= prefix_tiles;
+        const int k = own ? at - prefix_tiles : at;
+        window = -1;
+        if (at < last && k * 64 < (own ? q.len : t.prefix_len)) {
+          const int page = (own ? pages : t.prefix_pages)[k >> page_blocks];
+          if (page >= 0 && page < a.cache.n_pages)
+            window = head_at + page * page_bytes + (k & ((1 << page_blocks) - 1)) * (int64_t)kv_block_bytes<KV, HD>();
+        }
+      }
+      TileState x;
+      const int hi = __builtin_amdgcn_readlane((int)(window >> 32), tile - window_from);
+      x.block = (int64_t)hi << 32 | (uint32_t)__builtin_amdgcn_readlane((int)window, tile - window_from);
+      const int k = tile - prefix_tiles;
+      x.base = k >= 0 ? k * 64 : -1;
+      x.there = min((k >= 0 ? q.len : t.prefix_len) - (k >= 0 ? k : tile) * 64, 64);
+      if (hi < 0) x.there = 0, x.block = 0;
+      return x;
+    };
+    auto masked_of = [&](const TileState& x) { return x.there < 64 || (x.base >= 0 && x.base + 64 > all_see); };
+    auto seen_of = [&](const TileState& x) { return x.base >= 0 ? min(max(sees - x.base, 0), x.there) : x.there; };
+    // operands in LDS: the exchange puts n into bits of the address that only an exclusive or reaches.  Where a lane reads is worked out anew for
+    // each half tile: kept in registers, it would push others out to memory, and a wait for those is one for the copies under way
+    auto key_place = [&] {
+      const int l = Loader::thread() & 63, k = (l & 0x13) | (l & 4) << 1 | (l & 8) >> 1;
+      return k * Loader::ROWB + (((l >> 5) ^ (k & Loader::KMASK)) << 4);
+    };
+    auto value_place = [&] {
+      const int l = Loader::thread() & 63;
+      return (l & 31) * 128 + (((l >> 5) ^ (l & 7)) << 4);
+    };
+    auto key_operand = [&](int place, int at, int n) {  // (keys 32 further on have the same low bits)
+      return *reinterpret_cast<const bf16x8*>(sh.keys[at] + (place ^ (n >> 1) << 5) + (n & 1) * (32 * Loader::ROWB));
+    };
+    auto value_operand = [&](int place, int at, int n) {  // (features too)
+      return *reinterpret_cast<const frag*>(sh.values[at] + (place ^ (n / TD) << 5) + n % TD * (32 * 128));
+    };
+    auto clear = [&](f32x16(&x)[2]) {
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) x[k][e] = KV == kKvU4 ? -128.f * qsum : 0.f;  // (codes of 4 bits enter as 128 + c)
+    };
+    // scores 2 i, 2 i + 1, in bits, from products
+    auto finish_scores = [&](f32x16(&x)[2], int at, int i) {
+      const int k = i >> 3, e = 2 * (i & 7);
+      if constexpr (Q16) {
+        const float4 p = *reinterpret_cast<const float4*>(&sh.par[at][32 * k + 16 * (e >> 3) + 8 * h + (e & 7)]);
+        x[k][e] = fmaf(x[k][e], p.x, p.y * qsum);
+        x[k][e + 1] = fmaf(x[k][e + 1], p.z, p.w * qsum);
+      } else {
+        x[k][e] *= c;
+        x[k][e + 1] *= c;
+      }
+    };
+    auto mask = [&](f32x16(&x)[2], int seen) {
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (32 * k + 16 * (e >> 3) + 8 * h + (e & 7) >= seen) x[k][e] = kNone;
+    };
+    auto largest = [&](const f32x16(&x)[2]) {
+      float most = fmaxf(x[0][0], x[1][0]);
+#pragma unroll
+      for (int e = 1; e < 16; ++e) most = fmaxf(most, fmaxf(x[0][e], x[1][e]));
+      return most;
     };
 
-    int there = 0, there_next = 0;
-    const char* block = block_of(first, there);
-    __syncthreads();  // the buffers are free (the last segment's tile was read)
-    if (block) {
-      ld.begin(block, sh.data[0]);
-      ld.finish(sh, 0, there, c, v_run, info);
+    // bf16: the i-th of 2 STEPS pieces that a wave copies of a tile, keys first
+    const int copy_at = uniform(wave * Loader::STEPS * 1024);
+    auto copy = [&](int64_t block, int at, int i) {
+      const bool key = i < Loader::STEPS;
+      const int j = key ? i : i - Loader::STEPS, from = key ? Loader::key_source() ^ Loader::key_turn(j) : Loader::value_source();
+      to_lds_16(from + 1024 * j, a.cache.data + block, uniform((int)(uintptr_t)(key ? sh.keys[at] : sh.values[at]) + copy_at + 1024 * j));
+    };
+    // bf16: in a tile that not all rows see all of, what a wave has copied of the values (arrived, in buffer `at`) is gone through: 0 NaN = NaN, so what
+    // is not finite goes in as 0 (and is noted), and so does what lies behind the last token
+    auto clean = [&](const TileState& x, int at) {
+      unsigned long long which = 0ull;
+#pragma unroll
+      for (int i = 0; i < Loader::STEPS; ++i) {
+        const int piece = (copy_at + 1024 * i >> 4) + lane, chunk = (piece & 7) ^ (piece >> 3 & 7);
+        u32x4* from = reinterpret_cast<u32x4*>(sh.values[at]) + piece;
+        u32x4 d = *from;
+        unsigned bits = 0u;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          const int k = 8 * chunk + 2 * w;
+          d[w] = k >= x.there ? 0u : k + 1 >= x.there ? d[w] & 0xffffu : d[w];
+          if ((d[w] & 0x7f80u) == 0x7f80u) bits |= 1u << (2 * w), d[w] &= 0xffff0000u;
+          if ((d[w] & 0x7f800000u) == 0x7f800000u) bits |= 2u << (2 * w), d[w] &= 0xffffu;
+        }
+        *from = d;
+        which |= (unsigned long long)bits << (8 * chunk);
+      }
+      unsigned long long all = 0ull;
+      if (__any(which != 0ull))
+        for (int j = 0; j < 64; ++j) all |= (unsigned long long)(__any(which >> j & 1ull) ? 1 : 0) << j;
+      if (lane == 0) sh.odd[at][wave] = all;
+    };
+
+    TileState now = state_of(first);
+    __syncthreads();  // the buffers are free (the last segment's tiles were read)
+    if constexpr (Q16) {
+      ld.ask_keys(a.cache.data + now.block);
+      ld.ask_values(a.cache.data + now.block);
+      ld.put_keys(sh, 0, now.there, c);
+      v_exp = ld.put_values(sh, 0, now.there, v_run, odd);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 2 * Loader::STEPS; ++i) copy(now.block, 0, i);
     }
+    // queries arrived before the loop: a wait for them in it would wait for the tiles that are on their way to LDS as well
+#pragma unroll
+    for (int w = 0; w < KS; ++w) asm volatile("" : "+v"(qf[w]));
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    if (!Q16 && masked_of(now)) clean(now, 0);
     __syncthreads();
 
     for (int tile = first; tile < last; ++tile) {
-      const int buf = (tile - first) & 1;
-      const char* next = nullptr;
-      if (tile + 1 < last) {
-        next = block_of(tile + 1, there_next);
-        if (next) ld.begin(next, sh.data[buf ^ 1]);
+      const int at = tile - first & 1;
+      const TileState next = state_of(tile + 1);
+      if constexpr (Q16) {
+        ld.ask_keys(a.cache.data + next.block);
+        ld.ask_values(a.cache.data + next.block);
       }
-      const bool own = tile >= prefix_tiles;
-      const int base = own ? (tile - prefix_tiles) * 64 : 0;
-      const bool masked = own ? base + 64 > all_see : there < 64;
-      const int seen = own ? min(max(sees - base, 0), there) : there;
-      if (block) {
-        char* kb = sh.data[buf];
-        unsigned long long odd = info.odd;
-        if constexpr (!Q16) {
-          if (masked) {  // what a row does not see may be anything, and 0 NaN = NaN
-            if (threadIdx.x < 2) sh.odd[threadIdx.x] = 0u;
-            __syncthreads();
+      f32x16 x[2];
+      clear(x);
+      {
+        const int place = key_place();
+        pipelined<2 * KS>([&](int n) { return key_operand(place, at, n); }, [&](int n, bf16x8 f) { x[n & 1] = mfma32(f, qf[n >> 1], x[n & 1]); },
+                          [&](int n) {
+                            if constexpr (!Q16) {
+                              constexpr int EVERY = KS / Loader::STEPS;
+                              if (n % EVERY == 0) copy(next.block, at ^ 1, n / EVERY);
+                            }
+                          });
+      }
 #pragma unroll
-            for (int i = 0; i < HD * 8 / (64 * WAVES); ++i) {
-              const int piece = threadIdx.x + i * 64 * WAVES, f = piece >> 3, chunk = (piece & 7) ^ (f & 7);
-              u32x4* p = reinterpret_cast<u32x4*>(kb + Shared::kKeys + piece * 16);
-              u32x4 d = *p;
-              unsigned which = 0u;
+      for (int i = 0; i < 16; ++i) finish_scores(x, at, i);
+      if (masked_of(now)) mask(x, seen_of(now));
+      float most = largest(x);
+      int shift = 0;
+      if constexpr (Q16) {
+        if (v_exp > v_run) {
+          const float f = v_run - v_exp > -126 ? __uint_as_float((unsigned)(127 + v_run - v_exp) << 23) : 0.f;
 #pragma unroll
-              for (int w = 0; w < 4; ++w) {
-                const int at = 8 * chunk + 2 * w;
-                d[w] = at >= there ? 0u : at + 1 >= there ? d[w] & 0xffffu : d[w];
-                if ((d[w] & 0x7f80u) == 0x7f80u) which |= 1u << (2 * w), d[w] &= 0xffff0000u;
-                if ((d[w] & 0x7f800000u) == 0x7f800000u) which |= 2u << (2 * w), d[w] &= 0xffffu;
-              }
-              *p = d;
-              if (which) atomicOr(&sh.odd[chunk >> 2], which << (8 * (chunk & 3)));
-            }
-            __syncthreads();
-            odd = (unsigned long long)sh.odd[1] << 32 | sh.odd[0];
-          }
+          for (int i = 0; i < TD; ++i) o[i] *= f;
+          v_run = v_exp;
         }
-        f32x16 x[2];
+        shift = v_exp - v_run;  // at least -60
+      }
+      {
+        const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(most), __float_as_uint(most), false, false);
+        most = fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1]));
+      }
+      if (__any(most > m + 8.f)) {
+        const float raised = fmaxf(m, most), shrink = raised == kNone ? 1.f : __builtin_amdgcn_exp2f(m - raised);
+        l *= shrink;
 #pragma unroll
-        for (int k = 0; k < 2; ++k)
+        for (int i = 0; i < TD; ++i) o[i] *= shrink;
+        m = raised;
+      }
+      const float mb = (m == kNone ? 0.f : m) - (float)shift;
+      frag pf[4];
+      float sum[2] = {0.f, 0.f}, even = 0.f;
+      auto exponential = [&](int i) {
+        const int k = i >> 4, e = i & 15;
+        const float v = __builtin_amdgcn_exp2f(x[k][e] - mb);
+        sum[e & 1] += v;
+        if constexpr (!Q16) pf[2 * k + (e >> 3)][e & 7] = (bf16)v;
+        else if (e & 1) put_pair(pf[2 * k + (e >> 3)], e & 6, even, v);
+        else even = v;
+      };
 #pragma unroll
-          for (int e = 0; e < 16; ++e) x[k][e] = KV == kKvU4 ? -128.f * qsum : 0.f;  // (codes of 4 bits enter as 128 + c)
-        {
-          // (keys 32 further on have the same low bits)
-          const int key = (r & 0x13) | (r & 4) << 1 | (r & 8) >> 1;
-          const char* from = kb + key * Loader::ROWB;
-          pipelined<2 * KS>(
-              [&](int n) {
-                return *reinterpret_cast<const bf16x8*>(from + (n & 1) * (32 * Loader::ROWB) + (((2 * (n >> 1) + h) ^ (key & Loader::KMASK)) << 4));
-              },
-              [&](int n, bf16x8 f) { x[n & 1] = mfma32(f, qf[n >> 1], x[n & 1]); });
+      for (int i = 0; i < 8; ++i) exponential(i);
+      {
+        const int place = value_place();
+        pipelined<4 * TD>([&](int n) { return value_operand(place, at, n); }, [&](int n, frag f) { o[n % TD] = mfma32(f, pf[n / TD], o[n % TD]); },
+                          [&](int n) {  // for the next sixteen keys
+                            if (n < 3 * TD) {
+#pragma unroll
+                              for (int i = 8 + 8 * n / TD; i < 8 + 8 * (n + 1) / TD; ++i) exponential(i);
+                            }
+                          });
+      }
+      const float all = sum[0] + sum[1];
+      l += Q16 ? all * __uint_as_float((unsigned)(127 - shift) << 23) : all;
+      if constexpr (!Q16) {
+        odd = 0ull;
+        if (masked_of(now)) {
+#pragma unroll
+          for (int w = 0; w < WAVES; ++w) odd |= sh.odd[at][w];
+          odd = (unsigned long long)(uint32_t)uniform((int)(odd >> 32)) << 32 | (uint32_t)uniform((int)odd);
         }
+      }
+      if (odd) {
+        const int seen = seen_of(now);
+        const unsigned long long mine = seen >= 64 ? ~0ull : (1ull << seen) - 1;
         if constexpr (Q16) {
+          const float add = odd & mine ? __builtin_nanf("") : 0.f;
 #pragma unroll
-          for (int k = 0; k < 2; ++k)
-#pragma unroll
-            for (int e = 0; e < 16; e += 2) {
-              const float4 kp = *reinterpret_cast<const float4*>(&sh.keys[buf][32 * k + 16 * (e >> 3) + 8 * h + (e & 7)]);
-              x[k][e] = fmaf(x[k][e], kp.x, kp.y * qsum);
-              x[k][e + 1] = fmaf(x[k][e + 1], kp.z, kp.w * qsum);
-            }
-        }
-        if (masked) {
-#pragma unroll
-          for (int k = 0; k < 2; ++k)
-#pragma unroll
-            for (int e = 0; e < 16; ++e)
-              if (32 * k + 16 * (e >> 3) + 8 * h + (e & 7) >= seen) x[k][e] = kNone;
-        }
-        int shift = 0;
-        if constexpr (Q16) {
-          if (info.v_exp > v_run) {
-            const float f = v_run - info.v_exp > -126 ? __uint_as_float((unsigned)(127 + v_run - info.v_exp) << 23) : 0.f;
-#pragma unroll
-            for (int i = 0; i < TD; ++i) o[i] *= f;
-            v_run = info.v_exp;
-          }
-          shift = info.v_exp - v_run;  // at least -60
-        }
-        float most = fmaxf(x[0][0], x[1][0]);
-#pragma unroll
-        for (int e = 1; e < 16; ++e) most = fmaxf(most, fmaxf(x[0][e], x[1][e]));
-        most = fmaxf(most, __shfl_xor(most, 32));
-        if constexpr (!Q16) most *= c;
-        if (__any(most > m + 8.f)) {
-          const float raised = fmaxf(m, most), shrink = raised == kNone ? 1.f : __builtin_amdgcn_exp2f(m - raised);
-          l *= shrink;
-#pragma unroll
-          for (int i = 0; i < TD; ++i) o[i] *= shrink;
-          m = raised;
-        }
-        const float mb = (m == kNone ? 0.f : m) - (float)shift;
-        frag pf[4];
-        float sum[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int k = 0; k < 2; ++k)
-#pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            const float p = __builtin_amdgcn_exp2f(Q16 ? x[k][e] - mb : fmaf(x[k][e], c, -mb));
-            sum[e & 3] += p;
-            pf[2 * k + (e >> 3)][e & 7] = (elem)p;
-          }
-        const float all = (sum[0] + sum[1]) + (sum[2] + sum[3]);
-        l += Q16 ? all * __uint_as_float((unsigned)(127 - shift) << 23) : all;
-        {
-          const char* from = kb + Shared::kKeys + r * 128;  // (features 32 further on have the same low bits)
-          pipelined<4 * TD>([&](int n) { return *reinterpret_cast<const frag*>(from + n % TD * (32 * 128) + (((2 * (n / TD) + h) ^ (r & 7)) << 4)); },
-                            [&](int n, frag f) { o[n % TD] = mfma32(f, pf[n / TD], o[n % TD]); });
-        }
-        if (odd) {
-          const unsigned long long mine = seen >= 64 ? ~0ull : (1ull << seen) - 1;
-          if constexpr (Q16) {
-            const float add = odd & mine ? __builtin_nanf("") : 0.f;
-#pragma unroll
-            for (int i = 0; i < TD; ++i) o[i] += add;
-          } else {
-            const bf16* v = reinterpret_cast<const bf16*>(block + Loader::kHalf) + 4 * h * kBlockTokens;
+          for (int i = 0; i < TD; ++i) o[i] += add;
+        } else {
+          const bf16* v = reinterpret_cast<const bf16*>(a.cache.data + now.block + Loader::kHalf) + 4 * h * kBlockTokens;
 #pragma unroll 1
-            for (unsigned long long left = odd; left; left &= left - 1) {
-              const int j = __builtin_ctzll(left);
+          for (; odd; odd &= odd - 1) {
+            const int j = __builtin_ctzll(odd);
 #pragma unroll
-              for (int i = 0; i < TD; ++i)
+            for (int i = 0; i < TD; ++i)
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                  const float y = (float)v[(32 * i + (e & 3) + 8 * (e >> 2)) * kBlockTokens + j];
-                  if (j < seen && !(fabsf(y) <= kHuge)) o[i][e] += y;
-                }
-            }
+              for (int e = 0; e < 16; ++e) {
+                const float w = (float)v[(32 * i + (e & 3) + 8 * (e >> 2)) * kBlockTokens + j];
+                if (j < seen && !(fabsf(w) <= kHuge)) o[i][e] += w;
+              }
           }
         }
       }
-      if (next) ld.finish(sh, buf ^ 1, there_next, c, v_run, info_next);
+      if constexpr (Q16) {
+        ld.put_keys(sh, at ^ 1, next.there, c);
+        v_exp = ld.put_values(sh, at ^ 1, next.there, v_run, odd);
+      }
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      if (!Q16 && masked_of(next)) clean(next, at ^ 1);
       __syncthreads();
-      block = next;
-      info = info_next;
-      there = there_next;
+      now = next;
     }
 
     l += __shfl_xor(l, 32);
@@ -547,8 +647,9 @@ __global__ __launch_bounds__(64 * WAVES, HD == 256 && WAVES == 4 ? 1 : 2) void a
       }
     }
     if constexpr (PREFIX) break;
-    if (first == 0 && !whole) cut = int4{entry, head, (int)((unsigned)(u + tiles - 1) / (unsigned)per) - me + 1, 0};
-    u += last - first;
+    if (first == 0 && !whole) cut = int4{entry, head, (int)((unsigned)(u + (tiles - first) + (units - (last - first)) - 1) / (unsigned)per) - me + 1, 0};
+    u += units;
+    if (in + units == one) entry = 0;
   }
   if (!PREFIX && threadIdx.x == 0) t.cuts[me] = cut;
 }
@@ -582,9 +683,10 @@ __global__ __launch_bounds__(256) void join_tiles_kernel(TileArgs t) {
   const int4 cut = t.cuts[me];
   if (cut.z == 0) return;
   const AttendArgs& a = t.a;
-  const Sequence q = sequence_of(a, t.seq[cut.x]);
+  const int4 entry = t.list[cut.x];
+  const Sequence q = sequence_of(a, entry.y);
   const int r = blockIdx.y * (256 / TR) + threadIdx.x / TR, lane4 = 4 * (threadIdx.x % TR);
-  const int64_t row = (int64_t)t.row[cut.x] * R + r;
+  const int64_t row = (int64_t)entry.z * R + r;
   if (row >= (int64_t)q.count * a.group) return;
   const float2* ml = reinterpret_cast<const float2*>(t.part + (int64_t)2 * t.workers * R * HD);
   Joined j;

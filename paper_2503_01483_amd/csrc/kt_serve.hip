@@ -91,21 +91,23 @@ static KvCache device_cache(const kt_kv_cache* c) {
 constexpr int64_t kWaveWorkers = (int64_t)kNumCUs * 8;  // waves that share the key tiles of single tokens: two workgroups of four a CU
 constexpr int64_t kMaxTokens = (int64_t)1 << 30;         // of a sequence's pages, of a prefix
 constexpr int64_t kMaxSequences = 4096;                 // their tile counts are listed in LDS
-constexpr int kTileWaves = 8, kTileRows = 32 * kTileWaves;
-static int64_t tile_workers(int64_t hd) { return kNumCUs; }  // as many as are resident (LDS)
+// Waves of a workgroup of kt_attention_tiles.h: two a SIMD; one where a head of 256 features takes all registers.
+constexpr int tile_waves(int64_t hd) { return hd == 256 ? 4 : 8; }
+constexpr int64_t tile_rows(int64_t hd) { return 32 * tile_waves(hd); }
+constexpr int64_t kTileWorkers = kNumCUs;  // as many as are resident (LDS)
 
 // Single tokens (and few: up to 16 rows a head) take kt_attention.h, which reads each key for its own sequence only; what has more rows
-// takes kt_attention_tiles.h, whose tiles of 128 rows are wasted on fewer.
+// takes kt_attention_tiles.h, whose tiles of 256 rows are wasted on fewer.
 static bool few_rows(int64_t max_q, int64_t group) { return max_q * group <= kRows; }
 
 // Tiles of a prefix that single tokens share are split until the launch fills the card.
 static int64_t prefix_splits(int64_t n_tokens, int64_t hq, int64_t n_heads, int64_t hd, int64_t prefix_len) {
-  const int64_t items = ceil_div(n_tokens * (hq / n_heads), kTileRows) * n_heads;
-  return std::max<int64_t>(1, std::min(tile_workers(hd) / items, ceil_div(prefix_len, 64)));
+  const int64_t items = ceil_div(n_tokens * (hq / n_heads), tile_rows(hd)) * n_heads;
+  return std::max<int64_t>(1, std::min(kTileWorkers / items, ceil_div(prefix_len, 64)));
 }
 
 struct AttendPlan {
-  size_t tiles, cuts, part, whole, prefix, seq, row, bytes;
+  size_t tiles, list, cuts, part, whole, prefix, bytes;
 };
 // Offsets in the workspace; sized for either kernel (hq rows a token, at most kMaxSequences).
 static AttendPlan plan_attention(int64_t n_tokens, int64_t hq, int64_t hd, int64_t prefix_len) {
@@ -116,16 +118,15 @@ static AttendPlan plan_attention(int64_t n_tokens, int64_t hq, int64_t hd, int64
     at += (size_t)round_up(bytes, 256);
     return o;
   };
-  const int64_t entries = n_tokens * hq / kTileRows + kMaxSequences + 1, row = (hd + 2) * 4;
-  p.tiles = take(4 * std::max(entries, kMaxSequences + 1));
-  p.seq = take(4 * entries);
-  p.row = take(4 * entries);
+  const int64_t row = (hd + 2) * 4;
+  p.tiles = take(4 * (kMaxSequences + 1));
+  p.list = take(16 * (n_tokens * hq / tile_rows(hd) + kMaxSequences + 1));
   p.cuts = take(16 * kWaveWorkers);
-  p.part = take(2 * std::max(kWaveWorkers * kRows, tile_workers(hd) * kTileRows) * row);
+  p.part = take(2 * std::max(kWaveWorkers * kRows, kTileWorkers * tile_rows(hd)) * row);
   if (prefix_len) {
     p.whole = take(n_tokens * hq * row);
     // splits x rows: at most all rows once, or as many as fill the card
-    p.prefix = take(std::max(n_tokens * hq, tile_workers(hd) * kTileRows) * row);
+    p.prefix = take(std::max(n_tokens * hq, kTileWorkers * tile_rows(hd)) * row);
   }
   p.bytes = at;
   return p;
@@ -133,10 +134,10 @@ static AttendPlan plan_attention(int64_t n_tokens, int64_t hq, int64_t hd, int64
 
 template <int KV, int HD, bool PREFIX>
 static bool launch_tiles(const TileArgs& t, int64_t wgs, hipStream_t st) {
-  constexpr size_t lds = sizeof(TileShared<KV, HD, kTileWaves>);
-  auto kernel = attend_tiles_kernel<KV, HD, kTileWaves, PREFIX>;
+  constexpr size_t lds = sizeof(TileShared<KV, HD, tile_waves(HD)>);
+  auto kernel = attend_tiles_kernel<KV, HD, tile_waves(HD), PREFIX>;
   if (!ensure_dynamic_lds(reinterpret_cast<const void*>(kernel), lds)) return false;
-  kernel<<<dim3((unsigned)wgs), 64 * kTileWaves, lds, st>>>(t);
+  kernel<<<dim3((unsigned)wgs), 64 * tile_waves(HD), lds, st>>>(t);
   return true;
 }
 
@@ -276,14 +277,13 @@ kt_status kt_paged_attention(const kt_kv_cache* cache, const void* Q, int64_t ld
 
   const int64_t group = n_q_heads / cache->n_heads;
   const bool few = few_rows(max_q, group);
-  const int64_t entries = few ? n_seq : n_tokens * group / kTileRows + n_seq;
-  if (entries > INT32_MAX / cache->n_heads / (ceil_div(ldp * cache->page_size, 64) + (few ? 0 : ceil_div(prefix_len, 64))))
+  const int64_t entries = few ? n_seq : n_tokens * group / tile_rows(hd) + n_seq;
+  if (entries > INT32_MAX / cache->n_heads / (ceil_div(ldp * cache->page_size, 64) + (few ? 0 : ceil_div(prefix_len, 64) + kSegmentCost)))
     return fail(KT_ERR_NOT_SUPPORTED, "too many tiles of 64 keys for one call: hand in a narrower page table or fewer tokens");
 
   const AttendPlan p = plan_attention(n_tokens, n_q_heads, hd, prefix_len);
   char* ws = static_cast<char*>(workspace);
   auto floats = [&](size_t at) { return reinterpret_cast<float*>(ws + at); };
-  auto ints = [&](size_t at) { return reinterpret_cast<int*>(ws + at); };
   TileArgs t{};
   AttendArgs& a = t.a;
   a.cache = device_cache(cache);
@@ -302,28 +302,27 @@ kt_status kt_paged_attention(const kt_kv_cache* cache, const void* Q, int64_t ld
   a.ldo = ldo;
   a.lse = lse;
   a.workers = (int)kWaveWorkers;
-  a.tiles = t.cum = ints(p.tiles);
+  a.tiles = reinterpret_cast<int*>(ws + p.tiles);
+  t.list = reinterpret_cast<int4*>(ws + p.list);
   a.cuts = t.cuts = reinterpret_cast<int4*>(ws + p.cuts);
   a.part = t.part = floats(p.part);
   a.whole = prefix_len ? floats(p.whole) : nullptr;
   t.prefix_pages = prefix_pages;
   t.prefix_len = (int)prefix_len;
-  t.workers = (int)tile_workers(hd);
+  t.workers = (int)kTileWorkers;
   t.entries = (int)entries;
-  t.seq = ints(p.seq);
-  t.row = ints(p.row);
   t.prefix_part = prefix_len ? floats(p.prefix) : nullptr;
   t.splits = prefix_len ? (int)prefix_splits(n_tokens, n_q_heads, cache->n_heads, hd, prefix_len) : 0;
   hipStream_t st = static_cast<hipStream_t>(stream);
   const bool ok = with_cache(cache, [&](auto kv, auto h) {
-    constexpr int KV = decltype(kv)::value, HD = decltype(h)::value, kRowsOf = 1024 / HD;  // rows of a workgroup that joins
+    constexpr int KV = decltype(kv)::value, HD = decltype(h)::value, kRowsOf = 1024 / HD, ROWS = tile_rows(HD);  // (rows of a workgroup that joins)
     if (!few) {
-      plan_tiles_kernel<kTileRows><<<1, 1024, 0, st>>>(t);
+      plan_tiles_kernel<ROWS><<<1, 1024, 0, st>>>(t);
       if (!launch_tiles<KV, HD, false>(t, t.workers, st)) return false;
-      join_tiles_kernel<HD, kTileRows><<<dim3((unsigned)t.workers, kTileRows / kRowsOf), 256, 0, st>>>(t);
+      join_tiles_kernel<HD, ROWS><<<dim3((unsigned)t.workers, ROWS / kRowsOf), 256, 0, st>>>(t);
       return true;
     }
-    if (prefix_len && !launch_tiles<KV, HD, true>(t, ceil_div(n_tokens * group, kTileRows) * cache->n_heads * t.splits, st)) return false;
+    if (prefix_len && !launch_tiles<KV, HD, true>(t, ceil_div(n_tokens * group, ROWS) * cache->n_heads * t.splits, st)) return false;
     attend_rows_kernel<KV, HD><<<dim3(kWaveWorkers / 4), 256, (size_t)(n_seq + 1) * 4, st>>>(a);
     if (prefix_len) join_prefix_kernel<HD><<<dim3((unsigned)ceil_div(n_tokens * n_q_heads, kRowsOf)), 256, 0, st>>>(t);
     else attend_join_kernel<HD><<<dim3(kWaveWorkers, 4), 256, 0, st>>>(a);
