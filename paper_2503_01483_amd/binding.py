@@ -321,43 +321,47 @@ def kt_quant_sensitivity(Y, alphas, *, bits=4, workspace=None, stream=None):
     return out, gamma
 
 
-def _operands(device, **tensors):
-    """All given tensors have to live on one device, the current one (a kernel is launched there)."""
-    for name, t in tensors.items():
-        if t is not None and (not t.is_cuda or t.get_device() != device):
-            raise ValueError(f"{name} is on {t.device}: operands have to be on the current device, cuda:{device}")
-
-
 def _device(t, name):
-    if not t.is_cuda:
-        raise ValueError(f"{name} is on {t.device}: a GPU tensor is needed")
-    return torch.cuda.current_device()
+    """The current device, which `t` has to be on (a kernel is launched there)."""
+    dev = t.get_device()
+    if dev < 0 or dev != torch.cuda.current_device():
+        raise ValueError(f"{name} is on {t.device}: operands have to be on the current device")
+    return dev
 
 
-def _index(t, name, dtype, shape):
-    if t.dtype != dtype or t.shape != shape or not t.is_contiguous():
-        raise ValueError(f"{name}: contiguous {dtype} of shape {tuple(shape)} needed, got {t.dtype} {tuple(t.shape)}")
+def _refuse(name, t, dev, dtype, what):
+    raise ValueError(f"{name}: {dtype} {what} on cuda:{dev} needed, got {t.dtype} {tuple(t.shape)}, strides {t.stride()}, on {t.device}")
 
 
-def _rows(t, name, shape=None, dtype=None):
-    """Leading dimension of a [n][width] tensor whose rows are contiguous; checks against `shape`, `dtype` where given."""
-    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1) or (shape is not None and t.shape != shape) or \
-            (dtype is not None and t.dtype != dtype):
-        raise ValueError(f"{name}: {dtype or 'a tensor'} of shape {tuple(shape) if shape else '[n, width]'} with contiguous rows "
-                         f"needed, got {t.dtype} {tuple(t.shape)}, strides {t.stride()}")
-    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+def _index(t, name, dev, dtype, shape):
+    """Address of a contiguous tensor of that type and shape."""
+    if t.get_device() != dev or t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
+        _refuse(name, t, dev, dtype, f"of shape {tuple(shape)}, contiguous,")
+    return t.data_ptr()
 
 
-def _heads(t, name, n, heads, head_dim, dtype=None):
-    """Leading dimension of [n][heads][head_dim] (or [n][heads * head_dim]) rows with their heads next to each other."""
-    if t.dim() == 3:
-        if t.shape != (n, heads, head_dim) or t.stride(2) != 1 or (heads > 1 and t.stride(1) != head_dim):
-            raise ValueError(f"{name}: [{n}, {heads}, {head_dim}] with contiguous rows of heads needed, got {tuple(t.shape)}, "
-                             f"strides {t.stride()}")
-        if dtype is not None and t.dtype != dtype:
-            raise ValueError(f"{name}: {dtype} needed, got {t.dtype}")
-        return t.stride(0) if n > 1 else max(t.stride(0), heads * head_dim)
-    return _rows(t, name, (n, heads * head_dim), dtype)
+def _rows(t, name, dev, dtype, shape):
+    """Leading dimension of a tensor of shape [n, width] with contiguous rows."""
+    if t.get_device() != dev or t.dtype is not dtype or t.shape != shape:
+        _refuse(name, t, dev, dtype, f"of shape {tuple(shape)}")
+    ld, one = t.stride()
+    n, width = shape
+    if (one != 1 and width > 1) or (ld < width and n > 1):
+        _refuse(name, t, dev, dtype, "with contiguous rows")
+    return ld if ld > width else width
+
+
+def _heads(t, name, dev, dtype, n, heads, head_dim):
+    """Leading dimension of [n, heads, head_dim] (or [n, heads * head_dim]) rows with their heads next to each other."""
+    if t.dim() != 3:
+        return _rows(t, name, dev, dtype, (n, heads * head_dim))
+    if t.get_device() != dev or t.dtype is not dtype or t.shape != (n, heads, head_dim):
+        _refuse(name, t, dev, dtype, f"of shape {(n, heads, head_dim)}")
+    ld, of_head, one = t.stride()
+    width = heads * head_dim
+    if one != 1 or (of_head != head_dim and heads > 1) or (ld < width and n > 1):
+        _refuse(name, t, dev, dtype, "with contiguous rows of heads")
+    return ld if ld > width else width
 
 
 _CODE_TYPES = {KT_Q_INT4: (torch.int8,), KT_Q_INT8: (torch.int8,), KT_Q_E4M3: (torch.float8_e4m3fn, torch.uint8)}
@@ -366,22 +370,30 @@ _CODE_TYPES = {KT_Q_INT4: (torch.int8,), KT_Q_INT8: (torch.int8,), KT_Q_E4M3: (t
 def kt_add_rmsnorm_quant(X, *, res=None, gain=None, eps=1e-6, clip_ratio=1.0, format=KT_Q_INT8, res_out=None, Y=None,
                          codes=None, scales=None, stream=None):
     """Norm of the rows of X (+ res) [n][d] and their codes.  Writes the outputs that are given; returns (codes, scales)."""
-    dev = _device(X, "X")
-    _operands(dev, X=X, res=res, gain=gain, res_out=res_out, Y=Y, codes=codes, scales=scales)
-    xdt, ldx = _dtype_code(X), _rows(X, "X")
-    n, d = X.shape
-    ld = [0 if t is None else _rows(t, name, X.shape, X.dtype) for name, t in (("res", res), ("res_out", res_out), ("Y", Y))]
-    if gain is not None and (gain.shape != (d,) or not gain.is_contiguous()):
-        raise ValueError(f"gain: [{d}], contiguous, needed, got {tuple(gain.shape)}")
+    dev, dtype, shape = _device(X, "X"), X.dtype, X.shape
+    if len(shape) != 2:
+        raise ValueError(f"X: [n, d] needed, got {tuple(shape)}")
+    n, d = shape
+    xdt = gdt = _dtype_code(X)
+    ldx = _rows(X, "X", dev, dtype, shape)
+    ldres = ldro = ldy = ldc = 0
+    pres = pgain = pro = py = pc = ps = None
+    if res is not None:
+        ldres, pres = _rows(res, "res", dev, dtype, shape), res.data_ptr()
+    if gain is not None:
+        gdt, pgain = _dtype_code(gain), _index(gain, "gain", dev, gain.dtype, (d,))
+    if res_out is not None:
+        ldro, pro = _rows(res_out, "res_out", dev, dtype, shape), res_out.data_ptr()
+    if Y is not None:
+        ldy, py = _rows(Y, "Y", dev, dtype, shape), Y.data_ptr()
     if codes is not None:
         if codes.dtype not in _CODE_TYPES.get(format, ()):
             raise TypeError(f"codes of type {codes.dtype} do not fit format {format}")
-        ldc = _rows(codes, "codes", X.shape)
+        ldc, pc = _rows(codes, "codes", dev, codes.dtype, shape), codes.data_ptr()
     if scales is not None:
-        _index(scales, "scales", torch.float32, (n,))
-    _check(lib().kt_add_rmsnorm_quant(_ptr(X), ldx, _ptr(res), ld[0], _ptr(gain), n, d, xdt, xdt if gain is None else _dtype_code(gain),
-                                      eps, clip_ratio, format, _ptr(res_out), ld[1], _ptr(Y), ld[2], _ptr(codes),
-                                      0 if codes is None else ldc, _ptr(scales), _stream(stream)))
+        ps = _index(scales, "scales", dev, torch.float32, (n,))
+    _check(lib().kt_add_rmsnorm_quant(X.data_ptr(), ldx, pres, ldres, pgain, n, d, xdt, gdt, eps, clip_ratio, format, pro, ldro, py, ldy,
+                                      pc, ldc, ps, _stream(stream)))
     return codes, scales
 
 
@@ -406,79 +418,86 @@ class KVCache:
 def kt_kv_append(cache, K, V, slots, *, Q=None, positions=None, rope=None, interleaved=False, hadamard=False, Q_out=None,
                  stream=None):
     """Rotated, quantised K and V [n][heads][head_dim] into `slots` [n] of the cache; returns the rotated queries (Q_out or new)."""
-    dev = _device(K, "K")
-    if Q is not None and Q_out is None:
-        Q_out = torch.empty(Q.shape, dtype=Q.dtype, device=Q.device)
-    _operands(dev, cache=cache.data, K=K, V=V, slots=slots, Q=Q, positions=positions, rope=rope, Q_out=Q_out)
-    n, hd, dt = K.shape[0], cache.head_dim, _dtype_code(K)
-    ldk, ldv = _heads(K, "K", n, cache.n_heads, hd), _heads(V, "V", n, cache.n_heads, hd, K.dtype)
-    _index(slots, "slots", torch.int64, (n,))
-    hq = ldq = ldqo = 0
+    dev, dtype, n = _device(K, "K"), K.dtype, K.shape[0]
+    dt, hd, data = _dtype_code(K), cache.head_dim, cache.data
+    _index(data, "cache", dev, torch.uint8, data.shape)
+    ldk, ldv = _heads(K, "K", dev, dtype, n, cache.n_heads, hd), _heads(V, "V", dev, dtype, n, cache.n_heads, hd)
+    pslots = _index(slots, "slots", dev, torch.int64, (n,))
+    hq = ldq = ldqo = n_pos = rot = 0
+    pq = pqo = ppos = prope = None
     if Q is not None:
+        if Q_out is None:
+            Q_out = torch.empty(Q.shape, dtype=Q.dtype, device=Q.device)
         hq = Q.numel() // (n * hd) if n else 0
-        ldq, ldqo = _heads(Q, "Q", n, hq, hd, K.dtype), _heads(Q_out, "Q_out", n, hq, hd, K.dtype)
+        ldq, ldqo = _heads(Q, "Q", dev, dtype, n, hq, hd), _heads(Q_out, "Q_out", dev, dtype, n, hq, hd)
+        pq, pqo = Q.data_ptr(), Q_out.data_ptr()
     elif Q_out is not None:
         raise ValueError("Q_out without Q")
-    n_pos = rot = 0
     if rope is not None:
-        if positions is None:
-            raise ValueError("positions are needed with rope")
-        _index(positions, "positions", torch.int32, (n,))
-        if rope.dim() != 2:
-            raise ValueError("rope: [n_pos, rot_dim] needed")
-        _index(rope, "rope", torch.float32, rope.shape)
+        if positions is None or rope.dim() != 2:
+            raise ValueError("rope: [n_pos, rot_dim] needed, and positions with it")
+        ppos, prope = _index(positions, "positions", dev, torch.int32, (n,)), _index(rope, "rope", dev, torch.float32, rope.shape)
         n_pos, rot = rope.shape
-    _check(lib().kt_kv_append(cache.ref, _ptr(Q), ldq, _ptr(K), ldk, _ptr(V), ldv, n, hq, dt, _ptr(slots),
-                              _ptr(positions) if rope is not None else None, _ptr(rope), n_pos, rot, bool(interleaved),
-                              bool(hadamard), _ptr(Q_out), ldqo, _stream(stream)))
+    _check(lib().kt_kv_append(cache.ref, pq, ldq, K.data_ptr(), ldk, V.data_ptr(), ldv, n, hq, dt, pslots, ppos, prope, n_pos, rot,
+                              bool(interleaved), bool(hadamard), pqo, ldqo, _stream(stream)))
     return Q_out
 
 
 def kt_kv_gather(cache, slots, *, K=None, V=None, dtype=torch.bfloat16, stream=None):
-    """The values held in `slots` [n]: (K, V) [n][heads][head_dim], those given or, if neither is, new ones of `dtype`."""
-    dev = _device(slots, "slots")
-    n = slots.shape[0]
+    """The values held in `slots` [n]: (K, V) [n][heads][head_dim], those given or, if neither is, new ones of `dtype` (zeros for slots
+    outside the cache)."""
+    dev, n, data = _device(slots, "slots"), slots.shape[0], cache.data
     if K is None and V is None:
         K, V = (torch.zeros(n, cache.n_heads, cache.head_dim, dtype=dtype, device=slots.device) for _ in range(2))
-    _operands(dev, cache=cache.data, slots=slots, K=K, V=V)
-    _index(slots, "slots", torch.int64, (n,))
+    _index(data, "cache", dev, torch.uint8, data.shape)
+    pslots = _index(slots, "slots", dev, torch.int64, (n,))
     first = K if K is not None else V
-    ld = [0 if t is None else _heads(t, name, n, cache.n_heads, cache.head_dim, first.dtype) for name, t in (("K", K), ("V", V))]
-    _check(lib().kt_kv_gather(cache.ref, _ptr(slots), n, _ptr(K), ld[0], _ptr(V), ld[1], _dtype_code(first), _stream(stream)))
+    ldk = ldv = 0
+    pk = pv = None
+    if K is not None:
+        ldk, pk = _heads(K, "K", dev, first.dtype, n, cache.n_heads, cache.head_dim), K.data_ptr()
+    if V is not None:
+        ldv, pv = _heads(V, "V", dev, first.dtype, n, cache.n_heads, cache.head_dim), V.data_ptr()
+    _check(lib().kt_kv_gather(cache.ref, pslots, n, pk, ldk, pv, ldv, _dtype_code(first), _stream(stream)))
     return K, V
 
 
 def kt_paged_attention(Q, cache, pages, lens, *, q_starts=None, max_q=1, prefix_pages=None, prefix_len=0, scale=None, out=None,
                        lse=None, workspace=None, stream=None):
     """Attention of Q [n_tokens][heads][head_dim] over the cache; returns out (given or new).  scale: 1 / sqrt(head_dim)."""
-    dev = _device(Q, "Q")
+    dev, dtype, data = _device(Q, "Q"), Q.dtype, cache.data
     if Q.dim() != 3:
         raise ValueError(f"Q: [n_tokens, heads, head_dim] needed, got {tuple(Q.shape)}")
     n, hq, hd = Q.shape
-    if out is None:
-        out = (torch.empty if q_starts is None else torch.zeros)(n, hq, hd, dtype=Q.dtype, device=Q.device)
+    if hd != cache.head_dim:
+        raise ValueError(f"Q: heads of {hd} features, {cache.head_dim} in the cache")
+    if out is None:     # (rows in no sequence are not written)
+        out = (torch.empty if q_starts is None else torch.zeros)(n, hq, hd, dtype=dtype, device=Q.device)
     ws = workspace if workspace is not None else Workspace(Q.device)
-    _operands(dev, Q=Q, cache=cache.data, pages=pages, lens=lens, q_starts=q_starts, prefix_pages=prefix_pages, out=out, lse=lse)
+    _index(data, "cache", dev, torch.uint8, data.shape)
     n_seq = lens.shape[0]
-    ldq, ldo = _heads(Q, "Q", n, hq, cache.head_dim), _heads(out, "out", n, hq, cache.head_dim, Q.dtype)
-    _index(lens, "lens", torch.int32, (n_seq,))
-    if pages.dim() != 2 or pages.shape[0] != n_seq:
+    ldq, ldo = _heads(Q, "Q", dev, dtype, n, hq, hd), _heads(out, "out", dev, dtype, n, hq, hd)
+    plens = _index(lens, "lens", dev, torch.int32, (n_seq,))
+    if pages.dim() != 2:
         raise ValueError(f"pages: [{n_seq}, pages of a sequence] needed, got {tuple(pages.shape)}")
-    _index(pages, "pages", torch.int32, pages.shape)
+    ldp = pages.shape[1]
+    ppages = _index(pages, "pages", dev, torch.int32, (n_seq, ldp))
+    pstarts = pprefix = plse = None
     if q_starts is not None:
-        _index(q_starts, "q_starts", torch.int32, (n_seq + 1,))
+        pstarts = _index(q_starts, "q_starts", dev, torch.int32, (n_seq + 1,))
     if prefix_len:
         if prefix_pages is None or prefix_pages.dim() != 1 or prefix_pages.shape[0] * cache.page_size < prefix_len:
             raise ValueError("prefix_pages: one dimension of pages for prefix_len tokens needed")
-        _index(prefix_pages, "prefix_pages", torch.int32, prefix_pages.shape)
+        pprefix = _index(prefix_pages, "prefix_pages", dev, torch.int32, prefix_pages.shape)
     if lse is not None:
-        _index(lse, "lse", torch.float32, (n, hq))
-    need = lib().kt_paged_attention_bytes(n, hq, cache.head_dim, prefix_len)
-    buf = ws.get(need)
-    _check(lib().kt_paged_attention(cache.ref, _ptr(Q), ldq, _dtype_code(Q), _ptr(q_starts), _ptr(lens), _ptr(pages), pages.shape[1], n_seq, n,
-                                    max_q, hq, _ptr(prefix_pages) if prefix_len else None, prefix_len,
-                                    cache.head_dim ** -0.5 if scale is None else scale, _ptr(out), ldo, _ptr(lse), _ptr(buf), buf.numel(),
-                                    _stream(stream)))
+        plse = _index(lse, "lse", dev, torch.float32, (n, hq))
+    L = lib()
+    buf = ws.get(L.kt_paged_attention_bytes(n, hq, hd, prefix_len))
+    if buf.get_device() != dev:
+        raise ValueError(f"workspace is on {buf.device}: operands have to be on the current device")
+    _check(L.kt_paged_attention(cache.ref, Q.data_ptr(), ldq, _dtype_code(Q), pstarts, plens, ppages, ldp, n_seq, n, max_q, hq, pprefix,
+                                prefix_len, hd ** -0.5 if scale is None else scale, out.data_ptr(), ldo, plse, buf.data_ptr(), buf.numel(),
+                                _stream(stream)))
     return out
 
 

@@ -58,7 +58,7 @@ __device__ __forceinline__ int64_t first_entry(const AttendArgs& a, int s, int R
 }
 
 // What a segment costs beside its tiles, in tiles: its queries, the first tiles' way to LDS, its output.  Counted in the list, in front of them.
-constexpr int kSegmentCost = 2;
+constexpr int kSegmentCost = 4;
 
 // The list of row tiles.  One workgroup of 1024.
 template <int R>
@@ -125,7 +125,9 @@ template <int KV, int HD, int WAVES>
 struct TileLoader {
   using Shared = TileShared<KV, HD, WAVES>;
   static constexpr int THREADS = 64 * WAVES, kHalf = kv_half_bytes<KV, HD>(), ROWB = HD * 2;
-  static constexpr int KMASK = HD >= 128 ? 15 : 7;
+  // The chunks of key row `row` are exchanged with this: eight lanes that read together, rows 0 .. 3 and 8 .. 11 or the like, take eight
+  // different ones of the eight places that 32 banks have.  Linear: of rows without a common bit it is that of each, exclusive or.
+  __host__ __device__ static constexpr int exchange(int row) { return (row & 3) | (row & 8) >> 1 | (HD >= 128 ? (row & 4) << 1 : 0); }
   static constexpr int STEPS = Shared::kTile / 1024 / WAVES;                      // bf16: KiB of a wave, keys and values each
   // quantised: pieces of a thread
   static constexpr int KW = KV == kKvU4 ? HD / 32 : HD / 16;                      // dwords of a (token, quarter)
@@ -147,14 +149,14 @@ struct TileLoader {
   // bf16: where in a block lane and wave of the first of STEPS pieces of keys, of values, begin to read
   __device__ __forceinline__ static int key_source() {
     const int tid = thread(), byte = (tid >> 6) * (STEPS * 1024) + (tid & 63) * 16, row = byte / ROWB;
-    return row * ROWB + ((byte % ROWB / 16 ^ (row & KMASK)) << 4);
+    return row * ROWB + ((byte % ROWB / 16 ^ exchange(row)) << 4);
   }
   __device__ __forceinline__ static int value_source() {
     const int tid = thread(), byte = (tid >> 6) * (STEPS * 1024) + (tid & 63) * 16, row = byte / 128;
     return kHalf + row * 128 + ((byte % 128 / 16 ^ (row & 7)) << 4);
   }
   // what the exchange adds to the source of the i-th piece of keys: a KiB further on the row's number has other bits, without a carry
-  __device__ __forceinline__ static constexpr int key_turn(int i) { return (1024 / ROWB * i & KMASK) << 4; }
+  __device__ __forceinline__ static constexpr int key_turn(int i) { return exchange(1024 / ROWB * i) << 4; }
   // quantised: asks for keys and for values
   __device__ __forceinline__ void ask_keys(const char* block) {
     const int tid = thread();
@@ -188,7 +190,7 @@ struct TileLoader {
         bf16x8 out;
         if constexpr (KV == kKvU4) out = spread_nibbles(k[w]);
         else out = spread_bytes(k[2 * w], k[2 * w + 1]);
-        *reinterpret_cast<bf16x8*>(sh.keys[at] + token * ROWB + (((4 * w + g) ^ (token & KMASK)) << 4)) = out;
+        *reinterpret_cast<bf16x8*>(sh.keys[at] + token * ROWB + (((4 * w + g) ^ exchange(token)) << 4)) = out;
       }
     }
   }
@@ -410,7 +412,7 @@ __global__ __launch_bounds__(64 * WAVES, HD == 256 && WAVES == 4 ? 1 : 2) void a
     // each half tile: kept in registers, it would push others out to memory, and a wait for those is one for the copies under way
     auto key_place = [&] {
       const int l = Loader::thread() & 63, k = (l & 0x13) | (l & 4) << 1 | (l & 8) >> 1;
-      return k * Loader::ROWB + (((l >> 5) ^ (k & Loader::KMASK)) << 4);
+      return k * Loader::ROWB + (((l >> 5) ^ Loader::exchange(k)) << 4);
     };
     auto value_place = [&] {
       const int l = Loader::thread() & 63;

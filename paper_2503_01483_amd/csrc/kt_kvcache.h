@@ -48,15 +48,25 @@ struct AppendArgs {
   const float* rope;  // [n_pos][rot]: cosines, then sines
   int64_t n_pos;
   int n, hq, rot;
+  int chunks;  // workgroups of a token's queries and keys
   bool interleaved, hadamard;
 };
 
-// Value of lane `lane ^ O` (O < 8 LPR; rows of lanes lie next to each other).
+// Value of lane `lane ^ O`, on the vector ALU for distances up to 8 (a row of 16 lanes), where every lane is in use.
 template <int O>
-__device__ __forceinline__ float lane_xor(float x) { return __shfl_xor(x, O); }
+__device__ __forceinline__ float lane_xor(float x) {
+  const int v = __float_as_int(x);
+  if constexpr (O == 1) return __int_as_float(__builtin_amdgcn_mov_dpp(v, 0xb1, 0xf, 0xf, true));        // quad_perm 1 0 3 2
+  else if constexpr (O == 2) return __int_as_float(__builtin_amdgcn_mov_dpp(v, 0x4e, 0xf, 0xf, true));   // quad_perm 2 3 0 1
+  else if constexpr (O == 4)                                                                             // 7 - lane, then 3 - lane
+    return __int_as_float(__builtin_amdgcn_mov_dpp(__builtin_amdgcn_mov_dpp(v, 0x141, 0xf, 0xf, true), 0x1b, 0xf, 0xf, true));
+  else if constexpr (O == 8) return __int_as_float(__builtin_amdgcn_mov_dpp(v, 0x128, 0xf, 0xf, true));  // row_ror 8
+  else return __shfl_xor(x, O);
+}
 
-// Position rotation of the first `rot` of a row's features, 8 of which this lane holds (l-th lane of the row).
+// Position rotation of the first `rot` of a row's 8 LPR features, 8 of which this lane holds (l-th lane of the row).
 // fp32, one rounding an operation.
+template <int LPR>
 __device__ __forceinline__ void rotate_position(float (&y)[8], const float* row, int rot, bool interleaved, int l) {
 #pragma clang fp contract(off)
   const int half = rot / 2, lanes = rot / 16;  // lanes of each half
@@ -71,10 +81,15 @@ __device__ __forceinline__ void rotate_position(float (&y)[8], const float* row,
     return;
   }
   const bool second = l >= lanes;
-  const int other = (threadIdx.x & 63) + (l >= 2 * lanes ? 0 : second ? -lanes : lanes);
   float z[8];
+  if (rot == 8 * LPR) {
 #pragma unroll
-  for (int e = 0; e < 8; ++e) z[e] = __shfl(y[e], other);
+    for (int e = 0; e < 8; ++e) z[e] = lane_xor<LPR / 2>(y[e]);
+  } else {
+    const int other = (threadIdx.x & 63) + (l >= 2 * lanes ? 0 : second ? -lanes : lanes);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) z[e] = __shfl(y[e], other);
+  }
   if (l >= 2 * lanes) return;
   const int at = 8 * (second ? l - lanes : l);
   float c[8], s[8];
@@ -88,6 +103,15 @@ __device__ __forceinline__ void rotate_position(float (&y)[8], const float* row,
 }
 
 // H / sqrt(8 LPR) on the row, butterflies by distances 1, 2, 4, ...; fp32, one rounding an operation.
+template <int LPR, int S>
+__device__ __forceinline__ void butterfly(float (&y)[8], int l) {
+  if constexpr (S < LPR) {
+    const float sign = l & S ? -1.f : 1.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) y[e] = fmaf(y[e], sign, lane_xor<S>(y[e]));  // y + p or p - y: the product is exact
+    butterfly<LPR, 2 * S>(y, l);
+  }
+}
 template <int LPR>
 __device__ __forceinline__ void rotate_hadamard(float (&y)[8], int l) {
 #pragma clang fp contract(off)
@@ -100,94 +124,92 @@ __device__ __forceinline__ void rotate_hadamard(float (&y)[8], int l) {
         y[e] = a + b;
         y[e + s] = a - b;
       }
-#pragma unroll
-  for (int s = 1; s < LPR; s *= 2)
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const float p = __shfl_xor(y[e], s);
-      y[e] = l & s ? p - y[e] : y[e] + p;
-    }
+  butterfly<LPR, 1>(y, l);
   constexpr float norm = LPR == 8 ? 0.125f : LPR == 16 ? 0.08838834764831845f : 0.0625f;
 #pragma unroll
   for (int e = 0; e < 8; ++e) y[e] *= norm;
 }
 
+template <int LPR, int S, class F>
+__device__ __forceinline__ float row_reduce(float v, F f) {
+  if constexpr (S < LPR) return row_reduce<LPR, 2 * S>(f(v, lane_xor<S>(v)), f);
+  else return v;
+}
+
 // Codes and {step, minimum} of the row (LPR lanes of 8 values); a row with a value that is not finite gets NaN for both and codes 0.
+// A code is the quotient ((y - min) top) / width, rounded to fp32, rounded half to even.  The quotient times a reciprocal is within 2^-14 of it, so that
+// only one that near to the middle of two codes (of 512 values about one in ten waves has one; ties of bf16 inputs are common) is divided.
 template <int LPR>
 __device__ __forceinline__ void quantise_row(const float (&y)[8], float top, uint32_t (&code)[8], float& step, float& low) {
 #pragma clang fp contract(off)
   float lo = y[0], hi = y[0], bad = 0.f;
 #pragma unroll
   for (int e = 0; e < 8; ++e) lo = fminf(lo, y[e]), hi = fmaxf(hi, y[e]), bad += y[e] * 0.f;
-#pragma unroll
-  for (int s = 1; s < LPR; s *= 2) {
-    lo = fminf(lo, __shfl_xor(lo, s));
-    hi = fmaxf(hi, __shfl_xor(hi, s));
-    bad += __shfl_xor(bad, s);
-  }
+  lo = row_reduce<LPR, 1>(lo, [](float a, float b) { return fminf(a, b); });
+  hi = row_reduce<LPR, 1>(hi, [](float a, float b) { return fmaxf(a, b); });
+  const int shift = threadIdx.x & 63 & ~(LPR - 1);
+  const bool all_finite = (__ballot(!(bad == 0.f)) >> shift & ((1ull << LPR) - 1)) == 0ull;
   const float width = hi - lo;
   step = width / top;
   low = lo;
   if (step < kTiny) step = 0.f;
-  const bool finite = bad == 0.f && width * top <= kHuge;
+  const bool finite = all_finite && width * top <= kHuge, some = finite && step > 0.f;
+  const float inv = 1.f / width;  // (finite where step > 0)
 #pragma unroll
-  for (int e = 0; e < 8; ++e) code[e] = finite && step > 0.f ? (uint32_t)rintf(((y[e] - lo) * top) / width) : 0u;
+  for (int e = 0; e < 8; ++e) {
+    const float num = (y[e] - lo) * top;
+    float q = num * inv, n = rintf(q);
+    if (__any(some && fabsf(q - n) > 0.4999f)) n = rintf(num / width);
+    code[e] = some ? (uint32_t)n : 0u;
+  }
   if (!finite) step = low = __builtin_nanf("");
 }
 
-// One row of queries, keys or values by LPR = HD / 8 lanes of 8 values each: rotated, then to q_out or into its page.
+// Where token `slot` of a head lies: its block and number in it; null if the cache has no such slot.
+template <int KV, int HD>
+__device__ __forceinline__ char* place_of(const KvCache& c, int64_t slot, int head, int& tok) {
+  const int64_t page = slot >> c.log2_page;
+  if (slot < 0 || page >= c.n_pages) return nullptr;
+  const int in_page = (int)(slot & ((1ll << c.log2_page) - 1));
+  tok = in_page & 63;
+  return c.data + kv_block_offset<KV, HD>(c, page, head, in_page >> 6);
+}
+
+// HD / 8 lanes a row of 8 values each.  The first n * chunks workgroups take the queries and keys of a token: rotated, then to q_out or into
+// their pages.  The others take the values of one head and of as many tokens as the workgroup has rows: these cross over to rows by feature in LDS,
+// so that the bytes of neighbouring slots are written together.
+// Bound by HBM for prompts; 8192 tokens of 32 + 2 x 8 heads of 128, 4 bits: see the figures in front of kt_kv_append's launch.
 template <typename T, int KV, int HD>
 __global__ __launch_bounds__(256) void kv_append_kernel(AppendArgs a) {
   constexpr int LPR = HD / 8, ROWS = 256 / LPR, HALF = kv_half_bytes<KV, HD>();
-  const int l = threadIdx.x % LPR, hkv = a.cache.n_heads, rows = a.hq + 2 * hkv;
-  const int64_t index = (int64_t)blockIdx.x * ROWS + threadIdx.x / LPR;
-  const int64_t token = index / rows;
-  const int r = (int)(index - token * rows);
-  // a token without a slot or position of its own is passed over: its lanes stay for the exchanges and write nothing
-  const int64_t slot = token < a.n ? a.slots[token] : -1;
-  const int pos = a.rope && token < a.n ? a.positions[token] : 0;
-  const bool live = slot >= 0 && slot >> a.cache.log2_page < a.cache.n_pages && (!a.rope || (pos >= 0 && pos < a.n_pos));
-  const bool is_q = r < a.hq, is_k = !is_q && r < a.hq + hkv;
-  const int head = is_q ? r : is_k ? r - a.hq : r - a.hq - hkv;
-  const T* from = static_cast<const T*>(is_q ? a.q : is_k ? a.k : a.v);
+  constexpr float top = KV == kKvU8 ? 255.f : 15.f;
+  const int l = threadIdx.x % LPR, in_wg = threadIdx.x / LPR, w = l >> 2, g = l & 3, hkv = a.cache.n_heads;
+  const int64_t rotated = (int64_t)a.n * a.chunks;
   float y[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-  if (live) load8(from + token * (is_q ? a.ldq : is_k ? a.ldk : a.ldv) + head * HD + 8 * l, y);
-  {
-    float z[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) z[e] = y[e];
-    if (a.rope) rotate_position(z, a.rope + (live ? pos : 0) * (int64_t)a.rot, a.rot, a.interleaved, l);
-    if (a.hadamard) rotate_hadamard<LPR>(z, l);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) y[e] = is_q || is_k ? z[e] : y[e];
-  }
-  uint32_t code[8];
-  float step = 0.f, low = 0.f;
-  if constexpr (KV != kKvBf16) quantise_row<LPR>(y, KV == kKvU8 ? 255.f : 15.f, code, step, low);
-  [[maybe_unused]] uint32_t other[8];
-  if constexpr (KV == kKvU4) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) other[e] = (uint32_t)__shfl_xor((int)code[e], 2);
-  }
-  if (!live) return;
-  if (is_q) {
-    store8(static_cast<T*>(a.q_out) + token * a.ldqo + head * HD + 8 * l, y);
-    return;
-  }
-  const int64_t page = slot >> a.cache.log2_page;
-  const int in_page = (int)(slot & ((1ll << a.cache.log2_page) - 1)), tok = in_page & 63;
-  char* block = a.cache.data + kv_block_offset<KV, HD>(a.cache, page, head, in_page >> 6);
-  const int w = l >> 2, g = l & 3;
-  if constexpr (KV == kKvBf16) {
-    if (is_k) {
+  int tok = 0;
+  if (blockIdx.x < rotated) {
+    const int token = blockIdx.x / (unsigned)a.chunks, r = (blockIdx.x - token * a.chunks) * ROWS + in_wg;
+    // a token without a slot or position of its own is passed over
+    const int64_t slot = a.slots[token];
+    const int pos = a.rope ? a.positions[token] : 0;
+    if (!place_of<KV, HD>(a.cache, slot, 0, tok) || (a.rope && (pos < 0 || pos >= a.n_pos))) return;
+    const bool is_q = r < a.hq, live = r < a.hq + hkv;  // (lanes behind the last row stay for the exchanges and write nothing)
+    const int head = is_q ? r : r - a.hq;
+    if (live) load8(static_cast<const T*>(is_q ? a.q : a.k) + token * (is_q ? a.ldq : a.ldk) + head * HD + 8 * l, y);
+    if (a.rope) rotate_position<LPR>(y, a.rope + pos * (int64_t)a.rot, a.rot, a.interleaved, l);
+    if (a.hadamard) rotate_hadamard<LPR>(y, l);
+    [[maybe_unused]] uint32_t code[8];
+    [[maybe_unused]] float step, low;
+    if constexpr (KV != kKvBf16) quantise_row<LPR>(y, top, code, step, low);
+    if (!live) return;
+    if (is_q) {
+      store8(static_cast<T*>(a.q_out) + token * a.ldqo + head * HD + 8 * l, y);
+      return;
+    }
+    char* block = place_of<KV, HD>(a.cache, slot, head, tok);
+    if constexpr (KV == kKvBf16) {
       store8(reinterpret_cast<bf16*>(block) + tok * HD + 8 * l, y);
     } else {
-      bf16* v = reinterpret_cast<bf16*>(block + HALF) + tok;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[(8 * l + e) * kBlockTokens] = (bf16)y[e];
-    }
-  } else {
-    if (is_k) {
       if constexpr (KV == kKvU8) {
         const u32x2 t = {code[0] | code[1] << 8 | code[2] << 16 | code[3] << 24, code[4] | code[5] << 8 | code[6] << 16 | code[7] << 24};
         *reinterpret_cast<u32x2*>(block + tok * HD + g * (HD / 4) + 8 * w) = t;
@@ -195,17 +217,65 @@ __global__ __launch_bounds__(256) void kv_append_kernel(AppendArgs a) {
         const uint32_t t = code[0] | code[2] << 4 | code[4] << 8 | code[6] << 12 | code[1] << 16 | code[3] << 20 | code[5] << 24 | code[7] << 28;
         *reinterpret_cast<uint32_t*>(block + tok * (HD / 2) + (g * (HD / 32) + w) * 4) = t;
       }
-    } else {
-      uint8_t* v = reinterpret_cast<uint8_t*>(block + HALF) + tok;
-      if constexpr (KV == kKvU8) {
+      if (l == 0) reinterpret_cast<float2*>(block + 2 * HALF)[tok] = make_float2(step, low);
+    }
+    return;
+  }
+  // ---- values
+  constexpr int BYTES = KV == kKvBf16 ? 2 : 1, FEATURES = KV == kKvU4 ? HD / 2 : HD;  // of a token's entry in a row, rows
+  __shared__ __align__(16) char turned[FEATURES][ROWS * BYTES + (ROWS * BYTES < 16 ? 0 : 4)];
+  __shared__ int64_t slots[ROWS];
+  const int64_t index = blockIdx.x - rotated;
+  const int group = (int)(index / hkv), head = (int)(index - (int64_t)group * hkv);
+  const int64_t token = (int64_t)group * ROWS + in_wg;
+  const int64_t slot = token < a.n ? a.slots[token] : -1;
+  const int pos = a.rope && token < a.n ? a.positions[token] : 0;
+  char* block = place_of<KV, HD>(a.cache, slot, head, tok);
+  const bool live = block && (!a.rope || (pos >= 0 && pos < a.n_pos));
+  if (l == 0) slots[in_wg] = live ? slot : -1;
+  if (live) load8(static_cast<const T*>(a.v) + token * a.ldv + head * HD + 8 * l, y);
+  if constexpr (KV == kKvBf16) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[(8 * l + e) * kBlockTokens] = (uint8_t)code[e];
-      } else if (g < 2) {  // (the lanes of the first 16 of 32 features write both nibbles)
+    for (int e = 0; e < 8; ++e) reinterpret_cast<bf16*>(turned[8 * l + e])[in_wg] = (bf16)y[e];
+  } else {
+    uint32_t code[8];
+    float step, low;
+    quantise_row<LPR>(y, top, code, step, low);
+    if constexpr (KV == kKvU8) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[(16 * w + 8 * g + e) * kBlockTokens] = (uint8_t)(code[e] | other[e] << 4);
+      for (int e = 0; e < 8; ++e) turned[8 * l + e][in_wg] = (char)code[e];
+    } else {  // (the lanes of the first 16 of 32 features write both nibbles)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const uint32_t other = (uint32_t)__float_as_int(lane_xor<2>(__int_as_float((int)code[e])));
+        if (g < 2) turned[16 * w + 8 * g + e][in_wg] = (char)(code[e] | other << 4);
       }
     }
-    if (l == 0) reinterpret_cast<float2*>(block + 2 * HALF)[(is_k ? 0 : kBlockTokens) + tok] = make_float2(step, low);
+    if (live && l == 0) reinterpret_cast<float2*>(block + 2 * HALF)[kBlockTokens + tok] = make_float2(step, low);
+  }
+  __syncthreads();
+  // eight entries of a feature at a time: together where their slots are neighbours in a block and the first is a multiple of eight
+  constexpr int RUN = 8;
+  static_assert(ROWS % RUN == 0);
+  for (int i = threadIdx.x; i < FEATURES * (ROWS / RUN); i += 256) {
+    const int f = i / (ROWS / RUN), first = i % (ROWS / RUN) * RUN;
+    bool run = slots[first] >= 0 && (slots[first] & (RUN - 1)) == 0;
+#pragma unroll
+    for (int k = 1; k < RUN; ++k) run = run && slots[first + k] == slots[first] + k;
+    if (run) {
+      char* to = place_of<KV, HD>(a.cache, slots[first], head, tok) + HALF + (f * kBlockTokens + tok) * BYTES;
+#pragma unroll
+      for (int k = 0; k < 2 * BYTES; ++k) reinterpret_cast<uint32_t*>(to)[k] = *reinterpret_cast<const uint32_t*>(&turned[f][first * BYTES + 4 * k]);
+    } else {
+#pragma unroll
+      for (int k = 0; k < RUN; ++k) {
+        char* to = place_of<KV, HD>(a.cache, slots[first + k], head, tok);
+        if (!to) continue;
+        to += HALF + (f * kBlockTokens + tok) * BYTES;
+        if constexpr (BYTES == 2) *reinterpret_cast<uint16_t*>(to) = *reinterpret_cast<const uint16_t*>(&turned[f][(first + k) * 2]);
+        else *to = turned[f][first + k];
+      }
+    }
   }
 }
 
@@ -214,60 +284,85 @@ struct GatherArgs {
   const int64_t* slots;
   void *k, *v;
   int64_t ldk, ldv;
-  int n;
+  int n, chunks;  // workgroups of a token's keys (0: no keys)
 };
 
-// Keys and values of single slots as values; a row of one head by HD / 8 lanes.
+// Keys and values of single slots as values: the same workgroups the other way round.
 template <typename T, int KV, int HD>
 __global__ __launch_bounds__(256) void kv_gather_kernel(GatherArgs a) {
 #pragma clang fp contract(off)
   constexpr int LPR = HD / 8, ROWS = 256 / LPR, HALF = kv_half_bytes<KV, HD>();
-  const int l = threadIdx.x % LPR, hkv = a.cache.n_heads;
-  const int64_t index = (int64_t)blockIdx.x * ROWS + threadIdx.x / LPR;
-  const int64_t token = index / (2 * hkv);
-  if (token >= a.n) return;
-  const int r = (int)(index - token * (2 * hkv));
-  const bool is_k = r < hkv;
-  const int head = is_k ? r : r - hkv;
-  const int64_t slot = a.slots[token], page = slot >> a.cache.log2_page;
-  if (slot < 0 || page >= a.cache.n_pages) return;
-  if (is_k ? !a.k : !a.v) return;
-  const int in_page = (int)(slot & ((1ll << a.cache.log2_page) - 1)), tok = in_page & 63;
-  const char* block = a.cache.data + kv_block_offset<KV, HD>(a.cache, page, head, in_page >> 6);
-  const int w = l >> 2, g = l & 3;
+  const int l = threadIdx.x % LPR, in_wg = threadIdx.x / LPR, w = l >> 2, g = l & 3, hkv = a.cache.n_heads;
+  const int64_t with_keys = (int64_t)a.n * a.chunks;
   float y[8];
-  if constexpr (KV == kKvBf16) {
-    if (is_k) {
+  int tok = 0;
+  if (blockIdx.x < with_keys) {
+    const int token = blockIdx.x / (unsigned)a.chunks, head = (blockIdx.x - token * a.chunks) * ROWS + in_wg;
+    const char* block = head < hkv ? place_of<KV, HD>(a.cache, a.slots[token], head, tok) : nullptr;
+    if (!block) return;
+    if constexpr (KV == kKvBf16) {
       load8(reinterpret_cast<const bf16*>(block) + tok * HD + 8 * l, y);
     } else {
-      const bf16* v = reinterpret_cast<const bf16*>(block + HALF) + tok;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) y[e] = (float)v[(8 * l + e) * kBlockTokens];
-    }
-  } else {
-    uint32_t code[8];
-    if (is_k) {
+      const float2 p = reinterpret_cast<const float2*>(block + 2 * HALF)[tok];
       if constexpr (KV == kKvU8) {
         const u32x2 t = *reinterpret_cast<const u32x2*>(block + tok * HD + g * (HD / 4) + 8 * w);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) code[e] = t[e / 4] >> (8 * (e & 3)) & 0xffu;
+        for (int e = 0; e < 8; ++e) y[e] = (float)(t[e / 4] >> (8 * (e & 3)) & 0xffu) * p.x + p.y;
       } else {
         const uint32_t t = *reinterpret_cast<const uint32_t*>(block + tok * (HD / 2) + (g * (HD / 32) + w) * 4);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) code[e] = t >> (4 * (e / 2 + 4 * (e & 1))) & 15u;
+        for (int e = 0; e < 8; ++e) y[e] = (float)(t >> (4 * (e / 2 + 4 * (e & 1))) & 15u) * p.x + p.y;
       }
-    } else {
-      const uint8_t* v = reinterpret_cast<const uint8_t*>(block + HALF) + tok;
-#pragma unroll
-      for (int e = 0; e < 8; ++e)
-        code[e] = KV == kKvU8 ? v[(8 * l + e) * kBlockTokens] : v[(16 * w + 8 * (g & 1) + e) * kBlockTokens] >> (g & 2 ? 4 : 0) & 15;
     }
-    const float2 p = reinterpret_cast<const float2*>(block + 2 * HALF)[(is_k ? 0 : kBlockTokens) + tok];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) y[e] = (float)code[e] * p.x + p.y;
+    store8(static_cast<T*>(a.k) + token * a.ldk + head * HD + 8 * l, y);
+    return;
   }
-  if (is_k) store8(static_cast<T*>(a.k) + token * a.ldk + head * HD + 8 * l, y);
-  else store8(static_cast<T*>(a.v) + token * a.ldv + head * HD + 8 * l, y);
+  // ---- values
+  constexpr int BYTES = KV == kKvBf16 ? 2 : 1, FEATURES = KV == kKvU4 ? HD / 2 : HD, RUN = 8;
+  __shared__ __align__(16) char turned[FEATURES][ROWS * BYTES + (ROWS * BYTES < 16 ? 0 : 4)];
+  __shared__ int64_t slots[ROWS];
+  const int64_t index = blockIdx.x - with_keys;
+  const int group = (int)(index / hkv), head = (int)(index - (int64_t)group * hkv);
+  const int64_t token = (int64_t)group * ROWS + in_wg;
+  if (l == 0) slots[in_wg] = token < a.n ? a.slots[token] : -1;
+  __syncthreads();
+  for (int i = threadIdx.x; i < FEATURES * (ROWS / RUN); i += 256) {
+    const int f = i / (ROWS / RUN), first = i % (ROWS / RUN) * RUN;
+    bool run = (slots[first] & (RUN - 1)) == 0;
+#pragma unroll
+    for (int k = 1; k < RUN; ++k) run = run && slots[first + k] == slots[first] + k;
+    if (run) {
+      const char* from = place_of<KV, HD>(a.cache, slots[first], head, tok);
+      if (!from) continue;
+      from += HALF + (f * kBlockTokens + tok) * BYTES;
+#pragma unroll
+      for (int k = 0; k < 2 * BYTES; ++k) *reinterpret_cast<uint32_t*>(&turned[f][first * BYTES + 4 * k]) = reinterpret_cast<const uint32_t*>(from)[k];
+    } else {
+#pragma unroll
+      for (int k = 0; k < RUN; ++k) {
+        const char* from = place_of<KV, HD>(a.cache, slots[first + k], head, tok);
+        if (!from) continue;
+        from += HALF + (f * kBlockTokens + tok) * BYTES;
+        if constexpr (BYTES == 2) *reinterpret_cast<uint16_t*>(&turned[f][(first + k) * 2]) = *reinterpret_cast<const uint16_t*>(from);
+        else turned[f][first + k] = *from;
+      }
+    }
+  }
+  __syncthreads();
+  const char* block = place_of<KV, HD>(a.cache, slots[in_wg], head, tok);
+  if (!block) return;
+  if constexpr (KV == kKvBf16) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) y[e] = (float)reinterpret_cast<const bf16*>(turned[8 * l + e])[in_wg];
+  } else {
+    const float2 p = reinterpret_cast<const float2*>(block + 2 * HALF)[kBlockTokens + tok];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const uint32_t c = (uint8_t)turned[KV == kKvU8 ? 8 * l + e : 16 * w + 8 * (g & 1) + e][in_wg];
+      y[e] = (float)(KV == kKvU8 ? c : c >> (g & 2 ? 4 : 0) & 15u) * p.x + p.y;
+    }
+  }
+  store8(static_cast<T*>(a.v) + token * a.ldv + head * HD + 8 * l, y);
 }
 
 }  // namespace kt

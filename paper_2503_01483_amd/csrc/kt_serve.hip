@@ -205,10 +205,11 @@ kt_status kt_kv_append(const kt_kv_cache* cache, const void* Q, int64_t ldq, con
     if (misaligned(rope, 16)) return fail(KT_ERR_BAD_SHAPE, "rope must be 16-byte aligned");
   }
   if (misaligned(slots, 8) || misaligned(positions, 4)) return fail(KT_ERR_BAD_SHAPE, "slots and positions must be aligned to their type");
+  const int64_t rows = 256 / (hd / 8), chunks = ceil_div(n_q_heads + cache->n_heads, rows);
   AppendArgs a{device_cache(cache), Q, K, V, Q_out, ldq, ldk, ldv, ldqo, slots, positions, rope, n_pos, (int)n, (int)n_q_heads,
-               rope ? (int)rot_dim : 0, interleaved != 0, hadamard != 0};
+               rope ? (int)rot_dim : 0, (int)chunks, interleaved != 0, hadamard != 0};
   hipStream_t st = static_cast<hipStream_t>(stream);
-  const int64_t wgs = ceil_div(n * (n_q_heads + 2 * cache->n_heads), 256 / (hd / 8));
+  const int64_t wgs = n * chunks + ceil_div(n, rows) * cache->n_heads;
   if (wgs > INT32_MAX) return fail(KT_ERR_NOT_SUPPORTED, "too many rows for one call");
   with_cache(cache, [&](auto kv, auto h) {
     constexpr int KV = decltype(kv)::value, HD = decltype(h)::value;
@@ -229,9 +230,10 @@ kt_status kt_kv_gather(const kt_kv_cache* cache, const int64_t* slots, int64_t n
   if ((K && !rows_ok(K, ldk, cache->n_heads * hd, dtype)) || (V && !rows_ok(V, ldv, cache->n_heads * hd, dtype)))
     return fail(KT_ERR_BAD_SHAPE, "leading dimensions must be in [heads * head_dim, 2^24] and keep rows 16-byte aligned");
   if (misaligned(slots, 8)) return fail(KT_ERR_BAD_SHAPE, "slots must be aligned to their type");
-  GatherArgs a{device_cache(cache), slots, K, V, ldk, ldv, (int)n};
+  const int64_t rows = 256 / (hd / 8), chunks = K ? ceil_div(cache->n_heads, rows) : 0;
+  GatherArgs a{device_cache(cache), slots, K, V, ldk, ldv, (int)n, (int)chunks};
   hipStream_t st = static_cast<hipStream_t>(stream);
-  const int64_t wgs = ceil_div(n * 2 * cache->n_heads, 256 / (hd / 8));
+  const int64_t wgs = n * chunks + (V ? ceil_div(n, rows) * cache->n_heads : 0);
   if (wgs > INT32_MAX) return fail(KT_ERR_NOT_SUPPORTED, "too many rows for one call");
   with_cache(cache, [&](auto kv, auto h) {
     constexpr int KV = decltype(kv)::value, HD = decltype(h)::value;
