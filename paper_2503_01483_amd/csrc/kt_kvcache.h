@@ -189,18 +189,21 @@ __global__ __launch_bounds__(256) void kv_append_kernel(AppendArgs a) {
   int tok = 0;
   if (blockIdx.x < rotated) {
     const int token = blockIdx.x / (unsigned)a.chunks, r = (blockIdx.x - token * a.chunks) * ROWS + in_wg;
-    // a token without a slot or position of its own is passed over
-    const int64_t slot = a.slots[token];
-    const int pos = a.rope ? a.positions[token] : 0;
-    if (!place_of<KV, HD>(a.cache, slot, 0, tok) || (a.rope && (pos < 0 || pos >= a.n_pos))) return;
     const bool is_q = r < a.hq, live = r < a.hq + hkv;  // (lanes behind the last row stay for the exchanges and write nothing)
     const int head = is_q ? r : r - a.hq;
+    // (asked for together with slot and position, whatever these say)
     if (live) load8(static_cast<const T*>(is_q ? a.q : a.k) + token * (is_q ? a.ldq : a.ldk) + head * HD + 8 * l, y);
+    const int64_t slot = a.slots[token];
+    const int pos = a.rope ? a.positions[token] : 0;
+    // a token without a slot or position of its own is passed over
+    if (!place_of<KV, HD>(a.cache, slot, 0, tok) || (a.rope && (pos < 0 || pos >= a.n_pos))) return;
     if (a.rope) rotate_position<LPR>(y, a.rope + pos * (int64_t)a.rot, a.rot, a.interleaved, l);
     if (a.hadamard) rotate_hadamard<LPR>(y, l);
     [[maybe_unused]] uint32_t code[8];
     [[maybe_unused]] float step, low;
-    if constexpr (KV != kKvBf16) quantise_row<LPR>(y, top, code, step, low);
+    if constexpr (KV != kKvBf16) {
+      if (r - in_wg + ROWS > a.hq) quantise_row<LPR>(y, top, code, step, low);  // (a workgroup with keys)
+    }
     if (!live) return;
     if (is_q) {
       store8(static_cast<T*>(a.q_out) + token * a.ldqo + head * HD + 8 * l, y);
@@ -228,12 +231,12 @@ __global__ __launch_bounds__(256) void kv_append_kernel(AppendArgs a) {
   const int64_t index = blockIdx.x - rotated;
   const int group = (int)(index / hkv), head = (int)(index - (int64_t)group * hkv);
   const int64_t token = (int64_t)group * ROWS + in_wg;
+  if (token < a.n) load8(static_cast<const T*>(a.v) + token * a.ldv + head * HD + 8 * l, y);
   const int64_t slot = token < a.n ? a.slots[token] : -1;
   const int pos = a.rope && token < a.n ? a.positions[token] : 0;
   char* block = place_of<KV, HD>(a.cache, slot, head, tok);
   const bool live = block && (!a.rope || (pos >= 0 && pos < a.n_pos));
   if (l == 0) slots[in_wg] = live ? slot : -1;
-  if (live) load8(static_cast<const T*>(a.v) + token * a.ldv + head * HD + 8 * l, y);
   if constexpr (KV == kKvBf16) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) reinterpret_cast<bf16*>(turned[8 * l + e])[in_wg] = (bf16)y[e];
