@@ -204,20 +204,25 @@ struct Tile64 {
   }
 };
 
-// What has to be added to O where a value that not all rows of a tile see is not finite: products take such values as 0.  Feature `at` of
-// values `v` [feature][64].
-__device__ __forceinline__ float unfinite(const bf16* v, int at, int seen) {
-  float sum = 0.f;
-  for (int j = 0; j < seen; ++j) {
-    const float x = (float)v[at * kBlockTokens + j];
-    if (!(fabsf(x) <= kHuge)) sum += x;
-  }
-  return sum;
+// Takes values that are not finite, and those of tokens `there` on, out of a dword of the values of tokens `at` and at + 1 (0 NaN = NaN); the former
+// are noted in `which`.
+__device__ __forceinline__ uint32_t only_finite(uint32_t d, int at, int there, unsigned long long& which) {
+  d = at >= there ? 0u : at + 1 >= there ? d & 0xffffu : d;
+  if ((d & 0x7f80u) == 0x7f80u) which |= 1ull << at, d &= 0xffff0000u;
+  if ((d & 0x7f800000u) == 0x7f800000u) which |= 2ull << at, d &= 0xffffu;
+  return d;
+}
+// The tokens that any lane has noted; uniform.
+__device__ __forceinline__ unsigned long long any_lane(unsigned long long which) {
+  unsigned long long all = 0ull;
+  if (__any(which != 0ull))
+    for (int j = 0; j < 64; ++j) all |= (unsigned long long)(__any(which >> j & 1ull) ? 1 : 0) << j;
+  return all;
 }
 
 // The list's order: sequences, in each its heads, in each its tiles.
 template <int KV, int HD>
-__global__ __launch_bounds__(256) void attend_rows_kernel(AttendArgs a) {
+__global__ __launch_bounds__(256, HD == 256 ? 1 : 2) void attend_rows_kernel(AttendArgs a) {
   extern __shared__ int cum[];
   __shared__ float4 params[4][64];
   constexpr int TD = HD / 16;
@@ -348,26 +353,24 @@ __global__ __launch_bounds__(256) void attend_rows_kernel(AttendArgs a) {
       l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
       if constexpr (KV == kKvBf16) {
         if (masked) {  // what a row does not see may be anything, and 0 NaN = NaN
-          const int there = q.len - tile * 64;
-          bool odd = false;
+          unsigned long long odd = 0ull;
 #pragma unroll
           for (int i = 0; i < TD; ++i)
 #pragma unroll
             for (int j = 0; j < 2; ++j)
 #pragma unroll
-              for (int w = 0; w < 4; ++w) {
-                const int at = 32 * j + 8 * g + 2 * w;
-                uint32_t& d = t64.v[i][4 * j + w];
-                d = at >= there ? 0u : at + 1 >= there ? d & 0xffffu : d;
-                if ((d & 0x7f80u) == 0x7f80u) odd = true, d &= 0xffff0000u;
-                if ((d & 0x7f800000u) == 0x7f800000u) odd = true, d &= 0xffffu;
-              }
-          if (__any(odd)) {
-            const bf16* v = reinterpret_cast<const bf16*>(block + kv_half_bytes<KV, HD>());
+              for (int w = 0; w < 4; ++w) t64.v[i][4 * j + w] = only_finite(t64.v[i][4 * j + w], 32 * j + 8 * g + 2 * w, q.len - tile * 64, odd);
+          const bf16* v = reinterpret_cast<const bf16*>(block + kv_half_bytes<KV, HD>()) + 4 * g * kBlockTokens;
+#pragma unroll 1
+          for (odd = any_lane(odd); odd; odd &= odd - 1) {
+            const int j = __builtin_ctzll(odd);
 #pragma unroll
             for (int i = 0; i < TD; ++i)
 #pragma unroll
-              for (int e = 0; e < 4; ++e) o[i][e] += unfinite(v, 16 * i + 4 * g + e, seen);
+              for (int e = 0; e < 4; ++e) {
+                const float x = (float)v[(16 * i + e) * kBlockTokens + j];
+                if (j < seen && !(fabsf(x) <= kHuge)) o[i][e] += x;
+              }
           }
         }
 #pragma unroll

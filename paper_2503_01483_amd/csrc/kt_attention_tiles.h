@@ -472,20 +472,11 @@ __global__ __launch_bounds__(64 * WAVES, HD == 256 && WAVES == 4 ? 1 : 2) void a
         const int piece = (copy_at + 1024 * i >> 4) + lane, chunk = (piece & 7) ^ (piece >> 3 & 7);
         u32x4* from = reinterpret_cast<u32x4*>(sh.values[at]) + piece;
         u32x4 d = *from;
-        unsigned bits = 0u;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
-          const int k = 8 * chunk + 2 * w;
-          d[w] = k >= x.there ? 0u : k + 1 >= x.there ? d[w] & 0xffffu : d[w];
-          if ((d[w] & 0x7f80u) == 0x7f80u) bits |= 1u << (2 * w), d[w] &= 0xffff0000u;
-          if ((d[w] & 0x7f800000u) == 0x7f800000u) bits |= 2u << (2 * w), d[w] &= 0xffffu;
-        }
+        for (int w = 0; w < 4; ++w) d[w] = only_finite(d[w], 8 * chunk + 2 * w, x.there, which);
         *from = d;
-        which |= (unsigned long long)bits << (8 * chunk);
       }
-      unsigned long long all = 0ull;
-      if (__any(which != 0ull))
-        for (int j = 0; j < 64; ++j) all |= (unsigned long long)(__any(which >> j & 1ull) ? 1 : 0) << j;
+      const unsigned long long all = any_lane(which);
       if (lane == 0) sh.odd[at][wave] = all;
     };
 
