@@ -226,6 +226,7 @@ __global__ __launch_bounds__(256, HD == 256 ? 1 : 2) void attend_rows_kernel(Att
   extern __shared__ int cum[];
   __shared__ float4 params[4][64];
   constexpr int TD = HD / 16;
+  constexpr bool kEarly = KV == kKvU4 && HD <= 128;
   constexpr float kOffset = KV == kKvU4 ? 136.f : 128.f, kCentre = KV == kKvU4 ? 8.f : 128.f;
   constexpr float kNone = -__builtin_inff();
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, g = lane >> 4, heads = a.cache.n_heads;
@@ -274,14 +275,30 @@ __global__ __launch_bounds__(256, HD == 256 ? 1 : 2) void attend_rows_kernel(Att
     const int* pages = a.pages + s * a.ldp;
     Tile64<KV, HD> t64;
 
+    // Where a tile's block lies, and how many of its tokens there are: none of a page outside the cache (then some block's place is given).
+    auto place = [&](int tile, int& there) {
+      there = min(q.len - tile * 64, 64);
+      const int page = there > 0 ? pages[tile >> page_blocks] : -1;
+      if (page < 0 || page >= a.cache.n_pages) {
+        there = 0;
+        return (int64_t)0;
+      }
+      return kv_block_offset<KV, HD>(a.cache, page, head, tile & ((1 << page_blocks) - 1));
+    };
+    int there, there_next = 0;
+    int64_t block = place(first, there), block_next = 0;
+    if constexpr (kEarly) {
+      t64.load_keys(a.cache.data + block, lane);
+      t64.load_values(a.cache.data + block, lane);
+    }
     for (int tile = first; tile < last; ++tile) {
-      if (tile * 64 >= q.len) break;
-      const int64_t page = pages[tile >> page_blocks];
-      if (page < 0 || page >= a.cache.n_pages) continue;  // a page outside the cache holds nothing to see
-      const char* block = a.cache.data + kv_block_offset<KV, HD>(a.cache, page, head, tile & ((1 << page_blocks) - 1));
-      t64.load_keys(block, lane);
-      t64.load_values(block, lane);
-
+      // kEarly: the next tile's keys are asked for once these are used up, its values likewise: each has the other's time to arrive in
+      const bool more = tile + 1 < last;
+      if (more) block_next = place(tile + 1, there_next);
+      if constexpr (!kEarly) {
+        t64.load_keys(a.cache.data + block, lane);
+        t64.load_values(a.cache.data + block, lane);
+      }
       f32x4 x[4];
 #pragma unroll
       for (int t = 0; t < 4; ++t) {
@@ -309,8 +326,9 @@ __global__ __launch_bounds__(256, HD == 256 ? 1 : 2) void attend_rows_kernel(Att
           }
         __builtin_amdgcn_wave_barrier();
       }
-      const bool masked = tile * 64 + 64 > all_see;
-      const int seen = min(max(sees - tile * 64, 0), 64);
+      if (kEarly && more) t64.load_keys(a.cache.data + block_next, lane);
+      const bool masked = there < 64 || tile * 64 + 64 > all_see;
+      const int seen = min(max(sees - tile * 64, 0), there);
       if (masked) {
 #pragma unroll
         for (int t = 0; t < 4; ++t)
@@ -359,8 +377,8 @@ __global__ __launch_bounds__(256, HD == 256 ? 1 : 2) void attend_rows_kernel(Att
 #pragma unroll
             for (int j = 0; j < 2; ++j)
 #pragma unroll
-              for (int w = 0; w < 4; ++w) t64.v[i][4 * j + w] = only_finite(t64.v[i][4 * j + w], 32 * j + 8 * g + 2 * w, q.len - tile * 64, odd);
-          const bf16* v = reinterpret_cast<const bf16*>(block + kv_half_bytes<KV, HD>()) + 4 * g * kBlockTokens;
+              for (int w = 0; w < 4; ++w) t64.v[i][4 * j + w] = only_finite(t64.v[i][4 * j + w], 32 * j + 8 * g + 2 * w, there, odd);
+          const bf16* v = reinterpret_cast<const bf16*>(a.cache.data + block + kv_half_bytes<KV, HD>()) + 4 * g * kBlockTokens;
 #pragma unroll 1
           for (odd = any_lane(odd); odd; odd &= odd - 1) {
             const int j = __builtin_ctzll(odd);
@@ -399,6 +417,9 @@ __global__ __launch_bounds__(256, HD == 256 ? 1 : 2) void attend_rows_kernel(Att
           o[i] += t;
         }
       }
+      if (kEarly && more) t64.load_values(a.cache.data + block_next, lane);
+      block = block_next;
+      there = there_next;
     }
 
     l = quarters_sum(l);
