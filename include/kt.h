@@ -404,7 +404,7 @@ typedef struct {
   kt_kv_format format;
 } kt_kv_cache;
 
-/* Bytes of the cache's data (`data` is not looked at; 0 on bad sizes).  Host call. */
+/* Bytes of the cache's data (`data` is not looked at; 0 on bad sizes, those beyond 2^47 bytes among them).  Host call. */
 size_t kt_kv_cache_bytes(const kt_kv_cache* cache);
 
 /*
@@ -452,13 +452,18 @@ kt_status kt_kv_gather(const kt_kv_cache* cache, const int64_t* slots, int64_t n
  *     those of its queries (q_starts[i] .. q_starts[i + 1] - 1), which therefore are appended first.
  *  Q, O     [n_tokens][ldq], [n_tokens][ldo] bf16 (dtype must be KT_BF16), rows of Q 16-byte, of O 8-byte aligned.
  *  q_starts [n_seq + 1] int32, not descending, at most n_tokens; NULL: one query a sequence (n_tokens = n_seq, max_q = 1).  Rows in front
- *           of the first and behind the last sequence are left as they were.  max_q: a bound on the queries of a sequence.
+ *           of the first and behind the last sequence are left as they were.  max_q: a bound on the queries of a sequence (rows of a
+ *           longer one can be left as they were).
  *  lens     [n_seq] int32, at most ldp * page_size (what is above counts as that).   pages [n_seq][ldp] int32; entries behind a
  *           sequence's last page are not read, tokens of a page that is outside the cache count as not there.
  *  lse      [n_tokens][n_q_heads] fp32 or NULL: log sum_j exp(scale * q . k_j).
- * A query that sees nothing gives 0, and -inf in lse.  Scores, statistics and sums are fp32, the p_j are rounded to bf16 in front of
- * their product with the values.  All index arrays are on the device: the call can be captured and replayed with other
- * lengths and pages.  n_seq <= 4096, ldp * page_size and prefix_len <= 2^30, scale > 0.
+ * A query that sees nothing (or whose scores are all -inf) gives 0, and -inf in lse.  What a query does not see has no effect on it,
+ * whatever it is (bytes that no token was written to, infinities, NaN); a NaN that it sees makes its output NaN.  Scores, statistics
+ * and sums are fp32; in front of their product with the values the p_j are rounded to bf16 (KT_KV_BF16), p_j times the value's step to
+ * 16 bits (KT_KV_U8 and KT_KV_U4 with max_q * n_q_heads / n_heads <= 16), or p_j and the values to 11 bits of the largest of 64 (other
+ * calls).  The order of the sums depends on the call's sizes and lengths; the same call gives the same bits.  All index arrays are on
+ * the device: the call can be captured and replayed with other lengths and pages.  n_seq <= 4096, ldp * page_size and prefix_len <=
+ * 2^30, scale > 0.
  * Workspace: kt_paged_attention_bytes(n_tokens, n_q_heads, head_dim, prefix_len).
  */
 kt_status kt_paged_attention(const kt_kv_cache* cache, const void* Q, int64_t ldq, kt_dtype dtype, const int32_t* q_starts,

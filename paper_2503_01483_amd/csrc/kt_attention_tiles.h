@@ -45,13 +45,6 @@ __device__ __forceinline__ void to_lds_16(uint32_t voffset, const char* base, un
 __device__ __forceinline__ f32x16 mfma32(bf16x8 a, bf16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
 __device__ __forceinline__ f32x16 mfma32(f16x8 a, f16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
 
-template <class T>
-__device__ __forceinline__ const T* uniform_ptr(const T* p) {
-  const uint64_t v = reinterpret_cast<uint64_t>(p);
-  return reinterpret_cast<const T*>((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32 |
-                                    (uint32_t)__builtin_amdgcn_readfirstlane((int)v));
-}
-
 // Row tiles of R rows get numbers floor(first query * group / R) + s + 0, 1, ... (s their sequence): different for every sequence's.
 __device__ __forceinline__ int64_t first_entry(const AttendArgs& a, int s, int R) {
   return (int64_t)min(max(a.q_starts ? a.q_starts[s] : s, 0), a.n_tokens) * a.group / R + s;
@@ -469,7 +462,7 @@ __global__ __launch_bounds__(64 * WAVES, HD == 256 && WAVES == 4 ? 1 : 2) void a
       unsigned long long which = 0ull;
 #pragma unroll
       for (int i = 0; i < Loader::STEPS; ++i) {
-        const int piece = (copy_at + 1024 * i >> 4) + lane, chunk = (piece & 7) ^ (piece >> 3 & 7);
+        const int piece = (copy_at + 1024 * i) / 16 + lane, chunk = (piece & 7) ^ (piece >> 3 & 7);
         u32x4* from = reinterpret_cast<u32x4*>(sh.values[at]) + piece;
         u32x4 d = *from;
 #pragma unroll
