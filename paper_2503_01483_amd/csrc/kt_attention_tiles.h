@@ -12,7 +12,8 @@
 // in fp32 as in kt_attention.h; the values are expanded on the way, in fp16: a row s c + b is scaled by a power of two per
 // tile, found from the rows' {s, b}, so that its largest value is just below one, and rounded to 11 bits (2^-11 of it or less; bf16 would have 8, little
 // more than the codes of 8 bits).  The exponent is carried along with O like the running maximum.  The maximum is raised only
-// once a score passes it by 2^8 (p stays below 256 in either type).
+// once a score passes it by 2^8 (p stays below 256 in either type).  In fp16 p goes in times 2^7: what it cuts off where p is small then is
+// 2^-31 of the largest p at most, and a million tokens of it do not show in a result.
 //
 // All key tiles of all row tiles form one list, heads outermost; each workgroup takes an equal piece, neighbouring pieces on one XCD, whose
 // L2 then holds the keys of few heads.  Segments that are cut are joined by a second launch.
@@ -273,6 +274,7 @@ template <int KV, int HD, int WAVES, bool PREFIX>
 __global__ __launch_bounds__(64 * WAVES, HD == 256 && WAVES == 4 ? 1 : 2) void attend_tiles_kernel(TileArgs t) {
   constexpr int R = 32 * WAVES, TD = HD / 32, KS = HD / 16;
   constexpr bool Q16 = KV != kKvBf16;  // quantised: p and the values in fp16
+  constexpr int kUp = Q16 ? 7 : 0;     // p enters times 2^kUp: at most 2^15
   using frag = std::conditional_t<Q16, f16x8, bf16x8>;
   using Loader = TileLoader<KV, HD, WAVES>;
   using Shared = typename Loader::Shared;
@@ -535,7 +537,7 @@ __global__ __launch_bounds__(64 * WAVES, HD == 256 && WAVES == 4 ? 1 : 2) void a
         for (int i = 0; i < TD; ++i) o[i] *= shrink;
         m = raised;
       }
-      const float mb = (m == kNone ? 0.f : m) - (float)shift;
+      const float mb = (m == kNone ? 0.f : m) - (float)(shift + kUp);
       frag pf[4];
       float sum[2] = {0.f, 0.f}, even = 0.f;
       auto exponential = [&](int i) {
@@ -602,7 +604,8 @@ __global__ __launch_bounds__(64 * WAVES, HD == 256 && WAVES == 4 ? 1 : 2) void a
 
     l += __shfl_xor(l, 32);
     if constexpr (Q16) {
-      const float f = __uint_as_float((unsigned)(v_run + 1) << 23);
+      const float f = ldexpf(1.f, v_run - 126 - kUp);
+      l *= 1.f / (1 << kUp);
 #pragma unroll
       for (int i = 0; i < TD; ++i) o[i] *= f;
     }

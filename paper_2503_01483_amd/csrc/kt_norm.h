@@ -46,7 +46,7 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void add_rmsnorm_quant_kerne
   constexpr int ROWS = TPR >= 256 ? 1 : 256 / TPR;
   __shared__ float sh[TPR / 64][2];
   const int lane = threadIdx.x % TPR;
-  const int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / TPR;
+  const int64_t row = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * ROWS + threadIdx.x / TPR;
   if (row >= a.n) return;  // (a whole wave; rows that share a workgroup need no barrier)
   const T* x = static_cast<const T*>(a.x) + row * a.ldx;
   const T* res = a.res ? static_cast<const T*>(a.res) + row * a.ldres : nullptr;

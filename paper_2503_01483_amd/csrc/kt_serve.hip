@@ -12,6 +12,9 @@ namespace kt {
 
 static bool misaligned(const void* p, uintptr_t to) { return reinterpret_cast<uintptr_t>(p) & (to - 1); }
 
+// A launch's x has less than 2^32 threads.
+static bool grid_fits(int64_t wgs, int threads) { return wgs <= UINT32_MAX / threads; }
+
 // rows of `width` values of `dtype`: leading dimension and 16-byte alignment
 static bool rows_ok(const void* p, int64_t ld, int64_t width, kt_dtype dtype) {
   return ld >= width && ld <= ((int64_t)1 << 24) && ld % (dtype == KT_F32 ? 4 : 8) == 0 && !misaligned(p, 16);
@@ -23,7 +26,8 @@ static kt_status launch_norm(const NormArgs& a, hipStream_t st) {
   const int64_t chunks = ceil_div(a.d, 8);
   auto go = [&](auto tpr, auto ch) {
     constexpr int TPR = decltype(tpr)::value, CH = decltype(ch)::value, ROWS = TPR >= 256 ? 1 : 256 / TPR;
-    add_rmsnorm_quant_kernel<T, TG, FORMAT, TPR, CH><<<dim3((unsigned)ceil_div(a.n, ROWS)), TPR > 256 ? TPR : 256, 0, st>>>(a);
+    const int64_t wgs = ceil_div(a.n, ROWS), x = std::min<int64_t>(wgs, 1 << 20);
+    add_rmsnorm_quant_kernel<T, TG, FORMAT, TPR, CH><<<dim3((unsigned)x, (unsigned)ceil_div(wgs, x)), TPR > 256 ? TPR : 256, 0, st>>>(a);
   };
   using std::integral_constant;
   if (chunks <= 64) go(integral_constant<int, 64>{}, integral_constant<int, 1>{});
@@ -210,7 +214,7 @@ kt_status kt_kv_append(const kt_kv_cache* cache, const void* Q, int64_t ldq, con
                rope ? (int)rot_dim : 0, (int)chunks, interleaved != 0, hadamard != 0};
   hipStream_t st = static_cast<hipStream_t>(stream);
   const int64_t wgs = n * chunks + ceil_div(n, rows) * cache->n_heads;
-  if (wgs > INT32_MAX) return fail(KT_ERR_NOT_SUPPORTED, "too many rows for one call");
+  if (!grid_fits(wgs, 256)) return fail(KT_ERR_NOT_SUPPORTED, "too many rows for one call");
   with_cache(cache, [&](auto kv, auto h) {
     constexpr int KV = decltype(kv)::value, HD = decltype(h)::value;
     if (dtype == KT_F32) kv_append_kernel<float, KV, HD><<<dim3((unsigned)wgs), 256, 0, st>>>(a);
@@ -234,7 +238,7 @@ kt_status kt_kv_gather(const kt_kv_cache* cache, const int64_t* slots, int64_t n
   GatherArgs a{device_cache(cache), slots, K, V, ldk, ldv, (int)n, (int)chunks};
   hipStream_t st = static_cast<hipStream_t>(stream);
   const int64_t wgs = n * chunks + (V ? ceil_div(n, rows) * cache->n_heads : 0);
-  if (wgs > INT32_MAX) return fail(KT_ERR_NOT_SUPPORTED, "too many rows for one call");
+  if (!grid_fits(wgs, 256)) return fail(KT_ERR_NOT_SUPPORTED, "too many rows for one call");
   with_cache(cache, [&](auto kv, auto h) {
     constexpr int KV = decltype(kv)::value, HD = decltype(h)::value;
     if (dtype == KT_F32) kv_gather_kernel<float, KV, HD><<<dim3((unsigned)wgs), 256, 0, st>>>(a);
@@ -280,8 +284,11 @@ kt_status kt_paged_attention(const kt_kv_cache* cache, const void* Q, int64_t ld
   const int64_t group = n_q_heads / cache->n_heads;
   const bool few = few_rows(max_q, group);
   const int64_t entries = few ? n_seq : n_tokens * group / tile_rows(hd) + n_seq;
-  if (entries > INT32_MAX / cache->n_heads / (ceil_div(ldp * cache->page_size, 64) + (few ? 0 : ceil_div(prefix_len, 64) + kSegmentCost)))
+  if (entries > INT32_MAX / 2 / cache->n_heads / (ceil_div(ldp * cache->page_size, 64) + (few ? 0 : ceil_div(prefix_len, 64) + kSegmentCost)))
     return fail(KT_ERR_NOT_SUPPORTED, "too many tiles of 64 keys for one call: hand in a narrower page table or fewer tokens");
+
+  if (few && prefix_len && !grid_fits(ceil_div(n_tokens * n_q_heads, 1024 / hd), 256))
+    return fail(KT_ERR_NOT_SUPPORTED, "too many rows of queries for one call");
 
   const AttendPlan p = plan_attention(n_tokens, n_q_heads, hd, prefix_len);
   char* ws = static_cast<char*>(workspace);

@@ -173,3 +173,71 @@ def test_random_calls(seed):
     out, lse = torch.zeros(b.n, b.hq, hd, dtype=torch.bfloat16, device="cuda"), torch.zeros(b.n, b.hq, device="cuda")
     b.call(out=out, lse=lse)
     b.check(out, lse)
+
+
+@pytest.mark.parametrize("fmt", FMT, ids=IDS)
+def test_many_tokens_of_little_weight(fmt):
+    """One token outweighs each of 2^17 others by 2^25 and has a value of 0; the others' values are 1: together they are 2^-8 of it."""
+    hd, n, page, count = 64, (1 << 17) + 1, 1024, 20
+    cache = kt.KVCache(n // page + 1, page, 1, hd, fmt)
+    k, v = torch.zeros(n, 1, hd), torch.ones(n, 1, hd)
+    k[0, 0, 0], v[0] = 1, 0                                    # scores 25 ln 2 and 0, in every format
+    slots = torch.arange(n, device="cuda")
+    kt.kt_kv_append(cache, k.cuda(), v.cuda(), slots)
+    K, V = kt.kt_kv_gather(cache, slots, dtype=torch.float32)
+    assert torch.equal(K.cpu(), k) and torch.equal(V.cpu(), v)
+    q = torch.zeros(count, 1, hd, dtype=torch.bfloat16)
+    q[:, 0, 0] = 1
+    pages, lens = torch.arange(n // page + 1, dtype=torch.int32, device="cuda")[None], torch.tensor([n], dtype=torch.int32, device="cuda")
+    starts = torch.tensor([0, count], dtype=torch.int32, device="cuda")
+    lse = torch.zeros(count, 1, device="cuda")
+    out = kt.kt_paged_attention(q.cuda(), cache, pages, lens, q_starts=starts, max_q=count, scale=25 * math.log(2), lse=lse).cpu().double()
+    seen = n - count + torch.arange(count, dtype=torch.double)  # others than the first
+    mass = seen * 2.0 ** -25
+    want = (mass / (1 + mass))[:, None, None].expand_as(out)
+    # scale in fp32 times 1 / ln 2: the exponent is off by 2^-22 of 25 at most, p by 2^-18; a token's rounding 2^-31 (16 bits) or 2^-9; the result's 2^-9;
+    # 2^13 sums of 16 products, one after the other if the segment is not cut, each cut off to 24 bits: 2^-10
+    bound = want * (2.0 ** -18 + 2.0 ** -9 + 2.0 ** -10) * 1.01 + (want * 2.0 ** -9 if fmt == kt.KT_KV_BF16 else n * 2.0 ** -31)
+    assert bool(((out - want).abs() <= bound).all()), float(((out - want).abs() / bound).max())
+    assert bool(((lse.cpu()[:, 0].double() - (25 * math.log(2) + torch.log1p(mass))).abs() <= 2.0 ** -17).all())
+
+
+@pytest.mark.parametrize("fmt", FMT, ids=IDS)
+def test_values_near_the_end_of_the_range(fmt):
+    """Values of 2^124 and of 2^-120, each alone and together."""
+    for values in ([2.0 ** 124], [2.0 ** -120], [2.0 ** 124, 2.0 ** -120, 2.0 ** 124], [2.0 ** -120] * 3):
+        n, count = len(values), 1
+        cache = kt.KVCache(1, 64, 1, 64, fmt)
+        v = torch.tensor(values)[:, None, None].expand(n, 1, 64).contiguous()
+        kt.kt_kv_append(cache, torch.zeros(n, 1, 64, device="cuda"), v.cuda(), torch.arange(n, device="cuda"))
+        for group in (1, 32):                                   # few rows, many
+            q, pages, lens = torch.zeros(count, group, 64, dtype=torch.bfloat16), torch.zeros(1, 1, dtype=torch.int32), torch.tensor([n], dtype=torch.int32)
+            out = kt.kt_paged_attention(q.cuda(), cache, pages.cuda(), lens.cuda()).cpu().double()
+            want = sum(values) / n
+            assert bool(((out - want).abs() <= want * (2.0 ** -8 + 2.0 ** -10)).all()), (values, group)
+
+
+@pytest.mark.parametrize("hd", [64, 256])
+def test_as_many_sequences_as_a_call_takes(hd):
+    n = 4096
+    lens = [(7 * i) % 5 for i in range(n)]
+    b = Batch(kt.KT_KV_U8, hd, 1, 1, lens, seed=12, page=64)
+    out, lse = torch.zeros(b.n, b.hq, hd, dtype=torch.bfloat16, device="cuda"), torch.zeros(b.n, b.hq, device="cuda")
+    b.call(out=out, lse=lse)
+    b.check(out, lse)
+    wide = Batch(kt.KT_KV_U8, hd, 1, 32, lens, seed=13, page=64)
+    out, lse = torch.zeros(wide.n, wide.hq, hd, dtype=torch.bfloat16, device="cuda"), torch.zeros(wide.n, wide.hq, device="cuda")
+    wide.call(out=out, lse=lse)
+    wide.check(out, lse)
+
+
+@pytest.mark.parametrize("n,d", [((1 << 22) + 9, 8), ((1 << 20) + 3, 1024)])
+def test_norm_of_more_rows_than_a_row_of_workgroups(n, d):
+    x = torch.randn(n, d, dtype=torch.bfloat16, device="cuda")
+    call = lambda rows: kt.kt_add_rmsnorm_quant(rows, codes=torch.empty(rows.shape, dtype=torch.int8, device="cuda"),  # noqa: E731
+                                                scales=torch.empty(rows.shape[0], device="cuda"))
+    codes, scales = call(x)
+    for rows in (slice(0, 7), slice(n // 2, n // 2 + 9), slice(n - 11, n)):
+        want = call(x[rows].clone())
+        assert torch.equal(codes[rows], want[0]) and torch.equal(scales[rows], want[1])
+    assert bool((codes.abs().amax(1) == 127).all())

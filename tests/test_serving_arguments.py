@@ -91,7 +91,8 @@ def _attend(L, cache=None, Q=FAKE, ldq=512, dt=1, starts=FAKE, lens=FAKE, pages=
     (dict(pl=(1 << 30) + 1, pp=FAKE), 1, "prefix_len"), (dict(scale=0.0), 1, "scale"), (dict(scale=-1.0), 1, "scale"), (dict(scale=float("nan")), 1, "scale"),
     (dict(scale=float("inf")), 1, "scale"), (dict(ws=None), 4, "workspace"), (dict(wsb=1000), 4, "workspace"), (dict(ws=(1 << 20) + 16), 1, "256-byte"),
     (dict(lens=FAKE + 2), 2, "aligned"), (dict(lse=FAKE + 1), 2, "aligned"), (dict(cache=_cache(fmt=-3)), 3, "format"),
-    (dict(n_seq=4096, starts=None, n=4096, max_q=1, ldp=1 << 20), 6, "too many")])
+    (dict(n_seq=4096, starts=None, n=4096, max_q=1, ldp=1 << 20), 6, "too many"),
+    (dict(n=1 << 28, max_q=1, pl=64, pp=FAKE, wsb=1 << 62), 6, "too many")])
 def test_attention_refuses(bad, status, text):
     L = kt.lib()
     assert _attend(L, **bad) == status and text in kt.kt_last_error()
