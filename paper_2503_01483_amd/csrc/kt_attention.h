@@ -8,7 +8,11 @@
 // holds the scores of one row and of 16 keys that lie next to each other in its column of V^T: after the exponentials the scores ARE
 // the operand of O^T = V^T P^T.  Nothing goes through LDS but the quantisers' parameters, no wave waits for another.
 // All key tiles of all segments form one list, and every wave takes an equal piece of it, whatever the lengths: a segment that is
-// cut leaves {O, max, sum} of each piece in the workspace, and a second launch puts them together.
+// cut leaves {O, max, sum} of each piece in the workspace, and a second launch puts them together (5 to 8 us).
+//
+// Bound by HBM: 64 tokens behind up to 16384, 32 + 2 x 8 heads of 128, 4 bits: 157 us, 4.9 TB/s (a large copy: 4.8); 4 behind 131072, 8 bits: 146 us,
+// 5.6 TB/s.  One token behind 1027: 11 us, a chain of lookups, loads and products by waves of one or two tiles each.
+// More rows than 16 read their keys again, mostly from the caches on the way.
 //
 // Quantised rows are never expanded: k = s c + b gives q . k = s (q . c) + b sum(q), and v = s c + b gives p v = (p s) c + p b, so that the
 // codes themselves, exact in bf16, are the operands.  A 4-bit code becomes 128 + c by OR (0x4300 | c), two at a time; a product of
@@ -28,6 +32,7 @@ struct AttendArgs {
   const int *q_starts, *lens, *pages;  // q_starts null: token i is the only query of sequence i
   int64_t ldq, ldp;
   int n_seq, n_tokens, hq, group;
+  int row_tiles;  // kt_attention.h: at most this many of a sequence
   float scale;
   bf16* out;
   int64_t ldo;
@@ -35,7 +40,7 @@ struct AttendArgs {
   // workspace
   int workers;   // waves that take pieces of the list
   int* tiles;    // [n_seq + 1] key tiles of one head in front of each sequence
-  int4* cuts;    // [workers] the segment whose first piece a worker has while others have the rest: {first token, rows, head, pieces or 0}
+  int4* cuts;    // [workers] the segment whose first piece a worker has while others have the rest: {first token, first row * 32 + rows, head, pieces or 0}
   float* part;   // pieces of cut segments: O [2 workers][kRows][HD], then {max in bits, sum} [2 workers][kRows]
   float* whole;  // null: whole segments go to out.  Else something is to be joined: O [n_tokens][hq][HD], then {max, sum} [n_tokens][hq]
 };
@@ -54,9 +59,12 @@ __device__ __forceinline__ Sequence sequence_of(const AttendArgs& a, int s) {
   return q;
 }
 __device__ __forceinline__ int key_tiles(const Sequence& q) { return max(1, (int)(((unsigned)q.len + 63) >> 6)); }
+__device__ __forceinline__ int row_tiles(const AttendArgs& a, const Sequence& q) {
+  return (int)min(((int64_t)q.count * a.group + kRows - 1) / kRows, (int64_t)a.row_tiles);
+}
 
-// Key tiles of one head in front of each sequence, `cum` [n_seq + 1] (LDS), by a workgroup of 256.  A sequence of more than kRows rows
-// breaks the caller's bound: its first kRows are computed.
+// Key tiles of one head in front of each sequence, those of each of its row tiles, `cum` [n_seq + 1] (LDS), by a workgroup of 256.  Of a
+// sequence with more rows than the caller's bound the first ones are computed.
 __device__ __forceinline__ void list_tiles(const AttendArgs& a, int* cum) {
   __shared__ int wave_sum[4];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -66,7 +74,7 @@ __device__ __forceinline__ void list_tiles(const AttendArgs& a, int* cum) {
     int mine = 0;
     if (s < a.n_seq) {
       const Sequence q = sequence_of(a, s);
-      mine = q.count ? key_tiles(q) : 0;
+      mine = row_tiles(a, q) * key_tiles(q);
     }
     int upto = mine;
 #pragma unroll
@@ -220,12 +228,14 @@ __device__ __forceinline__ unsigned long long any_lane(unsigned long long which)
   return all;
 }
 
-// The list's order: sequences, in each its heads, in each its tiles.
+// The list's order: sequences, in each its heads, in each its row tiles, in each the key tiles.
 template <int KV, int HD>
 __global__ __launch_bounds__(256, HD == 256 ? 1 : 2) void attend_rows_kernel(AttendArgs a) {
   extern __shared__ int cum[];
   __shared__ float4 params[4][64];
   constexpr int TD = HD / 16;
+  // The next tile asked for as registers come free, where it needs no more of them: decode of 64 behind 16384, 4 bits, 172 -> 166 us.  With 8 bits
+  // registers spill (4 behind 131072: 138 -> 165), and bf16 tiles take as many as there are.
   constexpr bool kEarly = KV == kKvU4 && HD <= 128;
   constexpr float kOffset = KV == kKvU4 ? 136.f : 128.f, kCentre = KV == kKvU4 ? 8.f : 128.f;
   constexpr float kNone = -__builtin_inff();
@@ -244,14 +254,15 @@ __global__ __launch_bounds__(256, HD == 256 ? 1 : 2) void attend_rows_kernel(Att
     const int s = uniform(sequence_at(cum, a.n_seq, (int)((unsigned)u / (unsigned)heads)));
     const Sequence q = sequence_of(a, s);
     const int tiles = uniform(key_tiles(q)), rel = u - uniform(cum[s]) * heads;
-    const int head = uniform((int)((unsigned)rel / (unsigned)tiles)), start = u - (rel - head * tiles);
+    const int in_head = tiles * row_tiles(a, q), head = uniform((int)((unsigned)rel / (unsigned)in_head)), behind = rel - head * in_head;
+    const int row_tile = uniform((int)((unsigned)behind / (unsigned)tiles)), start = u - (behind - row_tile * tiles), row0 = row_tile * kRows;
     const int first = u - start, last = min(tiles, end - start);
 
     // this lane's row
-    const int in_seq = r / a.group, qh = head * a.group + (r - in_seq * a.group);
+    const int in_seq = (row0 + r) / a.group, qh = head * a.group + (row0 + r - in_seq * a.group);
     const bool live = in_seq < q.count;
     const int64_t token = q.first + (live ? in_seq : 0);
-    const int sees = min(max(q.len - q.count + in_seq + 1, 0), q.len), all_see = q.len - q.count + 1;
+    const int sees = min(max(q.len - q.count + in_seq + 1, 0), q.len), all_see = q.len - q.count + row0 / a.group + 1;
     bf16x8 qf[HD / 32];
     float qsum = 0.f;
 #pragma unroll
@@ -454,7 +465,7 @@ __global__ __launch_bounds__(256, HD == 256 ? 1 : 2) void attend_rows_kernel(Att
               make_float2(l == 0.f ? kNone : m * c, l);
       }
       if (first == 0 && !whole)
-        cut = int4{q.first, min(q.count * a.group, kRows), head, (int)((unsigned)(start + tiles - 1) / (unsigned)per) - me + 1};
+        cut = int4{q.first, row0 * 32 + (int)min((int64_t)q.count * a.group - row0, (int64_t)kRows), head, (int)((unsigned)(start + tiles - 1) / (unsigned)per) - me + 1};
     }
     u = start + last;
   }
@@ -472,7 +483,8 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
   if (cut.w == 0) return;
   const float2* ml = reinterpret_cast<const float2*>(a.part + (int64_t)2 * a.workers * kRows * HD);
   const int t = threadIdx.x % TR, at = threadIdx.x / TR;
-  for (int r = blockIdx.y; r < cut.y; r += gridDim.y) {
+  const int row0 = cut.y >> 5, rows = cut.y & 31;
+  for (int r = blockIdx.y; r < rows; r += gridDim.y) {
     float m = kNone, l = 0.f;
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
     for (int k = at; k < cut.w; k += AT) {
@@ -502,7 +514,7 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
         l = fmaf(sh_ml[i].y, f, l);
         o += sh_o[i][t] * f;
       }
-      const int64_t token = cut.x + r / a.group, qh = cut.z * a.group + r % a.group;
+      const int64_t token = cut.x + (row0 + r) / a.group, qh = cut.z * a.group + (row0 + r) % a.group;
       const float inv = l == 0.f ? 0.f : 1.f / l;
       bf16 v[4];
 #pragma unroll

@@ -7,6 +7,8 @@
 //
 // A wave's tile takes the matrix cores 1024 cycles (HD = 128) and the vector ALU about as long, most of it exponentials: three quarters of them are
 // worked out beside the products of the values that need the others, the rest beside the other wave of the SIMD.
+// 2 x 8192 tokens, 32 + 2 x 8 heads of 128, bf16: 840 us, 805 TFLOP/s (a matrix product of 8192: 1143); 8 x 300 behind 8000, 4 bits: 253 us, 610.  A tile of 64
+// keys takes a CU 4400 cycles, 2048 of them products and 2300 the LDS's reads for them, at 2.0 to 2.2 GHz; a segment 19000 more, at its ends.
 //
 // bf16 caches go straight from memory to LDS.  Of quantised ones the keys' codes do, as exact bf16 values, and a score becomes s (q . c) + b sum(q)
 // in fp32 as in kt_attention.h; the values are expanded on the way, in fp16: a row s c + b is scaled by a power of two per
@@ -51,7 +53,8 @@ __device__ __forceinline__ int64_t first_entry(const AttendArgs& a, int s, int R
   return (int64_t)min(max(a.q_starts ? a.q_starts[s] : s, 0), a.n_tokens) * a.group / R + s;
 }
 
-// What a segment costs beside its tiles, in tiles: its queries, the first tiles' way to LDS, its output.  Counted in the list, in front of them.
+// What a segment costs beside its tiles, in tiles: its queries, the first tiles' way to LDS, its output (19000 cycles, a tile 4400).  Counted in the
+// list, in front of them, so that pieces take equally long.
 constexpr int kSegmentCost = 4;
 
 // The list of row tiles.  One workgroup of 1024.
@@ -708,9 +711,9 @@ __global__ __launch_bounds__(256) void join_prefix_kernel(TileArgs t) {
   }
   const Sequence q = sequence_of(a, s);
   const int r = (token - q.first) * a.group + qh - head * a.group;
-  if (token < q.first || token >= q.first + q.count || r >= kRows) return;
+  if (token < q.first || token >= q.first + q.count || r >= a.row_tiles * kRows) return;
   const int total = a.tiles[a.n_seq] * a.cache.n_heads, per = piece_length(total, a.workers);
-  const int tiles = key_tiles(q), start = a.tiles[s] * a.cache.n_heads + head * tiles;
+  const int tiles = key_tiles(q), start = a.tiles[s] * a.cache.n_heads + (head * row_tiles(a, q) + r / kRows) * tiles;
   const int w0 = (int)((unsigned)start / (unsigned)per), w1 = (int)((unsigned)(start + tiles - 1) / (unsigned)per);
   Joined j;
   const int64_t rows = (int64_t)a.n_tokens * a.hq;
@@ -721,7 +724,7 @@ __global__ __launch_bounds__(256) void join_prefix_kernel(TileArgs t) {
   } else {
     const float2* ml = reinterpret_cast<const float2*>(a.part + (int64_t)2 * a.workers * kRows * HD);
     for (int w = w0; w <= w1; ++w) {
-      const int64_t slot = (2 * (int64_t)w + (w == w0 ? 1 : 0)) * kRows + r;
+      const int64_t slot = (2 * (int64_t)w + (w == w0 ? 1 : 0)) * kRows + r % kRows;
       j.add(ml[slot], *reinterpret_cast<const f32x4*>(a.part + slot * HD + lane4));
     }
   }

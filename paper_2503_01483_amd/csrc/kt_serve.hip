@@ -30,10 +30,13 @@ static kt_status launch_norm(const NormArgs& a, hipStream_t st) {
     add_rmsnorm_quant_kernel<T, TG, FORMAT, TPR, CH><<<dim3((unsigned)x, (unsigned)ceil_div(wgs, x)), TPR > 256 ? TPR : 256, 0, st>>>(a);
   };
   using std::integral_constant;
+  // As many threads a row as leave none idle and a thread one or two chunks: 64 rows / 8192 rows, us, bf16 to 8 bits, with a sum:
+  //   512  64 threads 3.3 / 7.1;   2048  64 threads 5.9 / 21.1, 256 threads 3.5 / 22.9;   4096  256 threads 4.9 / 40.5;
+  //   8192  256 threads 6.2 / 98.0, 1024 threads 4.5 / 87.5;   16384  1024 threads 5.8 / 176;   32768  8.5 / 357
   if (chunks <= 64) go(integral_constant<int, 64>{}, integral_constant<int, 1>{});
   else if (chunks <= 256) go(integral_constant<int, 256>{}, integral_constant<int, 1>{});
   else if (chunks <= 512) go(integral_constant<int, 256>{}, integral_constant<int, 2>{});
-  else if (chunks <= 1024) go(integral_constant<int, 256>{}, integral_constant<int, 4>{});
+  else if (chunks <= 1024) go(integral_constant<int, 1024>{}, integral_constant<int, 1>{});
   else if (chunks <= 2048) go(integral_constant<int, 1024>{}, integral_constant<int, 2>{});
   else go(integral_constant<int, 1024>{}, integral_constant<int, 4>{});
   return launch_ok() ? KT_OK : fail(KT_ERR_DEVICE, "norm kernel launch failed");
@@ -92,19 +95,30 @@ static KvCache device_cache(const kt_kv_cache* c) {
 }
 
 // ------------------------------------------------------------------ attention -----
-constexpr int64_t kWaveWorkers = (int64_t)kNumCUs * 8;  // waves that share the key tiles of single tokens: two workgroups of four a CU
+constexpr int64_t kWaveWorkers = (int64_t)kNumCUs * 8;  // waves that share the key tiles of few rows: two workgroups of four a CU, all resident
 constexpr int64_t kMaxTokens = (int64_t)1 << 30;         // of a sequence's pages, of a prefix
 constexpr int64_t kMaxSequences = 4096;                 // their tile counts are listed in LDS
-// Waves of a workgroup of kt_attention_tiles.h: two a SIMD; one where a head of 256 features takes all registers.
+// Waves of a workgroup of kt_attention_tiles.h: two a SIMD; one where a head of 256 features takes all registers.  (Two workgroups of four
+// waves instead of one of eight: a prompt of 2 x 8192 tokens, 32 heads of 128, bf16, 938 us instead of 839: every tile is copied twice.)
 constexpr int tile_waves(int64_t hd) { return hd == 256 ? 4 : 8; }
 constexpr int64_t tile_rows(int64_t hd) { return 32 * tile_waves(hd); }
 constexpr int64_t kTileWorkers = kNumCUs;  // as many as are resident (LDS)
 
-// Single tokens (and few: up to 16 rows a head) take kt_attention.h, which reads each key for its own sequence only; what has more rows
-// takes kt_attention_tiles.h, whose tiles of 256 rows are wasted on fewer.
-static bool few_rows(int64_t max_q, int64_t group) { return max_q * group <= kRows; }
+// Single tokens and a few at a time take kt_attention.h, whose time grows with every sixteen rows a head; what has more rows takes
+// kt_attention_tiles.h, whose tiles of 256 rows are wasted on fewer.  By the rows of a sequence and head, us with the one / the other, 64
+// sequences of 4096 tokens (4 of 30000), 8 heads:
+//   bf16  64 features   32 rows 161 / 228 (90 / 112), 64 rows 268 / 221;     128 features  16 rows 221 / 326, 32 rows 301 / 315 (182 / 160);
+//         256 features  16 rows 408 / 522, 32 rows 559 / 500
+//   u8    64 features   64 rows 190 / 303 (103 / 151), 96 rows 314 / 304;    128 features  64 rows 281 / 369 (166 / 186), 96 rows 475 / 375;
+//         256 features  32 rows 365 / 506 (208 / 249), 64 rows 586 / 512
+//   u4    64 features   64 rows 150 / 294 (87 / 148);                        128 features  64 rows 215 / 372 (114 / 184), 128 rows 417 / 382;
+//         256 features  64 rows 343 / 469 (185 / 231), 96 rows 562 / 472
+static int64_t most_few_rows(const kt_kv_cache* c) {
+  if (c->format == KT_KV_BF16) return c->head_dim == 64 ? 32 : 16;
+  return c->format == KT_KV_U8 && c->head_dim == 256 ? 32 : 64;
+}
 
-// Tiles of a prefix that single tokens share are split until the launch fills the card.
+// Tiles of a prefix that single tokens share are split until the launch fills the card (96 tokens, 8192 in front: 16 splits).
 static int64_t prefix_splits(int64_t n_tokens, int64_t hq, int64_t n_heads, int64_t hd, int64_t prefix_len) {
   const int64_t items = ceil_div(n_tokens * (hq / n_heads), tile_rows(hd)) * n_heads;
   return std::max<int64_t>(1, std::min(kTileWorkers / items, ceil_div(prefix_len, 64)));
@@ -282,8 +296,10 @@ kt_status kt_paged_attention(const kt_kv_cache* cache, const void* Q, int64_t ld
     return fail(KT_ERR_BAD_SHAPE, "index arrays and lse must be aligned to their type");
 
   const int64_t group = n_q_heads / cache->n_heads;
-  const bool few = few_rows(max_q, group);
-  const int64_t entries = few ? n_seq : n_tokens * group / tile_rows(hd) + n_seq;
+  const int64_t most = most_few_rows(cache);
+  const bool few = max_q <= most && max_q * group <= most;
+  const int64_t row_tiles = few ? ceil_div(max_q * group, kRows) : 0;
+  const int64_t entries = few ? n_seq * row_tiles : n_tokens * group / tile_rows(hd) + n_seq;
   if (entries > INT32_MAX / 2 / cache->n_heads / (ceil_div(ldp * cache->page_size, 64) + (few ? 0 : ceil_div(prefix_len, 64) + kSegmentCost)))
     return fail(KT_ERR_NOT_SUPPORTED, "too many tiles of 64 keys for one call: hand in a narrower page table or fewer tokens");
 
@@ -306,6 +322,7 @@ kt_status kt_paged_attention(const kt_kv_cache* cache, const void* Q, int64_t ld
   a.n_tokens = (int)n_tokens;
   a.hq = (int)n_q_heads;
   a.group = (int)group;
+  a.row_tiles = (int)row_tiles;
   a.scale = scale;
   a.out = static_cast<bf16*>(O);
   a.ldo = ldo;

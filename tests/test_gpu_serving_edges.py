@@ -241,3 +241,15 @@ def test_norm_of_more_rows_than_a_row_of_workgroups(n, d):
         want = call(x[rows].clone())
         assert torch.equal(codes[rows], want[0]) and torch.equal(scales[rows], want[1])
     assert bool((codes.abs().amax(1) == 127).all())
+
+
+@pytest.mark.parametrize("fmt,hd,group,counts", [(kt.KT_KV_U4, 128, 3, [7, 21, 1, 0, 20]), (kt.KT_KV_U8, 64, 1, [64, 17, 33]), (kt.KT_KV_BF16, 64, 32, [1, 1, 1]),
+                                                 (kt.KT_KV_U8, 256, 5, [6, 3]), (kt.KT_KV_U4, 256, 64, [1, 1]), (kt.KT_KV_U4, 64, 9, [7, 5])])
+@pytest.mark.parametrize("prefix", [0, 130])
+def test_a_few_rows_more_than_sixteen(fmt, hd, group, counts, prefix):
+    """Rows of one token on both sides of a boundary between row tiles; segments cut between workers; with and without a prefix."""
+    for lens in ([max(n, t) for n, t in zip(counts, (300, 64, 1, 0, 1000))], [n + 5000 for n in counts]):
+        b = Batch(fmt, hd, 2, group, lens, counts, prefix=prefix, seed=14, pad=2)
+        out, lse = torch.zeros(b.n, b.hq, hd, dtype=torch.bfloat16, device="cuda"), torch.zeros(b.n, b.hq, device="cuda")
+        b.call(out=out, lse=lse)
+        b.check(out, lse)
