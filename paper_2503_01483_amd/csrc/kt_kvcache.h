@@ -95,20 +95,40 @@ __device__ __forceinline__ void rotate_position(float (&y)[8], const float* row,
   float c[8], s[8];
   load8(row + at, c);
   load8(row + half + at, s);
+  const float sign = second ? 1.f : -1.f;
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
     const float p = y[e] * c[e], r = z[e] * s[e];
-    y[e] = second ? p + r : p - r;
+    y[e] = fmaf(r, sign, p);  // p + r or p - r: the product is exact
   }
 }
 
-// H / sqrt(8 LPR) on the row, butterflies by distances 1, 2, 4, ...; fp32, one rounding an operation.
+// H / sqrt(8 LPR) on the row, butterflies by distances 1, 2, 4, ...; fp32, one rounding an operation.  Across lanes the second of a pair takes
+// y - p for p - y, which makes a step one instruction on its neighbour's value; the sign (of the parity of the lane's number) is put right at the end.
+// (Assembly: the compiler makes it a move, a wait and a multiply-add.  A value that the vector ALU has written, or its mask of lanes, may be read across
+// lanes two and five instructions later.)
+// One step: y += sign * (y of the neighbour at distance S).
+template <int S>
+__device__ __forceinline__ void add_neighbours(float (&y)[8], float sign) {
+#define KT_EIGHT(how)                                                                                                        \
+  asm volatile("s_nop 4\n\tv_fmac_f32_dpp %0, %0, %8 " how "\n\tv_fmac_f32_dpp %1, %1, %8 " how "\n\tv_fmac_f32_dpp %2, %2, %8 " how      \
+      "\n\tv_fmac_f32_dpp %3, %3, %8 " how "\n\tv_fmac_f32_dpp %4, %4, %8 " how "\n\tv_fmac_f32_dpp %5, %5, %8 " how              \
+      "\n\tv_fmac_f32_dpp %6, %6, %8 " how "\n\tv_fmac_f32_dpp %7, %7, %8 " how                                                \
+      : "+v"(y[0]), "+v"(y[1]), "+v"(y[2]), "+v"(y[3]), "+v"(y[4]), "+v"(y[5]), "+v"(y[6]), "+v"(y[7])                       \
+      : "v"(sign))
+  if constexpr (S == 1) KT_EIGHT("quad_perm:[1,0,3,2] row_mask:0xf bank_mask:0xf");
+  else if constexpr (S == 2) KT_EIGHT("quad_perm:[2,3,0,1] row_mask:0xf bank_mask:0xf");
+  else if constexpr (S == 8) KT_EIGHT("row_ror:8 row_mask:0xf bank_mask:0xf");
+  else
+#pragma unroll
+    for (int e = 0; e < 8; ++e) y[e] = fmaf(lane_xor<S>(y[e]), sign, y[e]);
+#undef KT_EIGHT
+}
 template <int LPR, int S>
 __device__ __forceinline__ void butterfly(float (&y)[8], int l) {
   if constexpr (S < LPR) {
-    const float sign = l & S ? -1.f : 1.f;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) y[e] = fmaf(y[e], sign, lane_xor<S>(y[e]));  // y + p or p - y: the product is exact
+    const float sign = l & S ? -1.f : 1.f;  // (a product with it is exact)
+    add_neighbours<S>(y, sign);
     butterfly<LPR, 2 * S>(y, l);
   }
 }
@@ -125,7 +145,8 @@ __device__ __forceinline__ void rotate_hadamard(float (&y)[8], int l) {
         y[e + s] = a - b;
       }
   butterfly<LPR, 1>(y, l);
-  constexpr float norm = LPR == 8 ? 0.125f : LPR == 16 ? 0.08838834764831845f : 0.0625f;
+  constexpr float root = LPR == 8 ? 0.125f : LPR == 16 ? 0.08838834764831845f : 0.0625f;
+  const float norm = __popc(l) & 1 ? -root : root;
 #pragma unroll
   for (int e = 0; e < 8; ++e) y[e] *= norm;
 }
