@@ -199,7 +199,7 @@ __device__ __forceinline__ char* place_of(const KvCache& c, int64_t slot, int he
 // HD / 8 lanes a row of 8 values each.  The first n * chunks workgroups take the queries and keys of a token: rotated, then to q_out or into
 // their pages.  The others take the values of one head and of as many tokens as the workgroup has rows: these cross over to rows by feature in LDS,
 // so that the bytes of neighbouring slots are written together.
-// 8192 tokens of 32 + 2 x 8 heads of 128, rotated twice, to 4 bits: 73 us, 3.1 TB/s, bound by the vector ALU (450 instructions a wave; the bytes
+// 8192 tokens of 32 + 2 x 8 heads of 128, rotated twice, to 4 bits: 71 us, 3.2 TB/s, bound by the vector ALU (the bytes
 // alone would take 47); 64 tokens 5.1 us; 1537 of heads of 64, to 8 bits, 9.8 us.  A row takes HD / 8 lanes, so that a lane's loads are 16 bytes and the
 // exchanges of both rotations stay within a row of 16 lanes (vector ALU, no LDS) up to 128 features.
 template <typename T, int KV, int HD>
