@@ -1,0 +1,48 @@
+"""kt_paged_attention against what its documentation says of each rounding: no more is off, whatever the values' sizes."""
+import pytest
+import torch
+
+import paper_2503_01483_amd as kt
+from attention_bounds import check, replace
+from serving_util import Batch
+
+pytestmark = pytest.mark.gpu
+FMT = [kt.KT_KV_BF16, kt.KT_KV_U8, kt.KT_KV_U4]
+IDS = ["bf16", "u8", "u4"]
+
+
+def run(b, **kw):
+    out, lse = torch.zeros(b.n, b.hq, b.hd, dtype=torch.bfloat16, device="cuda"), torch.zeros(b.n, b.hq, device="cuda")
+    b.call(out=out, lse=lse, **kw)
+    return out, lse
+
+
+@pytest.mark.parametrize("fmt", FMT, ids=IDS)
+@pytest.mark.parametrize("hd,group", [(64, 3), (128, 4), (256, 2)])
+def test_every_rounding_is_within_its_bound(fmt, hd, group):
+    """Few rows and many, with and without a prefix: values of one size, and values that all lie on one side (their output does not cancel)."""
+    for counts in ([2, 1, 7], [70, 33, 5]):
+        for prefix in (0, 100):
+            b = Batch(fmt, hd, 2, group, [300, 64, 9], counts, prefix=prefix, seed=hd + prefix)
+            check(b, *run(b))
+
+
+@pytest.mark.parametrize("fmt", FMT, ids=IDS)
+def test_sums_are_not_biased(fmt):
+    """A value that all tokens share comes back as itself: what p is rounded by may go either way, not one.
+
+    256 values (sequences x heads), sixteen to a step of bf16, evenly and none nearer than 2^-12 to the middle of two: rounded to bf16 their errors cancel.
+    A row's 130 independent roundings of p (2^-11 each at most, fp16; 2^-8, bf16) move its sum by 2^-15 (2^-12), either way, and so change results of 16896 rows
+    by less than 2^-13 in the mean; p cut off to 11 bits is 2^-11.5 too small in the mean, which takes one of sixteen values a step of 2^-7 down: 2^-11."""
+    b = Batch(fmt, 64, 8, 1, [130] * 32, [66] * 32, seed=23)
+    step = torch.arange(256).reshape(32, 1, 8, 1)
+    value = 1 + step.div(16, rounding_mode="floor") * 2.0 ** -7 + (step % 16 + 0.5) * 2.0 ** -11
+    for s in range(32):
+        replace(b, s, range(130), v=value[s].expand(130, 8, 64).contiguous())
+    out, lse = run(b)
+    check(b, out, lse)
+    want = torch.cat([b.v[s][:1].expand(66, 8, 64) for s in range(32)])
+    if fmt != kt.KT_KV_BF16:
+        assert torch.equal(want[::66], value[:, 0].expand(32, 8, 64).double())        # (a row of one value is held as its minimum)
+    far = float((out.cpu().double() - want).mean().abs())
+    assert far < 2.0 ** -13, far
