@@ -12,8 +12,9 @@
 //
 // bf16 caches go straight from memory to LDS.  Of quantised ones the keys' codes do, as exact bf16 values, and a score becomes s (q . c) + b sum(q)
 // in fp32 as in kt_attention.h; the values are expanded on the way, in fp16: a row s c + b is scaled by a power of two per
-// tile, found from the rows' {s, b}, so that its largest value is just below one, and rounded to 11 bits (2^-11 of it or less; bf16 would have 8, little
-// more than the codes of 8 bits).  The exponent is carried along with O like the running maximum.  The maximum is raised only
+// tile, found from the rows' {s, b}, so that its largest value is just below one, and computed in fp16 as s (c - middle) + (b + s middle): the roundings
+// of both parts and of the sum are 1.5 x 2^-11 of that largest value together (uncentred, s c is off by up to 2^-11 of the row's whole width
+// more; bf16 would have 2^-8, little more than the codes of 8 bits).  The exponent is carried along with O like the running maximum.  The maximum is raised only
 // once a score passes it by 2^8 (p stays below 256 in either type).  In fp16 p goes in times 2^7: what it cuts off where p is small then is
 // 2^-31 of the largest p at most, and a million tokens of it do not show in a result.
 //
@@ -113,7 +114,7 @@ struct TileShared {
   char keys[2][kTile];          // [64][HD]
   char values[2][kTile];        // [HD][64]
   float2 par[2][64];            // {step, minimum} of the keys, times the factor of the exponentials
-  _Float16 expand[WAVES][2][64];  // steps and minima of the values that are being expanded
+  _Float16 expand[WAVES][2][64];  // steps of the values that are being expanded, and what their middle code stands for
   unsigned long long odd[2][WAVES];  // bf16: tokens of a masked tile with values that are not finite, those in the pieces of each wave
 };
 
@@ -195,7 +196,7 @@ struct TileLoader {
   // not finite (as 0).  v_run: exponent of O so far, for a floor.
   __device__ __forceinline__ int put_values(Shared& sh, int at, int there, int v_run, unsigned long long& odd) const {
     const int tid = thread(), lane = tid & 63, wave = uniform(tid >> 6);
-    constexpr float top = KV == kKvU4 ? 15.f : 255.f;
+    constexpr float top = KV == kKvU4 ? 15.f : 255.f, centre = KV == kKvU4 ? 8.f : 128.f;
     float vs = lane < there ? vp.x : 0.f, vb = lane < there ? vp.y : 0.f;
     float most = fmaxf(fabsf(vb), fabsf(fmaf(top, vs, vb)));
     const bool bad = !(most <= kHuge) || vs != vs;
@@ -204,11 +205,11 @@ struct TileLoader {
     const int v_exp = max(min(wave_max((int)(__float_as_uint(most) >> 23)), 252), v_run - 60);
     const float f = __uint_as_float((unsigned)(253 - v_exp) << 23);
     sh.expand[wave][0][lane] = (_Float16)(vs * f);
-    sh.expand[wave][1][lane] = (_Float16)(vb * f);
+    sh.expand[wave][1][lane] = (_Float16)(fmaf(centre, vs, vb) * f);
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
     __builtin_amdgcn_wave_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-    const f16x2 bias = {(_Float16)-1024.f, (_Float16)-1024.f};
+    const f16x2 bias = {(_Float16)(-1024.f - centre), (_Float16)(-1024.f - centre)};  // (1024 + c - 1024 - centre: exact)
     auto half2 = [](uint32_t x) { return __builtin_bit_cast(f16x2, x); };
 #pragma unroll
     for (int i = 0; i < VP; ++i) {

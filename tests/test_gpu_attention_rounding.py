@@ -46,3 +46,27 @@ def test_sums_are_not_biased(fmt):
         assert torch.equal(want[::66], value[:, 0].expand(32, 8, 64).double())        # (a row of one value is held as its minimum)
     far = float((out.cpu().double() - want).mean().abs())
     assert far < 2.0 ** -13, far
+
+
+def one_key_a_query(b, seq, tokens, seed):
+    """Queries of a sequence that each attend to one token, by 2^-20 or more."""
+    g = torch.Generator().manual_seed(seed)
+    k = torch.randn(b.lens[seq], b.hkv, b.hd, generator=g)
+    replace(b, seq, range(b.lens[seq]), k=k)
+    b.q[b.starts[seq]:b.starts[seq + 1]] = (64 / b.hd ** 0.5 * k[tokens]).repeat_interleave(b.hq // b.hkv, 1).to(torch.bfloat16)
+
+
+@pytest.mark.parametrize("fmt", FMT[1:], ids=IDS[1:])
+@pytest.mark.parametrize("hd", [64, 128, 256])
+def test_values_of_many_rows_lose_no_more_than_their_bound(fmt, hd):
+    """Rows just wider than -1 to 1, where the step's rounding and the middle's are as large as they get; one key a query, so that an output is a
+    value, and those near 0 show what their row's step and middle were rounded by.  (s c + b from s and b in fp16 is off by up to 2 x 2^-11.)"""
+    n, count, g = 512, 100, torch.Generator().manual_seed(21)
+    for tokens in (4 * torch.arange(count), n - count + torch.arange(count)):      # in tiles that all rows see, and in those that they do not
+        b = Batch(fmt, hd, 2, 2, [n], [count], seed=21)
+        wide = 1 + 0.03 * torch.rand(2, n, 2, 1, generator=g)
+        v = torch.rand(n, 2, hd, generator=g) * 0.1 - 0.05
+        v[..., :1], v[..., 1:2] = -wide[0], wide[1]
+        replace(b, 0, range(n), v=v)
+        one_key_a_query(b, 0, tokens, 22)
+        check(b, *run(b))
