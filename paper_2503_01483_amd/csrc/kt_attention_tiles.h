@@ -14,9 +14,10 @@
 // in fp32 as in kt_attention.h; the values are expanded on the way, in fp16: a row s c + b is scaled by a power of two per
 // tile, found from the rows' {s, b}, so that its largest value is just below one, and computed in fp16 as s (c - middle) + (b + s middle): the roundings
 // of both parts and of the sum are 1.5 x 2^-11 of that largest value together (uncentred, s c is off by up to 2^-11 of the row's whole width
-// more; bf16 would have 2^-8, little more than the codes of 8 bits).  The exponent is carried along with O like the running maximum.  The maximum is raised only
-// once a score passes it by 2^8 (p stays below 256 in either type).  In fp16 p goes in times 2^7: what it cuts off where p is small then is
-// 2^-31 of the largest p at most, and a million tokens of it do not show in a result.
+// more; bf16 would have 2^-8, little more than the codes of 8 bits).  A row has two running maxima, of the
+// scores for its sum of p and of score and exponent together for O, so that large values of little weight leave the others their bits.  They are raised only
+// once they are passed by 2^8 (p, and p times the power of two, stay below 256).  In fp16 p goes in times 2^7: it is rounded to 2^-31 of the row's largest
+// p |v| at worst, and a million tokens of it do not show in a result.
 //
 // All key tiles of all row tiles form one list, heads outermost; each workgroup takes an equal piece, neighbouring pieces on one XCD, whose
 // L2 then holds the keys of few heads.  Segments that are cut are joined by a second launch.
@@ -193,8 +194,8 @@ struct TileLoader {
     }
   }
   // Values, expanded, into buffer `at`; returns the exponent (biased by 126) that they are scaled down by, and the tokens whose values are
-  // not finite (as 0).  v_run: exponent of O so far, for a floor.
-  __device__ __forceinline__ int put_values(Shared& sh, int at, int there, int v_run, unsigned long long& odd) const {
+  // not finite (as 0).
+  __device__ __forceinline__ int put_values(Shared& sh, int at, int there, unsigned long long& odd) const {
     const int tid = thread(), lane = tid & 63, wave = uniform(tid >> 6);
     constexpr float top = KV == kKvU4 ? 15.f : 255.f, centre = KV == kKvU4 ? 8.f : 128.f;
     float vs = lane < there ? vp.x : 0.f, vb = lane < there ? vp.y : 0.f;
@@ -202,7 +203,7 @@ struct TileLoader {
     const bool bad = !(most <= kHuge) || vs != vs;
     odd = __ballot(bad);
     if (bad) vs = vb = most = 0.f;
-    const int v_exp = max(min(wave_max((int)(__float_as_uint(most) >> 23)), 252), v_run - 60);
+    const int v_exp = min(wave_max((int)(__float_as_uint(most) >> 23)), 252);
     const float f = __uint_as_float((unsigned)(253 - v_exp) << 23);
     sh.expand[wave][0][lane] = (_Float16)(vs * f);
     sh.expand[wave][1][lane] = (_Float16)(fmaf(centre, vs, vb) * f);
@@ -374,7 +375,7 @@ __global__ __launch_bounds__(64 * WAVES, HD == 256 && WAVES == 4 ? 1 : 2) void a
 #pragma unroll
       for (int e = 0; e < 16; ++e) o[i][e] = 0.f;
     float m = kNone, l = 0.f;  // m: in bits (times c)
-    int v_run = 0, v_exp = 0;  // exponents of O, of the values at hand
+    int v_run = 0, v_exp = 0;  // exponents of O (of this lane's row), of the values at hand
     unsigned long long odd = 0ull;
     Loader ld;
 
@@ -485,7 +486,7 @@ __global__ __launch_bounds__(64 * WAVES, HD == 256 && WAVES == 4 ? 1 : 2) void a
       ld.ask_keys(a.cache.data + now.block);
       ld.ask_values(a.cache.data + now.block);
       ld.put_keys(sh, 0, now.there, c);
-      v_exp = ld.put_values(sh, 0, now.there, v_run, odd);
+      v_exp = ld.put_values(sh, 0, now.there, odd);
     } else {
 #pragma unroll
       for (int i = 0; i < 2 * Loader::STEPS; ++i) copy(now.block, 0, i);
@@ -520,21 +521,28 @@ __global__ __launch_bounds__(64 * WAVES, HD == 256 && WAVES == 4 ? 1 : 2) void a
       for (int i = 0; i < 16; ++i) finish_scores(x, at, i);
       if (masked_of(now)) mask(x, seen_of(now));
       float most = largest(x);
-      int shift = 0;
-      if constexpr (Q16) {
-        if (v_exp > v_run) {
-          const float f = v_run - v_exp > -126 ? __uint_as_float((unsigned)(127 + v_run - v_exp) << 23) : 0.f;
-#pragma unroll
-          for (int i = 0; i < TD; ++i) o[i] *= f;
-          v_run = v_exp;
-        }
-        shift = v_exp - v_run;  // at least -60
-      }
       {
         const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(most), __float_as_uint(most), false, false);
         most = fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1]));
       }
-      if (__any(most > m + 8.f)) {
+      int shift = 0;
+      if constexpr (Q16) {
+        // O is held relative to 2^(m + v_run), the largest p |v| of the row so far, so that a large value of little weight takes no bits off the
+        // others; both parts of it are raised by the row's own scores alone.
+        const float need = most + (float)v_exp;
+        const bool higher = most > m + 8.f, raise = higher || need > m + (float)v_run + 8.f;
+        if (__any(raise)) {
+          const float to = higher ? most : m;
+          const int run = max(v_run - (int)fminf(to - m, 1024.f), (int)ceilf(fmaxf(need - to, -1024.f)));
+          const float shrink = raise ? __builtin_amdgcn_exp2f(m - to + (float)(v_run - run)) : 1.f;
+          l *= higher ? __builtin_amdgcn_exp2f(m - to) : 1.f;
+#pragma unroll
+          for (int i = 0; i < TD; ++i) o[i] *= shrink;
+          m = to;
+          if (raise) v_run = run;
+        }
+        shift = max(v_exp - v_run, -60);  // (p is nothing in fp16 from there on)
+      } else if (__any(most > m + 8.f)) {
         const float raised = fmaxf(m, most), shrink = raised == kNone ? 1.f : __builtin_amdgcn_exp2f(m - raised);
         l *= shrink;
 #pragma unroll
@@ -565,7 +573,7 @@ __global__ __launch_bounds__(64 * WAVES, HD == 256 && WAVES == 4 ? 1 : 2) void a
                           });
       }
       const float all = sum[0] + sum[1];
-      l += Q16 ? all * __uint_as_float((unsigned)(127 - shift) << 23) : all;
+      l += Q16 ? ldexpf(all, -shift) : all;
       if constexpr (!Q16) {
         odd = 0ull;
         if (masked_of(now)) {
@@ -598,7 +606,7 @@ __global__ __launch_bounds__(64 * WAVES, HD == 256 && WAVES == 4 ? 1 : 2) void a
       }
       if constexpr (Q16) {
         ld.put_keys(sh, at ^ 1, next.there, c);
-        v_exp = ld.put_values(sh, at ^ 1, next.there, v_run, odd);
+        v_exp = ld.put_values(sh, at ^ 1, next.there, odd);
       }
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
       if (!Q16 && masked_of(next)) clean(next, at ^ 1);
@@ -608,10 +616,13 @@ __global__ __launch_bounds__(64 * WAVES, HD == 256 && WAVES == 4 ? 1 : 2) void a
 
     l += __shfl_xor(l, 32);
     if constexpr (Q16) {
-      const float f = ldexpf(1.f, v_run - 126 - kUp);
-      l *= 1.f / (1 << kUp);
+      const int over = max(v_run - 200, 0);  // so that sums of the largest values stay in range
+      m += (float)over;
+      l = ldexpf(l, -kUp - over);
 #pragma unroll
-      for (int i = 0; i < TD; ++i) o[i] *= f;
+      for (int i = 0; i < TD; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[i][e] = ldexpf(o[i][e], v_run - 126 - kUp - over);
     }
     const bool whole = !PREFIX && first == 0 && last == tiles;
     if (live) {

@@ -70,3 +70,45 @@ def test_values_of_many_rows_lose_no_more_than_their_bound(fmt, hd):
         replace(b, 0, range(n), v=v)
         one_key_a_query(b, 0, tokens, 22)
         check(b, *run(b))
+
+
+@pytest.mark.parametrize("fmt", FMT, ids=IDS)
+@pytest.mark.parametrize("hd", [64, 128, 256])
+@pytest.mark.parametrize("prefix", [0, 64])
+@pytest.mark.parametrize("group", [3, 65])
+def test_large_values_of_next_to_no_weight_take_no_bits_off_others(fmt, hd, prefix, group):
+    """64 tokens in front have values 2^e times as large and weights of 2^-70 or less: what follows is as exact as without them, in few rows and many.
+    (Lengths and heads for which a workgroup goes through several tiles of a segment in turn.)"""
+    g = torch.Generator().manual_seed(31)
+    heads, lens = 8, [1500, 100, 1500, 1500, 1400, 1500]
+    b = Batch(fmt, hd, heads, group, lens, prefix=prefix, seed=30)
+    b.q[..., 0] = 32
+    for s, t in enumerate(lens):
+        k = torch.randn(t, heads, hd, generator=g)
+        k[..., 0] = 0
+        replace(b, s, range(t), k=k)
+    far = torch.randn(64, heads, hd, generator=g)
+    far[..., 0] = -3.5 * hd ** 0.5                       # scores of -112 and a little: 2^-161
+    for e in (0, 8, 14, 17, 20, 32, 60, 90):
+        for s in [None] if prefix else range(len(lens)):
+            replace(b, s, range(64), k=far, v=torch.randn(64, heads, hd, generator=g) * 2.0 ** e)
+        print(f"2^{e}", end=" ")
+        check(b, *run(b))
+
+
+@pytest.mark.parametrize("fmt", FMT[1:], ids=IDS[1:])
+@pytest.mark.parametrize("lift", [0, 100, -100])
+def test_values_that_grow_and_shrink_along_a_sequence(fmt, lift):
+    """Every tile of 64 tokens has values and scores of another size: values that rise and fall by 2^30, near the ends of the range too."""
+    g = torch.Generator().manual_seed(32)
+    hd, heads, t = 128, 8, 1280
+    b = Batch(fmt, hd, heads, 65, [t] * 8, seed=33)
+    b.q[..., 0] = 8
+    for s in range(len(b.lens)):
+        k, v = torch.randn(t, heads, hd, generator=g), torch.randn(t, heads, hd, generator=g)
+        for tile in range(t // 64):
+            at = slice(64 * tile, 64 * tile + 64)
+            k[at, :, 0] = 30 * (torch.rand(1, generator=g) - 0.5)
+            v[at] *= 2.0 ** (lift + 30 * float(torch.rand(1, generator=g) - 0.5))
+        replace(b, s, range(t), k=k, v=v)
+    check(b, *run(b))
