@@ -11,8 +11,9 @@
 // keys takes a CU 4400 cycles, 2048 of them products and 2300 the LDS's reads for them, at 2.0 to 2.2 GHz; a segment 19000 more, at its ends.
 //
 // bf16 caches go straight from memory to LDS.  Of quantised ones the keys' codes do, as exact bf16 values, and a score becomes s (q . c) + b sum(q)
-// in fp32 as in kt_attention.h; the values are expanded on the way, in fp16: a row s c + b is scaled by a power of two per
-// tile, found from the rows' {s, b}, so that its largest value is just below one, and computed in fp16 as s (c - middle) + (b + s middle): the roundings
+// in fp32 as in kt_attention.h; the values are expanded on the way, in fp16: a row s c + b is scaled by a power of two, one a
+// tile, found from the rows' {s, b}, so that its largest value is just below one (one a token, entering with p, in tiles that some row does not see all of, so
+// that no row depends on what it does not see, and where sizes differ by more than 2^6), and computed in fp16 as s (c - middle) + (b + s middle): the roundings
 // of both parts and of the sum are 1.5 x 2^-11 of that largest value together (uncentred, s c is off by up to 2^-11 of the row's whole width
 // more; bf16 would have 2^-8, little more than the codes of 8 bits).  A row has two running maxima, of the
 // scores for its sum of p and of score and exponent together for O, so that large values of little weight leave the others their bits.  They are raised only
@@ -116,6 +117,7 @@ struct TileShared {
   char values[2][kTile];        // [HD][64]
   float2 par[2][64];            // {step, minimum} of the keys, times the factor of the exponentials
   _Float16 expand[WAVES][2][64];  // steps of the values that are being expanded, and what their middle code stands for
+  float power[2][64];             // exponents of the tokens' values, where each has its own
   unsigned long long odd[2][WAVES];  // bf16: tokens of a masked tile with values that are not finite, those in the pieces of each wave
 };
 
@@ -193,17 +195,35 @@ struct TileLoader {
       }
     }
   }
-  // Values, expanded, into buffer `at`; returns the exponent (biased by 126) that they are scaled down by, and the tokens whose values are
-  // not finite (as 0).
-  __device__ __forceinline__ int put_values(Shared& sh, int at, int there, unsigned long long& odd) const {
+  // The largest value of token `lane`; 0 of one that does not exist or has a value that is not finite (bad).
+  __device__ __forceinline__ float largest_value(int lane, int there, bool& bad) const {
+    constexpr float top = KV == kKvU4 ? 15.f : 255.f;
+    const float vs = lane < there ? vp.x : 0.f, vb = lane < there ? vp.y : 0.f, most = fmaxf(fabsf(vb), fabsf(fmaf(top, vs, vb)));
+    bad = !(most <= kHuge) || vs != vs;
+    return bad ? 0.f : most;
+  }
+  __device__ __forceinline__ static int power_of(float most) { return min((int)(__float_as_uint(most) >> 23), 252); }
+  // Looks at the sizes of the values that were asked for: returns the exponent (biased by 126) that they are to be scaled down by.  each: every token by one of
+  // its own (0 is returned), as asked for, or because a token's is more than 2^6 below the largest.
+  __device__ __forceinline__ int look(int there, bool& each) const {
+    bool bad;
+    const float most = largest_value(thread() & 63, there, bad);
+    const int mine = power_of(most), v_exp = wave_max(mine);
+    each = each || __any(most > 0.f && mine + 6 < v_exp);
+    return each ? 0 : v_exp;
+  }
+  // Values, expanded, into buffer `at`, scaled as `look` has found; odd: the tokens whose values are not finite (as 0).
+  __device__ __forceinline__ void put_values(Shared& sh, int at, int there, int v_exp, bool each, unsigned long long& odd) const {
     const int tid = thread(), lane = tid & 63, wave = uniform(tid >> 6);
-    constexpr float top = KV == kKvU4 ? 15.f : 255.f, centre = KV == kKvU4 ? 8.f : 128.f;
-    float vs = lane < there ? vp.x : 0.f, vb = lane < there ? vp.y : 0.f;
-    float most = fmaxf(fabsf(vb), fabsf(fmaf(top, vs, vb)));
-    const bool bad = !(most <= kHuge) || vs != vs;
+    constexpr float centre = KV == kKvU4 ? 8.f : 128.f;
+    bool bad;
+    const float most = largest_value(lane, there, bad);
     odd = __ballot(bad);
-    if (bad) vs = vb = most = 0.f;
-    const int v_exp = min(wave_max((int)(__float_as_uint(most) >> 23)), 252);
+    const float vs = bad || lane >= there ? 0.f : vp.x, vb = bad || lane >= there ? 0.f : vp.y;
+    if (each) {
+      v_exp = power_of(most);
+      if (wave == 0) sh.power[at][lane] = (float)v_exp;
+    }
     const float f = __uint_as_float((unsigned)(253 - v_exp) << 23);
     sh.expand[wave][0][lane] = (_Float16)(vs * f);
     sh.expand[wave][1][lane] = (_Float16)(fmaf(centre, vs, vb) * f);
@@ -237,7 +257,6 @@ struct TileLoader {
       }
     }
     __builtin_amdgcn_wave_barrier();
-    return v_exp;
   }
 };
 
@@ -376,6 +395,7 @@ __global__ __launch_bounds__(64 * WAVES, HD == 256 && WAVES == 4 ? 1 : 2) void a
       for (int e = 0; e < 16; ++e) o[i][e] = 0.f;
     float m = kNone, l = 0.f;  // m: in bits (times c)
     int v_run = 0, v_exp = 0;  // exponents of O (of this lane's row), of the values at hand
+    bool each = false;         // these have one a token
     unsigned long long odd = 0ull;
     Loader ld;
 
@@ -486,7 +506,9 @@ __global__ __launch_bounds__(64 * WAVES, HD == 256 && WAVES == 4 ? 1 : 2) void a
       ld.ask_keys(a.cache.data + now.block);
       ld.ask_values(a.cache.data + now.block);
       ld.put_keys(sh, 0, now.there, c);
-      v_exp = ld.put_values(sh, 0, now.there, odd);
+      each = masked_of(now);
+      v_exp = ld.look(now.there, each);
+      ld.put_values(sh, 0, now.there, v_exp, each, odd);
     } else {
 #pragma unroll
       for (int i = 0; i < 2 * Loader::STEPS; ++i) copy(now.block, 0, i);
@@ -505,6 +527,8 @@ __global__ __launch_bounds__(64 * WAVES, HD == 256 && WAVES == 4 ? 1 : 2) void a
         ld.ask_keys(a.cache.data + next.block);
         ld.ask_values(a.cache.data + next.block);
       }
+      [[maybe_unused]] int v_next = 0;
+      [[maybe_unused]] bool each_next = false;
       f32x16 x[2];
       clear(x);
       {
@@ -514,6 +538,9 @@ __global__ __launch_bounds__(64 * WAVES, HD == 256 && WAVES == 4 ? 1 : 2) void a
                             if constexpr (!Q16) {
                               constexpr int EVERY = KS / Loader::STEPS;
                               if (n % EVERY == 0) copy(next.block, at ^ 1, n / EVERY);
+                            } else if (n == 2 * KS - 6) {  // (behind the loads, not yet in front of the barrier: 284 -> 281 us for the chunk)
+                              each_next = masked_of(next);
+                              v_next = ld.look(next.there, each_next);
                             }
                           });
       }
@@ -521,15 +548,29 @@ __global__ __launch_bounds__(64 * WAVES, HD == 256 && WAVES == 4 ? 1 : 2) void a
       for (int i = 0; i < 16; ++i) finish_scores(x, at, i);
       if (masked_of(now)) mask(x, seen_of(now));
       float most = largest(x);
-      {
-        const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(most), __float_as_uint(most), false, false);
-        most = fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1]));
-      }
+      auto of_halves = [](float v) {
+        const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        return fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1]));
+      };
+      most = of_halves(most);
       int shift = 0;
       if constexpr (Q16) {
         // O is held relative to 2^(m + v_run), the largest p |v| of the row so far, so that a large value of little weight takes no bits off the
         // others; both parts of it are raised by the row's own scores alone.
-        const float need = most + (float)v_exp;
+        float need = most + (float)v_exp, alone = 0.f;
+        if (each) {  // p alone for its sum, and with the token's exponent
+          const float* power = &sh.power[at][8 * h];
+          const float base = most == kNone ? 0.f : most;
+          need = kNone;
+#pragma unroll
+          for (int i = 0; i < 32; ++i) {
+            const float s = x[i >> 4][i & 15], with = s + power[32 * (i >> 4) + 16 * (i >> 3 & 1) + (i & 7)];
+            alone += __builtin_amdgcn_exp2f(s - base);
+            need = fmaxf(need, with);
+            x[i >> 4][i & 15] = with;
+          }
+          need = of_halves(need);
+        }
         const bool higher = most > m + 8.f, raise = higher || need > m + (float)v_run + 8.f;
         if (__any(raise)) {
           const float to = higher ? most : m;
@@ -541,7 +582,8 @@ __global__ __launch_bounds__(64 * WAVES, HD == 256 && WAVES == 4 ? 1 : 2) void a
           m = to;
           if (raise) v_run = run;
         }
-        shift = max(v_exp - v_run, -60);  // (p is nothing in fp16 from there on)
+        shift = max(v_exp - v_run, each ? -1000 : -60);  // (p is nothing in fp16 from 2^-60 on)
+        if (each) l += alone * (m == kNone ? 1.f : __builtin_amdgcn_exp2f(most - m + (float)kUp));
       } else if (__any(most > m + 8.f)) {
         const float raised = fmaxf(m, most), shrink = raised == kNone ? 1.f : __builtin_amdgcn_exp2f(m - raised);
         l *= shrink;
@@ -573,7 +615,8 @@ __global__ __launch_bounds__(64 * WAVES, HD == 256 && WAVES == 4 ? 1 : 2) void a
                           });
       }
       const float all = sum[0] + sum[1];
-      l += Q16 ? ldexpf(all, -shift) : all;
+      if constexpr (!Q16) l += all;
+      else if (!each) l += ldexpf(all, -shift);
       if constexpr (!Q16) {
         odd = 0ull;
         if (masked_of(now)) {
@@ -606,7 +649,9 @@ __global__ __launch_bounds__(64 * WAVES, HD == 256 && WAVES == 4 ? 1 : 2) void a
       }
       if constexpr (Q16) {
         ld.put_keys(sh, at ^ 1, next.there, c);
-        v_exp = ld.put_values(sh, at ^ 1, next.there, odd);
+        each = each_next;
+        v_exp = v_next;
+        ld.put_values(sh, at ^ 1, next.there, v_exp, each, odd);
       }
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
       if (!Q16 && masked_of(next)) clean(next, at ^ 1);

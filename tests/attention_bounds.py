@@ -38,7 +38,7 @@ def expected(b, scale=None, max_q=None):
       bf16        p to bf16: 2^-8 of p |v|
       few rows    (their own tokens) p step to 16 bits: 2^-16 of p step (a centred code: up to 8 or 128); codes enter uncentred: fp32 sums of p step (136 + 15) or p step 256
       many rows, and the tokens of a prefix in either
-                  p to fp16: 2^-11 of p |v|, and nothing below 2^-31 of the largest p |v|;  v to 1.5 x 2^-11 of the largest value that the row sees of its 64 tokens,
+                  p to fp16: 2^-11 of p |v|, its exponent, score plus size, up to 512 in fp32: 2^-15; nothing below 2^-31 of the largest p |v|;  v to 1.5 x 2^-11 of the largest value that the row sees of its 64 tokens,
                   or of 2^7 times its token's own largest, whichever is less
     """
     scale = b.hd ** -0.5 if scale is None else scale
@@ -77,7 +77,7 @@ def expected(b, scale=None, max_q=None):
                 each = torch.where(seen, own, torch.zeros(()))                      # [rows, tokens]
                 tiles = torch.zeros(len(rows), int(places.max()) + 1, dtype=torch.float64).scatter_reduce(1, places.expand(len(rows), -1), each, "amax")
                 most = torch.minimum(tiles[:, places], 128 * own)                   # [rows, tokens]
-                off += 2.0 ** -11 * (p * as_many) @ v.abs() + 1.5 * 2.0 ** -11 * (p * most[:, None]).sum(-1)[..., None]
+                off += (2.0 ** -11 + 2.0 ** -15) * (p * as_many) @ v.abs() + 1.5 * 2.0 ** -11 * (p * most[:, None]).sum(-1)[..., None]
                 off += 2.0 ** -31 * ((p * own).amax(-1) * sees[:, None])[..., None]
             out[rows, h * G:(h + 1) * G], lse[rows, h * G:(h + 1) * G] = o, z
             tol[rows, h * G:(h + 1) * G] = off

@@ -112,3 +112,48 @@ def test_values_that_grow_and_shrink_along_a_sequence(fmt, lift):
             v[at] *= 2.0 ** (lift + 30 * float(torch.rand(1, generator=g) - 0.5))
         replace(b, s, range(t), k=k, v=v)
     check(b, *run(b))
+
+
+@pytest.mark.parametrize("fmt", FMT, ids=IDS)
+@pytest.mark.parametrize("hd,group,counts,prefix", [(64, 3, [70, 30], 0), (128, 4, [90, 17], 0), (128, 1, [100, 66], 70), (256, 2, [70, 40], 0), (256, 1, [70, 40], 64),
+                                                    (64, 2, [5, 3], 0), (128, 4, [9, 4], 30), (256, 8, [2, 2], 0)])
+def test_large_values_of_later_tokens_have_no_effect(fmt, hd, group, counts, prefix):
+    """A token in the middle of each chunk has values 2^e times as large: queries in front of it give the same bits, the others are as exact as ever."""
+    b = Batch(fmt, hd, 2, group, [200, 100], counts, prefix=prefix, seed=40)
+    out, lse = run(b)
+    check(b, out, lse)
+    g = torch.Generator().manual_seed(41)
+    for e in (8, 10, 12, 14, 16, 20, 40, 100):
+        print(f"2^{e}", end=" ")
+        for s, (t, n) in enumerate(zip(b.lens, b.counts)):
+            replace(b, s, [t - n + n // 2], v=torch.randn(1, 2, hd, generator=g) * 2.0 ** e)
+        now, lse2 = run(b)
+        for s, n in enumerate(b.counts):
+            rows = slice(b.starts[s], b.starts[s] + n // 2)
+            assert torch.equal(now[rows], out[rows]) and torch.equal(lse2[rows], lse[rows])
+        check(b, now, lse2)
+
+
+@pytest.mark.parametrize("fmt", FMT, ids=IDS)
+@pytest.mark.parametrize("hd", [64, 128, 256])
+@pytest.mark.parametrize("prefix", [0, 200])
+def test_sizes_that_differ_within_64_tokens(fmt, hd, prefix):
+    """Single tokens with values 2^e times as large, or as small, as their neighbours', of next to no weight or of an ordinary one."""
+    g = torch.Generator().manual_seed(42)
+    heads, lens, at = 8, [900, 70, 900, 800], [3, 60, 69]
+    b = Batch(fmt, hd, heads, 65, lens, prefix=prefix, seed=43)
+    b.q[..., 0] = 32
+    for s, t in enumerate(lens):
+        k = torch.randn(t, heads, hd, generator=g)
+        k[..., 0] = 0
+        replace(b, s, range(t), k=k)
+    for weight in (-3.5 * hd ** 0.5, 0.0):
+        far = torch.randn(len(at), heads, hd, generator=g)
+        far[..., 0] = weight
+        for e in (-40, -9, 5, 7, 12, 20, 40, 100):
+            for s in range(len(lens)):
+                replace(b, s, at, k=far, v=torch.randn(len(at), heads, hd, generator=g) * 2.0 ** e)
+            if prefix:
+                replace(b, None, at, k=far, v=torch.randn(len(at), heads, hd, generator=g) * 2.0 ** e)
+            print(f"2^{e}", end=" ")
+            check(b, *run(b))
