@@ -353,7 +353,7 @@ __global__ __launch_bounds__(256, HD == 256 ? 1 : 2) void attend_rows_kernel(Att
       most = quarters_max(most);
       const float mc = most == kNone ? 0.f : most * c;
       if (__any(most > m)) {
-        const float shrink = __builtin_amdgcn_exp2f(fmaf(m, c, -mc));
+        const float shrink = most > m ? __builtin_amdgcn_exp2f(fmaf(m, c, -mc)) : 1.f;  // (1 +- 2^-24 |mc| otherwise: a row's bits go by its own scores)
         l *= shrink;
         low *= shrink;
 #pragma unroll

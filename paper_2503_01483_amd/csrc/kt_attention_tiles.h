@@ -585,11 +585,12 @@ __global__ __launch_bounds__(64 * WAVES, HD == 256 && WAVES == 4 ? 1 : 2) void a
         shift = max(v_exp - v_run, each ? -1000 : -60);  // (p is nothing in fp16 from 2^-60 on)
         if (each) l += alone * (m == kNone ? 1.f : __builtin_amdgcn_exp2f(most - m + (float)kUp));
       } else if (__any(most > m + 8.f)) {
-        const float raised = fmaxf(m, most), shrink = raised == kNone ? 1.f : __builtin_amdgcn_exp2f(m - raised);
+        const bool raise = most > m + 8.f;  // (of a row by its own scores alone)
+        const float shrink = raise ? __builtin_amdgcn_exp2f(m - most) : 1.f;
         l *= shrink;
 #pragma unroll
         for (int i = 0; i < TD; ++i) o[i] *= shrink;
-        m = raised;
+        if (raise) m = most;
       }
       const float mb = (m == kNone ? 0.f : m) - (float)(shift + kUp);
       frag pf[4];

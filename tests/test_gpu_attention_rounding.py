@@ -157,3 +157,23 @@ def test_sizes_that_differ_within_64_tokens(fmt, hd, prefix):
                 replace(b, None, at, k=far, v=torch.randn(len(at), heads, hd, generator=g) * 2.0 ** e)
             print(f"2^{e}", end=" ")
             check(b, *run(b))
+
+
+@pytest.mark.parametrize("fmt", FMT, ids=IDS)
+@pytest.mark.parametrize("hd,group,counts", [(64, 1, 70), (128, 2, 70), (256, 1, 70), (64, 2, 8), (128, 4, 4), (128, 1, 16), (256, 2, 7)])
+def test_keys_of_later_tokens_have_no_effect(fmt, hd, group, counts):
+    """Later tokens that outweigh all others: queries in front of them give the same bits, also where they share a wave with queries that see them and
+    a workgroup goes through several tiles in turn."""
+    lens = [1500, 1480, 1500, 1300, 1490, 1500, 1500, 1410]
+    b = Batch(fmt, hd, 8, group, lens, [counts] * len(lens), seed=50)
+    out, lse = run(b)
+    g = torch.Generator().manual_seed(51)
+    for size in (3.0, 30.0, 1000.0):
+        for s, t in enumerate(lens):
+            n = counts // 4
+            replace(b, s, range(t - n, t), k=torch.randn(n, 8, hd, generator=g) * size)
+        now, lse2 = run(b)
+        for s in range(len(lens)):
+            rows = slice(b.starts[s], b.starts[s] + counts - counts // 4)
+            assert torch.equal(now[rows], out[rows]), f"{int((now[rows] != out[rows]).sum())} values"
+            assert torch.equal(lse2[rows], lse[rows])
