@@ -379,7 +379,7 @@ kt_status kt_fuse_rotation(const float* W, int64_t ldw, const float* R, int64_t 
  *  codes    [n][ldc] bytes or NULL, 8-byte aligned, ldc a multiple of 8.   scales [n] fp32 or NULL.
  *  d        a multiple of 8 up to 32768, rows 16-byte aligned.  1 <= n < 2^31.
  * A row whose t is below the smallest normal number has codes and scale 0.  A row with a value of h or u that is not finite, or
- * with a sum of squares beyond fp32, has codes 0 and scale NaN.  No workspace.
+ * with a sum of squares beyond fp32, has codes 0 and scale NaN (KT_Q_NONE: Y is NaN if the sum of squares is not finite).  No workspace.
  */
 kt_status kt_add_rmsnorm_quant(const void* X, int64_t ldx, const void* res, int64_t ldres, const void* gain, int64_t n,
                                int64_t d, kt_dtype dtype, kt_dtype gain_dtype, float eps, float clip_ratio,

@@ -94,7 +94,7 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void add_rmsnorm_quant_kerne
   float r = 0.f, scale = 0.f;
   if (t >= kTiny) r = 1.f / t, scale = t * rstd;
   if (!finite) scale = __builtin_nanf("");
-  if constexpr (FORMAT == kFormatNone) scale = rstd;
+  if constexpr (FORMAT == kFormatNone) scale = sum <= kHuge ? rstd : __builtin_nanf("");  // (1 / inf would pass for a row of zeros)
   if (FORMAT != kFormatNone && a.scales && lane == 0) a.scales[row] = scale;
 #pragma unroll
   for (int c = 0; c < CH; ++c) {
