@@ -398,30 +398,46 @@ def kt_add_rmsnorm_quant(X, *, res=None, gain=None, eps=1e-6, clip_ratio=1.0, fo
 
 
 class KVCache:
-    """A paged key / value cache: its shape, and `data`, a uint8 tensor of as many bytes (allocated here unless given)."""
+    """A paged key / value cache: its shape, which does not change, and `data`, a uint8 tensor of as many bytes (allocated here unless
+    given; another one can be put in its place)."""
 
     def __init__(self, n_pages, page_size, n_heads, head_dim, format, *, data=None, device="cuda"):
-        self.n_pages, self.page_size, self.n_heads, self.head_dim, self.format = n_pages, page_size, n_heads, head_dim, format
         self.desc = _CacheDesc(None, n_pages, page_size, n_heads, head_dim, format)
-        nbytes = lib().kt_kv_cache_bytes(ctypes.byref(self.desc))
-        if nbytes == 0:
-            raise KtError(2, kt_last_error() or "bad cache sizes")
-        if data is None:
-            data = torch.empty(nbytes, dtype=torch.uint8, device=device)
-        if data.dtype != torch.uint8 or not data.is_contiguous() or data.numel() != nbytes:
-            raise ValueError(f"data: {nbytes} contiguous bytes (uint8) needed, got {data.dtype} {tuple(data.shape)}")
-        self.data = data
-        self.desc.data = data.data_ptr()
         self.ref = ctypes.byref(self.desc)
+        self.nbytes = lib().kt_kv_cache_bytes(self.ref)
+        if self.nbytes == 0:
+            raise KtError(2, kt_last_error() or "bad cache sizes")
+        self.data = torch.empty(self.nbytes, dtype=torch.uint8, device=device) if data is None else data
+
+    # the sizes that a call checks its operands against are those that the kernels go by
+    n_pages, page_size, n_heads, head_dim, format = (property(lambda self, name=name: getattr(self.desc, name))
+                                                     for name in ("n_pages", "page_size", "n_heads", "head_dim", "format"))
+
+    @property
+    def data(self):
+        return self._data
+
+    @data.setter
+    def data(self, data):
+        if data.dtype != torch.uint8 or not data.is_contiguous() or data.numel() != self.nbytes:
+            raise ValueError(f"data: {self.nbytes} contiguous bytes (uint8) needed, got {data.dtype} {tuple(data.shape)}")
+        self._data = data
+
+    def _on(self, dev):
+        """The descriptor for a call on device `dev`, with the address that the data has now."""
+        data = self._data
+        if data.get_device() != dev or data.numel() != self.nbytes or not data.is_contiguous():
+            _refuse("cache", data, dev, torch.uint8, f"of {self.nbytes} bytes, contiguous,")
+        self.desc.data = data.data_ptr()
+        return self.ref
 
 
 def kt_kv_append(cache, K, V, slots, *, Q=None, positions=None, rope=None, interleaved=False, hadamard=False, Q_out=None,
                  stream=None):
     """Rotated, quantised K and V [n][heads][head_dim] into `slots` [n] of the cache; returns the rotated queries (Q_out or new)."""
     dev, dtype, n = _device(K, "K"), K.dtype, K.shape[0]
-    dt, hd, data = _dtype_code(K), cache.head_dim, cache.data
-    _index(data, "cache", dev, torch.uint8, data.shape)
-    ldk, ldv = _heads(K, "K", dev, dtype, n, cache.n_heads, hd), _heads(V, "V", dev, dtype, n, cache.n_heads, hd)
+    dt, hd, heads, ref = _dtype_code(K), cache.head_dim, cache.n_heads, cache._on(dev)
+    ldk, ldv = _heads(K, "K", dev, dtype, n, heads, hd), _heads(V, "V", dev, dtype, n, heads, hd)
     pslots = _index(slots, "slots", dev, torch.int64, (n,))
     hq = ldq = ldqo = n_pos = rot = 0
     pq = pqo = ppos = prope = None
@@ -438,7 +454,7 @@ def kt_kv_append(cache, K, V, slots, *, Q=None, positions=None, rope=None, inter
             raise ValueError("rope: [n_pos, rot_dim] needed, and positions with it")
         ppos, prope = _index(positions, "positions", dev, torch.int32, (n,)), _index(rope, "rope", dev, torch.float32, rope.shape)
         n_pos, rot = rope.shape
-    _check(lib().kt_kv_append(cache.ref, pq, ldq, K.data_ptr(), ldk, V.data_ptr(), ldv, n, hq, dt, pslots, ppos, prope, n_pos, rot,
+    _check(lib().kt_kv_append(ref, pq, ldq, K.data_ptr(), ldk, V.data_ptr(), ldv, n, hq, dt, pslots, ppos, prope, n_pos, rot,
                               bool(interleaved), bool(hadamard), pqo, ldqo, _stream(stream)))
     return Q_out
 
@@ -446,26 +462,26 @@ def kt_kv_append(cache, K, V, slots, *, Q=None, positions=None, rope=None, inter
 def kt_kv_gather(cache, slots, *, K=None, V=None, dtype=torch.bfloat16, stream=None):
     """The values held in `slots` [n]: (K, V) [n][heads][head_dim], those given or, if neither is, new ones of `dtype` (zeros for slots
     outside the cache)."""
-    dev, n, data = _device(slots, "slots"), slots.shape[0], cache.data
+    dev, n, heads, hd = _device(slots, "slots"), slots.shape[0], cache.n_heads, cache.head_dim
     if K is None and V is None:
-        K, V = (torch.zeros(n, cache.n_heads, cache.head_dim, dtype=dtype, device=slots.device) for _ in range(2))
-    _index(data, "cache", dev, torch.uint8, data.shape)
+        K, V = (torch.zeros(n, heads, hd, dtype=dtype, device=slots.device) for _ in range(2))
+    ref = cache._on(dev)
     pslots = _index(slots, "slots", dev, torch.int64, (n,))
     first = K if K is not None else V
     ldk = ldv = 0
     pk = pv = None
     if K is not None:
-        ldk, pk = _heads(K, "K", dev, first.dtype, n, cache.n_heads, cache.head_dim), K.data_ptr()
+        ldk, pk = _heads(K, "K", dev, first.dtype, n, heads, hd), K.data_ptr()
     if V is not None:
-        ldv, pv = _heads(V, "V", dev, first.dtype, n, cache.n_heads, cache.head_dim), V.data_ptr()
-    _check(lib().kt_kv_gather(cache.ref, pslots, n, pk, ldk, pv, ldv, _dtype_code(first), _stream(stream)))
+        ldv, pv = _heads(V, "V", dev, first.dtype, n, heads, hd), V.data_ptr()
+    _check(lib().kt_kv_gather(ref, pslots, n, pk, ldk, pv, ldv, _dtype_code(first), _stream(stream)))
     return K, V
 
 
 def kt_paged_attention(Q, cache, pages, lens, *, q_starts=None, max_q=1, prefix_pages=None, prefix_len=0, scale=None, out=None,
                        lse=None, workspace=None, stream=None):
     """Attention of Q [n_tokens][heads][head_dim] over the cache; returns out (given or new).  scale: 1 / sqrt(head_dim)."""
-    dev, dtype, data = _device(Q, "Q"), Q.dtype, cache.data
+    dev, dtype = _device(Q, "Q"), Q.dtype
     if Q.dim() != 3:
         raise ValueError(f"Q: [n_tokens, heads, head_dim] needed, got {tuple(Q.shape)}")
     n, hq, hd = Q.shape
@@ -474,7 +490,7 @@ def kt_paged_attention(Q, cache, pages, lens, *, q_starts=None, max_q=1, prefix_
     if out is None:     # (rows in no sequence are not written)
         out = (torch.empty if q_starts is None else torch.zeros)(n, hq, hd, dtype=dtype, device=Q.device)
     ws = workspace if workspace is not None else Workspace(Q.device)
-    _index(data, "cache", dev, torch.uint8, data.shape)
+    ref = cache._on(dev)
     n_seq = lens.shape[0]
     ldq, ldo = _heads(Q, "Q", dev, dtype, n, hq, hd), _heads(out, "out", dev, dtype, n, hq, hd)
     plens = _index(lens, "lens", dev, torch.int32, (n_seq,))
@@ -495,7 +511,7 @@ def kt_paged_attention(Q, cache, pages, lens, *, q_starts=None, max_q=1, prefix_
     buf = ws.get(L.kt_paged_attention_bytes(n, hq, hd, prefix_len))
     if buf.get_device() != dev:
         raise ValueError(f"workspace is on {buf.device}: operands have to be on the current device")
-    _check(L.kt_paged_attention(cache.ref, Q.data_ptr(), ldq, _dtype_code(Q), pstarts, plens, ppages, ldp, n_seq, n, max_q, hq, pprefix,
+    _check(L.kt_paged_attention(ref, Q.data_ptr(), ldq, _dtype_code(Q), pstarts, plens, ppages, ldp, n_seq, n, max_q, hq, pprefix,
                                 prefix_len, hd ** -0.5 if scale is None else scale, out.data_ptr(), ldo, plse, buf.data_ptr(), buf.numel(),
                                 _stream(stream)))
     return out
