@@ -434,7 +434,8 @@ class KVCache:
 
 def kt_kv_append(cache, K, V, slots, *, Q=None, positions=None, rope=None, interleaved=False, hadamard=False, Q_out=None,
                  stream=None):
-    """Rotated, quantised K and V [n][heads][head_dim] into `slots` [n] of the cache; returns the rotated queries (Q_out or new)."""
+    """Rotated, quantised K and V [n][heads][head_dim] into `slots` [n] of the cache; returns the rotated queries (Q_out, or new ones, 0 for
+    tokens that are passed over)."""
     dev, dtype, n = _device(K, "K"), K.dtype, K.shape[0]
     dt, hd, heads, ref = _dtype_code(K), cache.head_dim, cache.n_heads, cache._on(dev)
     ldk, ldv = _heads(K, "K", dev, dtype, n, heads, hd), _heads(V, "V", dev, dtype, n, heads, hd)
@@ -443,7 +444,7 @@ def kt_kv_append(cache, K, V, slots, *, Q=None, positions=None, rope=None, inter
     pq = pqo = ppos = prope = None
     if Q is not None:
         if Q_out is None:
-            Q_out = torch.empty(Q.shape, dtype=Q.dtype, device=Q.device)
+            Q_out = torch.zeros(Q.shape, dtype=Q.dtype, device=Q.device)     # (rows of tokens that are passed over are not written)
         hq = Q.numel() // (n * hd) if n else 0
         ldq, ldqo = _heads(Q, "Q", dev, dtype, n, hq, hd), _heads(Q_out, "Q_out", dev, dtype, n, hq, hd)
         pq, pqo = Q.data_ptr(), Q_out.data_ptr()

@@ -24,3 +24,22 @@ def test_rows_without_codes_whose_sum_of_squares_is_not_finite(dt, d):
         h = x[row].to(dt).double()
         want = h / torch.sqrt(h.square().mean() + 1e-6)
         assert bool(((y[row] - want).abs() <= (torch.finfo(dt).eps / 2 + 23 * 2.0 ** -24) * want.abs()).all())
+
+
+@pytest.mark.parametrize("dt", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
+def test_queries_of_a_padded_batch_are_zeros_where_nothing_was_written(dt):
+    """New rows for the queries hold nothing of what the memory held before."""
+    n, heads, hd = 300, 4, 128
+    cache = kt.KVCache(8, 64, 2, hd, kt.KT_KV_U4)
+    q, k, v = (torch.randn(n, h, hd, dtype=dt, device="cuda") for h in (heads, 2, 2))
+    slots = torch.arange(n, device="cuda")
+    slots[100:] = -1
+    slots[50] = 8 * 64
+    rope, pos = torch.ones(64, hd, device="cuda"), torch.arange(n, dtype=torch.int32, device="cuda")
+    for more, written in ((dict(), [i for i in range(100) if i != 50]), (dict(rope=rope, positions=pos), [i for i in range(64) if i != 50])):
+        for _ in range(3):
+            torch.full_like(q, math.nan)            # (freed at once: the next tensor of this size lies there)
+            out = kt.kt_kv_append(cache, k, v, slots, Q=q, **more)
+            keep = torch.zeros(n, dtype=torch.bool, device="cuda")
+            keep[written] = True
+            assert bool((out[~keep] == 0).all()) and bool((out[keep] != 0).any(-1).all())
