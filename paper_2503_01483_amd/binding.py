@@ -479,9 +479,10 @@ def kt_kv_gather(cache, slots, *, K=None, V=None, dtype=torch.bfloat16, stream=N
     return K, V
 
 
-def kt_paged_attention(Q, cache, pages, lens, *, q_starts=None, max_q=1, prefix_pages=None, prefix_len=0, scale=None, out=None,
+def kt_paged_attention(Q, cache, pages, lens, *, q_starts=None, max_q=None, prefix_pages=None, prefix_len=0, scale=None, out=None,
                        lse=None, workspace=None, stream=None):
-    """Attention of Q [n_tokens][heads][head_dim] over the cache; returns out (given or new).  scale: 1 / sqrt(head_dim)."""
+    """Attention of Q [n_tokens][heads][head_dim] over the cache; returns out (given or new).  scale: 1 / sqrt(head_dim).
+    max_q: a bound on the queries of a sequence (rows of a longer one can be left as they were); without one, all of Q's."""
     dev, dtype = _device(Q, "Q"), Q.dtype
     if Q.dim() != 3:
         raise ValueError(f"Q: [n_tokens, heads, head_dim] needed, got {tuple(Q.shape)}")
@@ -493,6 +494,8 @@ def kt_paged_attention(Q, cache, pages, lens, *, q_starts=None, max_q=1, prefix_
     ws = workspace if workspace is not None else Workspace(Q.device)
     ref = cache._on(dev)
     n_seq = lens.shape[0]
+    if max_q is None:
+        max_q = 1 if q_starts is None else n
     ldq, ldo = _heads(Q, "Q", dev, dtype, n, hq, hd), _heads(out, "out", dev, dtype, n, hq, hd)
     plens = _index(lens, "lens", dev, torch.int32, (n_seq,))
     if pages.dim() != 2:

@@ -5,6 +5,7 @@ import pytest
 import torch
 
 import paper_2503_01483_amd as kt
+from serving_util import Batch
 
 pytestmark = pytest.mark.gpu
 
@@ -43,3 +44,15 @@ def test_queries_of_a_padded_batch_are_zeros_where_nothing_was_written(dt):
             keep = torch.zeros(n, dtype=torch.bool, device="cuda")
             keep[written] = True
             assert bool((out[~keep] == 0).all()) and bool((out[keep] != 0).any(-1).all())
+
+
+@pytest.mark.parametrize("fmt", [kt.KT_KV_BF16, kt.KT_KV_U8, kt.KT_KV_U4], ids=["bf16", "u8", "u4"])
+@pytest.mark.parametrize("counts", [[3, 1, 2], [40, 0, 90]])
+def test_all_rows_are_computed_without_a_bound_on_the_queries(fmt, counts):
+    """q_starts without max_q: as if the bound were the number of rows; none is left out."""
+    b = Batch(fmt, 128, 2, 4, [100, 64, 120], counts, seed=60)
+    starts = torch.tensor(b.starts, dtype=torch.int32, device="cuda")
+    lens = torch.tensor(b.lens, dtype=torch.int32, device="cuda")
+    lse = torch.full((b.n, b.hq), 9.0, device="cuda")
+    out = kt.kt_paged_attention(b.q.cuda(), b.cache, b.pages, lens, q_starts=starts, lse=lse)
+    b.check(out, lse)
