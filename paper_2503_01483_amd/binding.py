@@ -156,6 +156,15 @@ def _check(status):
         raise KtError(status, kt_last_error())
 
 
+def _new(make, stream, *args, **kwargs):
+    """What a call makes for a kernel on `stream` (a stream, its handle, or None: the current one), made on that stream: it is filled in front
+    of the kernel, and its memory, once freed, is given to nobody who does not wait for the kernel."""
+    if stream is None:
+        return make(*args, **kwargs)
+    with torch.cuda.stream(stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(stream)):
+        return make(*args, **kwargs)
+
+
 class Workspace:
     """A caller-owned scratch buffer (torch uint8 tensor) that grows on demand."""
 
@@ -189,10 +198,10 @@ def kt_kurtosis_loss_grad(X, R, *, kappa_target=0.0, loss=None, row_kurt=None, d
     backward pass instead of keeping it (same result)."""
     X, R, batch, n, d = _xr_dims(X, R)
     if loss is None:
-        loss = torch.empty(batch, dtype=torch.float32, device=X.device)
+        loss = _new(torch.empty, stream, batch, dtype=torch.float32, device=X.device)
     xdt = _dtype_code(X)
     need = kt_workspace_bytes(KT_OP_LOSS_GRAD_RECOMPUTE if recompute else KT_OP_LOSS_GRAD, batch, n, d, xdt)
-    ws = (workspace or Workspace(X.device)).get(need)
+    ws = _new((workspace or Workspace(X.device)).get, stream, need)
     _check(lib().kt_kurtosis_loss_grad(_ptr(X), X.stride(1), _ptr(R), R.stride(1), batch, n, d, xdt,
                                        _dtype_code(R), float(kappa_target), _ptr(loss),
                                        _ptr(row_kurt), _ptr(dR), _ptr(ws), need if recompute else ws.numel(),
@@ -206,11 +215,11 @@ def kt_pooled_kurtosis_loss_grad(X, R, *, kappa_target=1.8, rms_eps=0.0, loss=No
     recompute: as for kt_kurtosis_loss_grad."""
     X, R, batch, n, d = _xr_dims(X, R)
     if loss is None:
-        loss = torch.empty(batch, dtype=torch.float32, device=X.device)
+        loss = _new(torch.empty, stream, batch, dtype=torch.float32, device=X.device)
     xdt = _dtype_code(X)
     need = kt_workspace_bytes(KT_OP_POOLED_LOSS_GRAD_RECOMPUTE if recompute else KT_OP_POOLED_LOSS_GRAD,
                               batch, n, d, xdt)
-    ws = (workspace or Workspace(X.device)).get(need)
+    ws = _new((workspace or Workspace(X.device)).get, stream, need)
     _check(lib().kt_pooled_kurtosis_loss_grad(_ptr(X), X.stride(1), _ptr(R), R.stride(1), batch, n, d, xdt,
                                               _dtype_code(R), float(kappa_target), float(rms_eps), _ptr(loss),
                                               _ptr(kappa), _ptr(dR), _ptr(ws), need if recompute else ws.numel(),
@@ -225,7 +234,7 @@ def kt_cayley_step(R, dR, lr, *, R_lowp=None, ortho_err=None, info=None, workspa
     assert Rv.is_contiguous() and dR.is_contiguous() and dR.numel() == Rv.numel()
     assert R.dtype == torch.float32 and dR.dtype == torch.float32
     need = kt_workspace_bytes(KT_OP_CAYLEY, batch, 0, d, KT_F32)
-    ws = (workspace or Workspace(R.device)).get(need)
+    ws = _new((workspace or Workspace(R.device)).get, stream, need)
     _check(lib().kt_cayley_step(_ptr(Rv), _ptr(dR), _ptr(R_lowp), batch, d, float(lr), _ptr(ortho_err),
                                 _ptr(info), _ptr(ws), ws.numel(), _stream(stream)))
     return R
@@ -251,7 +260,7 @@ def kt_cayley_adam_step(R, dR, M, v, step, lr, *, beta1=0.9, beta2=0.99, eps=1e-
     assert dR.numel() == Rv.numel() and M.numel() == Rv.numel() and v.numel() == batch
     assert R.dtype == dR.dtype == M.dtype == v.dtype == torch.float32
     need = kt_workspace_bytes(KT_OP_CAYLEY, batch, 0, d, KT_F32)
-    ws = (workspace or Workspace(R.device)).get(need)
+    ws = _new((workspace or Workspace(R.device)).get, stream, need)
     _check(lib().kt_cayley_adam_step(_ptr(Rv), _ptr(dR), _ptr(M), _ptr(v), int(step), _ptr(R_lowp), batch, d,
                                      float(lr), float(beta1), float(beta2), float(eps), float(q),
                                      _ptr(ortho_err), _ptr(info), _ptr(scalars), _ptr(ws), ws.numel(),
@@ -264,7 +273,7 @@ def kt_rotate_fakequant_int4(X, R, *, clip_ratio=1.0, scales_in=None, scales_out
     X, R, batch, n, d = _xr_dims(X, R)
     xdt = _dtype_code(X)
     need = kt_workspace_bytes(KT_OP_FAKEQUANT, batch, n, d, xdt)
-    ws = (workspace or Workspace(X.device)).get(need)
+    ws = _new((workspace or Workspace(X.device)).get, stream, need)
     _check(lib().kt_rotate_fakequant_int4(_ptr(X), X.stride(1), _ptr(R), R.stride(1), batch, n, d, xdt,
                                           _dtype_code(R), float(clip_ratio), _ptr(scales_in),
                                           _ptr(scales_out), _ptr(codes), _ptr(err), _ptr(ws),
@@ -276,7 +285,7 @@ def kt_rotate_quant_metrics(X, R, *, quantile=0.98, Y=None, amax=None, threshold
     X, R, batch, n, d = _xr_dims(X, R)
     xdt = _dtype_code(X)
     need = kt_workspace_bytes(KT_OP_QUANT_METRICS, batch, n, d, xdt)
-    ws = (workspace or Workspace(X.device)).get(need)
+    ws = _new((workspace or Workspace(X.device)).get, stream, need)
     _check(lib().kt_rotate_quant_metrics(_ptr(X), X.stride(1), _ptr(R), R.stride(1), batch, n, d, xdt,
                                          _dtype_code(R), float(quantile), _ptr(Y), _ptr(amax), _ptr(threshold),
                                          _ptr(err_sym), _ptr(err_asym), _ptr(success), _ptr(ws), ws.numel(),
@@ -287,7 +296,7 @@ def kt_hadamard_rows(X, *, signs=None, out=None, stream=None):
     """Y = (X * signs) H_d / sqrt(d) on the rows of X [n][d] (fp32 or bf16); returns Y (out or new)."""
     assert X.dim() == 2 and X.stride(1) == 1
     n, d = X.shape
-    Y = torch.empty_like(X) if out is None else out
+    Y = _new(torch.empty_like, stream, X) if out is None else out
     assert Y.shape == X.shape and Y.dtype == X.dtype and Y.stride(1) == 1
     if signs is not None:
         assert signs.dtype == torch.int8 and signs.numel() == d and signs.is_contiguous()
@@ -301,9 +310,9 @@ def kt_fuse_rotation(W, R, side, *, out=None, workspace=None, stream=None):
     d = R.shape[-1]
     k = W.shape[0] if side == 0 else W.shape[1]
     assert W.dtype == R.dtype == torch.float32 and W.stride(1) == 1 and R.stride(-1) == 1 and R.dim() == 2
-    out = torch.empty_like(W) if out is None else out
+    out = _new(torch.empty_like, stream, W) if out is None else out
     need = kt_workspace_bytes(KT_OP_FUSE_ROTATION, 1, k, d, KT_F32)
-    ws = (workspace or Workspace(W.device)).get(need)
+    ws = _new((workspace or Workspace(W.device)).get, stream, need)
     _check(lib().kt_fuse_rotation(_ptr(W), W.stride(0), _ptr(R), R.stride(0), _ptr(out), out.stride(0), k, d,
                                   int(side), _ptr(ws), ws.numel(), _stream(stream)))
     return out
@@ -312,10 +321,10 @@ def kt_fuse_rotation(W, R, side, *, out=None, workspace=None, stream=None):
 def kt_quant_sensitivity(Y, alphas, *, bits=4, workspace=None, stream=None):
     """Returns (out [2] = {s_opt, MSE(s_opt)}, gamma [len(alphas)]) as device tensors."""
     assert Y.dtype == torch.float32 and Y.is_contiguous() and alphas.dtype == torch.float32
-    out = torch.empty(2, dtype=torch.float32, device=Y.device)
-    gamma = torch.empty(alphas.numel(), dtype=torch.float32, device=Y.device)
+    out = _new(torch.empty, stream, 2, dtype=torch.float32, device=Y.device)
+    gamma = _new(torch.empty, stream, alphas.numel(), dtype=torch.float32, device=Y.device)
     need = kt_workspace_bytes(KT_OP_SENSITIVITY, 1, 1, 128, KT_F32)
-    ws = (workspace or Workspace(Y.device)).get(need)
+    ws = _new((workspace or Workspace(Y.device)).get, stream, need)
     _check(lib().kt_quant_sensitivity(_ptr(Y), Y.numel(), int(bits), _ptr(alphas), alphas.numel(), _ptr(out),
                                       _ptr(gamma), _ptr(ws), ws.numel(), _stream(stream)))
     return out, gamma
@@ -444,7 +453,7 @@ def kt_kv_append(cache, K, V, slots, *, Q=None, positions=None, rope=None, inter
     pq = pqo = ppos = prope = None
     if Q is not None:
         if Q_out is None:
-            Q_out = torch.zeros(Q.shape, dtype=Q.dtype, device=Q.device)     # (rows of tokens that are passed over are not written)
+            Q_out = _new(torch.zeros, stream, Q.shape, dtype=Q.dtype, device=Q.device)     # (rows of tokens that are passed over are not written)
         hq = Q.numel() // (n * hd) if n else 0
         ldq, ldqo = _heads(Q, "Q", dev, dtype, n, hq, hd), _heads(Q_out, "Q_out", dev, dtype, n, hq, hd)
         pq, pqo = Q.data_ptr(), Q_out.data_ptr()
@@ -465,7 +474,7 @@ def kt_kv_gather(cache, slots, *, K=None, V=None, dtype=torch.bfloat16, stream=N
     outside the cache)."""
     dev, n, heads, hd = _device(slots, "slots"), slots.shape[0], cache.n_heads, cache.head_dim
     if K is None and V is None:
-        K, V = (torch.zeros(n, heads, hd, dtype=dtype, device=slots.device) for _ in range(2))
+        K, V = (_new(torch.zeros, stream, n, heads, hd, dtype=dtype, device=slots.device) for _ in range(2))
     ref = cache._on(dev)
     pslots = _index(slots, "slots", dev, torch.int64, (n,))
     first = K if K is not None else V
@@ -490,7 +499,7 @@ def kt_paged_attention(Q, cache, pages, lens, *, q_starts=None, max_q=None, pref
     if hd != cache.head_dim:
         raise ValueError(f"Q: heads of {hd} features, {cache.head_dim} in the cache")
     if out is None:     # (rows in no sequence are not written)
-        out = (torch.empty if q_starts is None else torch.zeros)(n, hq, hd, dtype=dtype, device=Q.device)
+        out = _new(torch.empty if q_starts is None else torch.zeros, stream, n, hq, hd, dtype=dtype, device=Q.device)
     ws = workspace if workspace is not None else Workspace(Q.device)
     ref = cache._on(dev)
     n_seq = lens.shape[0]
@@ -512,7 +521,7 @@ def kt_paged_attention(Q, cache, pages, lens, *, q_starts=None, max_q=None, pref
     if lse is not None:
         plse = _index(lse, "lse", dev, torch.float32, (n, hq))
     L = lib()
-    buf = ws.get(L.kt_paged_attention_bytes(n, hq, hd, prefix_len))
+    buf = _new(ws.get, stream, L.kt_paged_attention_bytes(n, hq, hd, prefix_len))
     if buf.get_device() != dev:
         raise ValueError(f"workspace is on {buf.device}: operands have to be on the current device")
     _check(L.kt_paged_attention(ref, Q.data_ptr(), ldq, _dtype_code(Q), pstarts, plens, ppages, ldp, n_seq, n, max_q, hq, pprefix,

@@ -56,3 +56,72 @@ def test_all_rows_are_computed_without_a_bound_on_the_queries(fmt, counts):
     lse = torch.full((b.n, b.hq), 9.0, device="cuda")
     out = kt.kt_paged_attention(b.q.cuda(), b.cache, b.pages, lens, q_starts=starts, lse=lse)
     b.check(out, lse)
+
+
+def _busy():
+    """Keeps the current stream busy for some milliseconds."""
+    a = torch.ones(4096, 4096, device="cuda")
+    for _ in range(20):
+        a = a @ a * 2.0 ** -12
+    return a
+
+
+@pytest.mark.parametrize("handle", [False, True], ids=["stream", "handle"])
+def test_a_stream_handed_in_orders_what_the_call_makes_for_itself(handle):
+    """Rows that the binding zeroes are zeroed in front of the kernel, on its stream, also while the current one is busy."""
+    n, heads, hd = 200, 2, 128
+    cache = kt.KVCache(4, 64, heads, hd, kt.KT_KV_U8)
+    q, k, v = (torch.randn(n, h, hd, dtype=torch.bfloat16, device="cuda") for h in (4, heads, heads))
+    slots = torch.arange(n, device="cuda")
+    want_q = kt.kt_kv_append(cache, k, v, slots, Q=q, hadamard=True)
+    want = kt.kt_kv_gather(cache, slots)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    stream = side.cuda_stream if handle else side
+    for _ in range(3):
+        a = _busy()
+        K, V = kt.kt_kv_gather(cache, slots, stream=stream)
+        qo = kt.kt_kv_append(cache, k, v, slots, Q=q, hadamard=True, stream=stream)
+        torch.cuda.synchronize()
+        assert torch.equal(K, want[0]) and torch.equal(V, want[1]) and torch.equal(qo, want_q)
+        del a
+
+
+def test_a_workspace_made_for_another_stream_stays_its_own(monkeypatch):
+    """Attention on a stream that is handed in: outputs and scratch come from that stream's memory, so that nothing of the current stream takes it
+    while the kernels run.  (Where tensors are made is looked at: nothing is run into a used workspace.)"""
+    b = Batch(kt.KT_KV_U4, 128, 2, 4, [300, 200], [80, 70], seed=61)
+    want = b.call()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    made = []
+    for name in ("empty", "zeros"):
+        plain = getattr(torch, name)
+        monkeypatch.setattr(torch, name, lambda *a, plain=plain, **kw: made.append(torch.cuda.current_stream().cuda_stream) or plain(*a, **kw))
+    lens, starts = torch.tensor(b.lens, dtype=torch.int32).cuda(), torch.tensor(b.starts, dtype=torch.int32).cuda()
+    q = b.q.cuda()
+    torch.cuda.synchronize()
+    out = kt.kt_paged_attention(q, b.cache, b.pages, lens, q_starts=starts, max_q=80, stream=side)
+    assert len(made) == 2 and all(s == side.cuda_stream for s in made) and torch.cuda.current_stream() != side
+    side.synchronize()
+    assert torch.equal(out, want)
+    # a workspace of the caller's grows there too
+    ws = kt.Workspace()
+    del made[:]
+    assert torch.equal(kt.kt_paged_attention(q, b.cache, b.pages, lens, q_starts=starts, max_q=80, out=out, workspace=ws, stream=side.cuda_stream), out)
+    side.synchronize()
+    assert made == [side.cuda_stream] and torch.equal(out, want)
+
+
+def test_other_calls_on_a_stream_that_is_handed_in():
+    """The rotation's calls make their outputs and scratch on that stream too."""
+    x, r = torch.randn(1, 700, 512, device="cuda").bfloat16(), torch.eye(512, device="cuda")[None]
+    want, had = kt.kt_kurtosis_loss_grad(x, r), kt.kt_hadamard_rows(x[0])
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    for stream in (side, side.cuda_stream, torch.cuda.current_stream(), 0):
+        a = _busy()
+        loss, rows = kt.kt_kurtosis_loss_grad(x, r, stream=stream), kt.kt_hadamard_rows(x[0], stream=stream)
+        torch.cuda.synchronize()
+        assert torch.equal(loss, want) and torch.equal(rows, had)
+        del a
