@@ -3,7 +3,8 @@ import pytest
 import torch
 
 import paper_2503_01483_amd as kt
-from attention_bounds import check, replace
+from attention_bounds import check, expected, replace
+import serving_util as su
 from serving_util import Batch
 
 pytestmark = pytest.mark.gpu
@@ -177,3 +178,30 @@ def test_keys_of_later_tokens_have_no_effect(fmt, hd, group, counts):
             rows = slice(b.starts[s], b.starts[s] + counts - counts // 4)
             assert torch.equal(now[rows], out[rows]), f"{int((now[rows] != out[rows]).sum())} values"
             assert torch.equal(lse2[rows], lse[rows])
+
+
+@pytest.mark.parametrize("fmt", FMT[1:], ids=IDS[1:])
+@pytest.mark.parametrize("hd,group", [(64, 3), (128, 4), (128, 1), (256, 2)])
+def test_few_rows_keep_sixteen_bits_of_weight_times_step(fmt, hd, group):
+    """Rows from 0 up, half of their features 0: the part of the centred codes and that of the middle cancel there, and what p step was rounded by is left.
+    One term of 8 bits instead of two (computed here, in 64 bits) would be outside the bound."""
+    b = Batch(fmt, hd, 2, group, [500, 130, 64], [1, 2, 5], seed=70)
+    g = torch.Generator().manual_seed(71)
+    for s, t in enumerate(b.lens):
+        v = torch.rand(t, 2, hd, generator=g) * (1 + torch.rand(t, 2, 1, generator=g))
+        v[..., ::2] = 0
+        replace(b, s, range(t), v=v)
+    out, lse = run(b)
+    check(b, out, lse)
+    _, _, tol, _ = expected(b)
+    worst = 0.0
+    for row in range(b.n):
+        s = next(i for i in range(len(b.lens)) if row < b.starts[i + 1])
+        sees = b.lens[s] - b.counts[s] + row - b.starts[s] + 1
+        for h in range(b.hq):
+            x = b.k[s][:sees, h // group] @ b.q[row, h].double() * hd ** -0.5
+            p = torch.exp(x - x.max())
+            step = b.v[s][:sees, h // group].amax(1) / su.TOP[fmt]
+            lost = ((p * step).to(torch.bfloat16).double() - p * step).sum() * (8 if fmt == kt.KT_KV_U4 else 128) / p.sum()
+            worst = max(worst, float(lost.abs() / tol[row, h, 0]))
+    assert worst > 4, worst
