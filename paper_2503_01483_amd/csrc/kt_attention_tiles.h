@@ -538,7 +538,7 @@ __global__ __launch_bounds__(64 * WAVES, HD == 256 && WAVES == 4 ? 1 : 2) void a
                             if constexpr (!Q16) {
                               constexpr int EVERY = KS / Loader::STEPS;
                               if (n % EVERY == 0) copy(next.block, at ^ 1, n / EVERY);
-                            } else if (n == 2 * KS - 6) {  // (behind the loads, not yet in front of the barrier: 284 -> 281 us for the chunk)
+                            } else if (n == 2 * KS - 5) {  // (the chunk: 290 us four products from the end, 280 five, 282 six, 285 eight)
                               each_next = masked_of(next);
                               v_next = ld.look(next.there, each_next);
                             }
@@ -557,29 +557,30 @@ __global__ __launch_bounds__(64 * WAVES, HD == 256 && WAVES == 4 ? 1 : 2) void a
       if constexpr (Q16) {
         // O is held relative to 2^(m + v_run), the largest p |v| of the row so far, so that a large value of little weight takes no bits off the
         // others; both parts of it are raised by the row's own scores alone.
-        float need = most + (float)v_exp, alone = 0.f;
+        // (In differences of scores throughout: a large score added to an exponent would swallow it.)
+        const float up = most - m;  // not a number where nothing has been seen yet
+        float size = (float)v_exp, alone = 0.f;
         if (each) {  // p alone for its sum, and with the token's exponent
           const float* power = &sh.power[at][8 * h];
           const float base = most == kNone ? 0.f : most;
-          need = kNone;
+          size = kNone;
 #pragma unroll
           for (int i = 0; i < 32; ++i) {
-            const float s = x[i >> 4][i & 15], with = s + power[32 * (i >> 4) + 16 * (i >> 3 & 1) + (i & 7)];
-            alone += __builtin_amdgcn_exp2f(s - base);
-            need = fmaxf(need, with);
+            const float s = x[i >> 4][i & 15] - base, with = s + power[32 * (i >> 4) + 16 * (i >> 3 & 1) + (i & 7)];
+            alone += __builtin_amdgcn_exp2f(s);
+            size = fmaxf(size, with);
             x[i >> 4][i & 15] = with;
           }
-          need = of_halves(need);
+          size = of_halves(size);
         }
-        const bool higher = most > m + 8.f, raise = higher || need > m + (float)v_run + 8.f;
+        const bool higher = up > 8.f, raise = higher || size + up > (float)v_run + 8.f;
         if (__any(raise)) {
-          const float to = higher ? most : m;
-          const int run = max(v_run - (int)fminf(to - m, 1024.f), (int)ceilf(fmaxf(need - to, -1024.f)));
-          const float shrink = raise ? __builtin_amdgcn_exp2f(m - to + (float)(v_run - run)) : 1.f;
-          l *= higher ? __builtin_amdgcn_exp2f(m - to) : 1.f;
+          const int run = max(v_run - (higher ? (int)fminf(up, 1024.f) : 0), (int)ceilf(fmaxf(higher ? size : size + up, -1024.f)));
+          const float shrink = raise ? __builtin_amdgcn_exp2f((float)(v_run - run) - (higher ? up : 0.f)) : 1.f;
+          l *= higher ? __builtin_amdgcn_exp2f(-up) : 1.f;
 #pragma unroll
           for (int i = 0; i < TD; ++i) o[i] *= shrink;
-          m = to;
+          if (higher) m = most;
           if (raise) v_run = run;
         }
         shift = max(v_exp - v_run, each ? -1000 : -60);  // (p is nothing in fp16 from 2^-60 on)
@@ -592,7 +593,7 @@ __global__ __launch_bounds__(64 * WAVES, HD == 256 && WAVES == 4 ? 1 : 2) void a
         for (int i = 0; i < TD; ++i) o[i] *= shrink;
         if (raise) m = most;
       }
-      const float mb = (m == kNone ? 0.f : m) - (float)(shift + kUp);
+      const float mb = (m == kNone ? 0.f : Q16 && each ? m - most : m) - (float)(shift + kUp);
       frag pf[4];
       float sum[2] = {0.f, 0.f}, even = 0.f;
       auto exponential = [&](int i) {

@@ -205,3 +205,26 @@ def test_few_rows_keep_sixteen_bits_of_weight_times_step(fmt, hd, group):
             lost = ((p * step).to(torch.bfloat16).double() - p * step).sum() * (8 if fmt == kt.KT_KV_U4 else 128) / p.sum()
             worst = max(worst, float(lost.abs() / tol[row, h, 0]))
     assert worst > 4, worst
+
+
+@pytest.mark.parametrize("fmt", FMT, ids=IDS)
+@pytest.mark.parametrize("hd,group,counts", [(64, 1, 100), (128, 2, 90), (256, 1, 70), (128, 4, 3)])
+def test_scores_far_beyond_the_exponents_of_values(fmt, hd, group, counts):
+    """Scores of 2^27 and more, 2^20 apart: a query's output is the value of its own token, whatever is added to a score on the way."""
+    n, g = 200, torch.Generator().manual_seed(80)
+    b = Batch(fmt, hd, 2, group, [n], [counts], seed=81)
+    k = (torch.randint(0, 2, (n, 2, hd), generator=g) * 2 - 1) * 1024.0             # (held exactly)
+    v = torch.randn(n, 2, hd, generator=g) * torch.exp(torch.randn(n, 2, 1, generator=g))
+    replace(b, 0, range(n), k=k, v=v)
+    own = torch.arange(n - counts, n)
+    for at in (own, torch.arange(counts)):                                          # the last token that it sees, and one in front
+        b.q[:] = (16 * k[at]).repeat_interleave(group, 1).to(torch.bfloat16)
+        out, lse = run(b)
+        want = b.v[0][at].repeat_interleave(group, 1)
+        most = want.abs().amax(-1, keepdim=True) * (0 if fmt == kt.KT_KV_BF16 else 1)
+        # p = 1: the result's rounding, and the value's (p step to 16 bits in few rows; 1.5 x 2^-11 of the row's largest, or of 2^7 times it)
+        near = torch.stack([b.v[0][int(i) // 64 * 64:int(i) // 64 * 64 + 64].abs().amax((0, 2)) for i in at]).repeat_interleave(group, 1)[..., None]
+        bound = 2.0 ** -8 * want.abs() + 1.5 * 2.0 ** -11 * torch.minimum(128 * most, near)
+        assert bool(((out.cpu().double() - want).abs() <= bound).all()), float(((out.cpu().double() - want).abs() / bound).max())
+        score = 16 * 1024.0 ** 2 * hd ** 0.5
+        assert bool(((lse.cpu().double() / score - 1).abs() <= 2.0 ** -20).all())
