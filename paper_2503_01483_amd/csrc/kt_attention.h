@@ -8,10 +8,10 @@
 // holds the scores of one row and of 16 keys that lie next to each other in its column of V^T: after the exponentials the scores ARE
 // the operand of O^T = V^T P^T.  Nothing goes through LDS but the quantisers' parameters, no wave waits for another.
 // All key tiles of all segments form one list, and every wave takes an equal piece of it, whatever the lengths: a segment that is
-// cut leaves {O, max, sum} of each piece in the workspace, and a second launch puts them together (5 to 8 us).
+// cut leaves {O, max, sum} of each piece in the workspace, and a second launch puts them together (4 to 9 us).
 //
-// Bound by HBM: 64 tokens behind up to 16384, 32 + 2 x 8 heads of 128, 4 bits: 157 us, 4.9 TB/s (a large copy: 4.8); 4 behind 131072, 8 bits: 146 us,
-// 5.6 TB/s.  One token behind 1027: 11 us, a chain of lookups, loads and products by waves of one or two tiles each.
+// Bound by HBM: 64 tokens behind up to 16384, 32 + 2 x 8 heads of 128, 4 bits: 159 us, 4.8 TB/s (a large copy: 4.8); 4 behind 131072, 8 bits: 159 us,
+// 5.2 TB/s.  One token behind 1027: 11 us, a chain of lookups, loads and products by waves of one or two tiles each.
 // More rows than 16 read their keys again, mostly from the caches on the way.
 //
 // Quantised rows are never expanded: k = s c + b gives q . k = s (q . c) + b sum(q), and v = s c + b gives p v = (p s) c + p b, so that the

@@ -199,8 +199,8 @@ __device__ __forceinline__ char* place_of(const KvCache& c, int64_t slot, int he
 // HD / 8 lanes a row of 8 values each.  The first n * chunks workgroups take the queries and keys of a token: rotated, then to q_out or into
 // their pages.  The others take the values of one head and of as many tokens as the workgroup has rows: these cross over to rows by feature in LDS,
 // so that the bytes of neighbouring slots are written together.
-// 8192 tokens of 32 + 2 x 8 heads of 128, rotated twice, to 4 bits: 71 us, 3.2 TB/s, bound by the vector ALU (the bytes
-// alone would take 47); 64 tokens 5.1 us; 1537 of heads of 64, to 8 bits, 9.8 us.  A row takes HD / 8 lanes, so that a lane's loads are 16 bytes and the
+// 8192 tokens of 32 + 2 x 8 heads of 128, rotated twice, to 4 bits: 71 us, 2.6 TB/s, bound by the vector ALU (issuing 98 % of the cycles; the
+// 182 MB alone would take 38); 64 tokens 5.1 us; 1537 of heads of 64, to 8 bits, 10 us.  A row takes HD / 8 lanes, so that a lane's loads are 16 bytes and the
 // exchanges of both rotations stay within a row of 16 lanes (vector ALU, no LDS) up to 128 features.
 template <typename T, int KV, int HD>
 __global__ __launch_bounds__(256) void kv_append_kernel(AppendArgs a) {
@@ -313,8 +313,8 @@ struct GatherArgs {
   int n, chunks;  // workgroups of a token's keys (0: no keys)
 };
 
-// Keys and values of single slots as values: the same workgroups the other way round.  HBM-bound: 8192 tokens of 8 heads of 128, 4 bits, 18.7 us
-// (42 MB, most of it written); 64 tokens 4.7.
+// Keys and values of single slots as values: the same workgroups the other way round.  Bound by waits: 8192 tokens of 8 heads of 128, 4 bits, 18.7 us
+// (43 MB, most of it written: 2.3 TB/s, half of a copy's), the vector ALU 54 % of the cycles; rows of values are read 8 bytes at a time.  64 tokens 4.7.
 template <typename T, int KV, int HD>
 __global__ __launch_bounds__(256) void kv_gather_kernel(GatherArgs a) {
 #pragma clang fp contract(off)

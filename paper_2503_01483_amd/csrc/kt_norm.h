@@ -4,7 +4,7 @@
 // The codes of y with the step clip max|y| / L are those of u with the step t = clip max|u| / L: rstd cancels, so both statistics
 // of a row, sum h^2 and max |u|, come from one pass over registers, and the codes do not depend on how the sum is rounded.
 // A row stays in the registers of its threads, so that memory is read and written once: HBM-bound.  16384 rows of 4096, bf16, residual in
-// and out, 4-bit codes as values: 98 us, 5.5 TB/s.  Small calls are bound by the launch: one row of 2048 takes 3.0 us, 193 of 4096 4.8.
+// and out, 4-bit codes as values: 99 us, 5.4 TB/s.  Small calls are bound by the launch: one row of 2048 takes 3.0 us, 193 of 4096 4.8.
 // The arithmetic of the codes is part of the interface (fp32, one rounding an operation): contraction is off.
 #pragma once
 #include "kt_serve_util.h"

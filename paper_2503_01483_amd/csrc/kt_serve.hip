@@ -95,7 +95,7 @@ static KvCache device_cache(const kt_kv_cache* c) {
 }
 
 // ------------------------------------------------------------------ attention -----
-constexpr int64_t kWaveWorkers = (int64_t)kNumCUs * 8;  // waves that share the key tiles of few rows: two workgroups of four a CU, all resident
+constexpr int64_t kWaveWorkers = (int64_t)kNumCUs * 8;  // waves that share the key tiles of few rows: two workgroups of four a CU (heads of 256, bf16 or 8 bits: registers for one, the others follow)
 constexpr int64_t kMaxTokens = (int64_t)1 << 30;         // of a sequence's pages, of a prefix
 constexpr int64_t kMaxSequences = 4096;                 // their tile counts are listed in LDS
 // Waves of a workgroup of kt_attention_tiles.h: two a SIMD; one where a head of 256 features takes all registers.  (Two workgroups of four
