@@ -228,3 +228,25 @@ def test_scores_far_beyond_the_exponents_of_values(fmt, hd, group, counts):
         assert bool(((out.cpu().double() - want).abs() <= bound).all()), float(((out.cpu().double() - want).abs() / bound).max())
         score = 16 * 1024.0 ** 2 * hd ** 0.5
         assert bool(((lse.cpu().double() / score - 1).abs() <= 2.0 ** -20).all())
+
+
+@pytest.mark.parametrize("seed", range(24))
+def test_random_sizes(seed):
+    """Calls of any shape whose tokens' values and keys are of any size."""
+    g = torch.Generator().manual_seed(900 + seed)
+    pick = lambda *v: v[int(torch.randint(0, len(v), (1,), generator=g))]  # noqa: E731
+    whole = lambda lo, hi: int(torch.randint(lo, hi + 1, (1,), generator=g))  # noqa: E731
+    fmt, hd, hkv, group = pick(*FMT), pick(64, 128, 256), pick(1, 2, 8), pick(1, 2, 5, 8, 65)
+    lens = [whole(0, pick(70, 400, 1500)) for _ in range(whole(1, 6))]
+    counts = None if group == 65 else [whole(0, min(t, pick(1, 5, 90))) for t in lens]
+    if counts is not None and sum(counts) == 0:
+        lens[0], counts[0] = max(lens[0], 1), 1
+    prefix, spread, tilt = pick(0, 0, 1, 64, 300), pick(0.0, 1.0, 5.0, 20.0), pick(0.0, 1.0, 10.0)
+    print(f"seed {seed} fmt {fmt} hd {hd} hkv {hkv} group {group} lens {lens} counts {counts} prefix {prefix} spread {spread} tilt {tilt}", flush=True)
+    b = Batch(fmt, hd, hkv, group, lens, counts, prefix=prefix, page=pick(64, 128), seed=seed, pad=whole(0, 3) if counts else 0)
+    for s, t in [*enumerate(lens), (None, prefix)]:
+        if t:
+            size = torch.exp2(spread * torch.randn(t, 1, 1, generator=g))
+            k = torch.randn(t, hkv, hd, generator=g) + tilt * torch.randn(t, hkv, 1, generator=g) / hd ** 0.5
+            replace(b, s, range(t), k=k, v=torch.randn(t, hkv, hd, generator=g) * size)
+    check(b, *run(b))
