@@ -7,8 +7,8 @@
 //
 // A wave's tile takes the matrix cores 1024 cycles (HD = 128) and the vector ALU about as long, most of it exponentials: three quarters of them are
 // worked out beside the products of the values that need the others, the rest beside the other wave of the SIMD.
-// 2 x 8192 tokens, 32 + 2 x 8 heads of 128, bf16: 808 to 825 us, 820 to 835 TFLOP/s (a matrix product of 8192: 1143); 8 x 300 behind 8000, 4 bits: 262 to 288 us,
-// 535 to 590, by the card.  No unit is the bound: of the cycles (at 1.9 to 2.0 GHz, counted) the matrix cores are busy 40 % / 30 %, the vector ALU 63 % in both, the LDS
+// 2 x 8192 tokens, 32 + 2 x 8 heads of 128, bf16: 808 to 838 us, 806 to 835 TFLOP/s (a matrix product of 8192: 1143); 8 x 300 behind 8000, 4 bits: 262 to 292 us,
+// 530 to 590, by the card.  No unit is the bound: of the cycles (at 1.9 to 2.0 GHz, counted) the matrix cores are busy 40 % / 30 %, the vector ALU 63 % in both, the LDS
 // 30 % / 37 %, a third / a quarter of that for bank conflicts.  What is missing is overlap: quantised tiles are expanded between the last product and
 // the barrier, by all waves at once, and a segment's ends cost 19000 cycles.
 //
