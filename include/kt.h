@@ -459,8 +459,9 @@ kt_status kt_kv_gather(const kt_kv_cache* cache, const int64_t* slots, int64_t n
  *  lse      [n_tokens][n_q_heads] fp32 or NULL: log sum_j exp(scale * q . k_j).
  * A query that sees nothing (or whose scores are all -inf) gives 0, and -inf in lse.  What a query does not see has no effect on it,
  * whatever it is (bytes that no token was written to, infinities, NaN); a NaN that it sees makes its output NaN.  Scores, statistics
- * and sums are fp32 (values of 2^119 over the number of tokens and more can make a sum infinite); in front of their product with the values the p_j are rounded to bf16 (KT_KV_BF16), p_j times the value's step to
- * 16 bits (KT_KV_U8 and KT_KV_U4 with max_q * n_q_heads / n_heads <= 64; <= 32 for KT_KV_U8 with head_dim = 256), or p_j to 11 bits,
+ * and sums are fp32 (values of 2^119 over the number of tokens and more can make a sum infinite); in front of their product with the
+ * values the p_j are rounded to bf16 (KT_KV_BF16), p_j times the value's step to 16 bits (KT_KV_U8 and KT_KV_U4 with
+ * max_q * n_q_heads / n_heads <= 64; <= 32 for KT_KV_U8 with head_dim = 256), or p_j to 11 bits,
  * but not beyond 2^-31 of the row's largest p_j max |v_j|, and the values to 1.5 x 2^-11 of the largest of 64 tokens that the row
  * sees, or of 2^7 times their token's own largest if that is less (other calls, and over the prefix in all).  The order of the
  * sums depends on the call's sizes and lengths; the same call gives the same bits.  All index arrays are on the device: the call can
