@@ -477,6 +477,74 @@ kt_status kt_paged_attention(const kt_kv_cache* cache, const void* Q, int64_t ld
 size_t kt_paged_attention_bytes(int64_t n_tokens, int64_t n_q_heads, int64_t head_dim, int64_t prefix_len);
 
 /*
+ * Attention of the tokens of a drafted tree over the cache: kt_paged_attention, where a query sees, of its sequence's tokens, those in front of the
+ * sequence's queries and the queries that its mask names, whatever their order.  All queries are appended first, as in kt_paged_attention.
+ *  tree     [n_tokens][ldt] uint64: bit d % 64 of word d / 64 of a query's row says whether it sees query d of its sequence (usually its ancestors and
+ *           itself).  Bits of queries that the sequence does not have are passed over.  ldt at least ceil(max_q / 64), 8-byte aligned.
+ *  q_starts NULL: one query a sequence, whose bit 0 says whether it sees itself.
+ * A query without tokens in front and with no bit set gives 0, and -inf in lse.  Everything else, the prefix, the workspace (kt_paged_attention_bytes)
+ * and how results are rounded among it, is as kt_paged_attention says.  Queries whose masks name all queries up to their own are chunks; the
+ * order of sums can be another than kt_paged_attention's.
+ */
+kt_status kt_tree_attention(const kt_kv_cache* cache, const void* Q, int64_t ldq, kt_dtype dtype, const int32_t* q_starts,
+                            const int32_t* lens, const int32_t* pages, int64_t ldp, int64_t n_seq, int64_t n_tokens,
+                            int64_t max_q, int64_t n_q_heads, const uint64_t* tree, int64_t ldt, const int32_t* prefix_pages,
+                            int64_t prefix_len, float scale, void* O, int64_t ldo, float* lse, void* workspace,
+                            size_t workspace_bytes, void* stream);
+
+/*
+ * The attention weight that cached tokens receive from new queries, accumulated a token and key head, to evict by:
+ *
+ *   mass_j <- decay * mass_j + sum_r exp(scale * q_r . k_j - lse_r)
+ *
+ * for every token j of a sequence and key / value head, r running over the queries of that sequence that see j (those in front of it do not) and over
+ * the query heads that read the head.  A token that is itself one of the queries starts from 0: mass needs no initialisation where every
+ * token has been a query once, nor with decay = 0, which does not read it.
+ *  mass     [n_pages][n_heads][page_size] fp32, read and written: token t of a sequence has the place that it has in the cache's pages.  Of
+ *           places that no sequence's tokens lie in nothing is read or written.  A page that several sequences name gets the sum of one of them.
+ *  lse      [n_tokens][n_q_heads] fp32, as kt_paged_attention writes it (with a prefix: over both; the prefix's own tokens get no mass here).  Rows whose
+ *           lse is not finite add nothing.
+ *  max_q    a bound on the queries of a sequence, by which the launch is laid out; the rows of a longer one are added all the same.
+ * The other arguments are those of kt_paged_attention.  Scores, exponentials and sums are fp32, in a fixed order: scores and lse are off by a few 2^-24 of
+ * sum |q k| scale + |lse|, and so is, relatively, each term.  decay >= 0.  Tokens of a page outside the cache are passed over.  No workspace.
+ */
+kt_status kt_attention_mass(const kt_kv_cache* cache, const void* Q, int64_t ldq, kt_dtype dtype, const int32_t* q_starts,
+                            const int32_t* lens, const int32_t* pages, int64_t ldp, int64_t n_seq, int64_t n_tokens,
+                            int64_t max_q, int64_t n_q_heads, float scale, const float* lse, float decay, float* mass, void* stream);
+
+/*
+ * Which tokens of every sequence and key / value head stay within a budget:  n_kept[i] = min(lens[i], keep[i], ldk)  tokens of sequence i, in
+ * every head the last `recent` ones, then the first `sink` ones, as far as there is room, and of those between them the ones with the largest
+ * mass, of equal ones the lower index (0 and -0 are equal; a NaN, and the mass of a token whose page is outside the cache, is below all others).
+ *  cache    its sizes; `data` is not looked at.        mass  [n_pages][n_heads][page_size] fp32, as kt_attention_mass keeps it.
+ *  keep     [n_seq] int32 (negative: 0).   lens, pages, ldp, n_seq: as in kt_paged_attention.
+ *  kept     [n_seq][n_heads][ldk] int32, written: the tokens that stay, ascending; entries behind n_kept[i] are left as they were.
+ *  n_kept   [n_seq] int32, written; may be `keep` itself, not `lens`.
+ * No workspace.
+ */
+kt_status kt_kv_select(const kt_kv_cache* cache, const float* mass, const int32_t* lens, const int32_t* pages, int64_t ldp,
+                       int64_t n_seq, const int32_t* keep, int64_t sink, int64_t recent, int32_t* kept, int64_t ldk,
+                       int32_t* n_kept, void* stream);
+
+/*
+ * Tokens of the cache moved together: token src[j] of a sequence becomes its token first + j, for j < count, byte for byte (keys stay rotated by the
+ * positions that they were appended with), with its mass where that is given.  For the tokens that kt_kv_select has chosen, and for the accepted
+ * ones of a drafted tree.
+ *  pages    [n_seq][ldp] int32: where sequences are read.   to_pages [n_seq][ldt] int32: where they are written, pages that no sequence of the call
+ *           is read from; or NULL (or `pages` itself, ldt = ldp): in place.
+ *  src      [n_seq][lds] int32, or with per_head [n_seq][n_heads][lds]: indices of tokens in the sequence.  In place they ascend, and src[j] >= first + j; a
+ *           list that does not leaves unspecified tokens in the places that are written.  Into other pages any order, and any index twice.
+ *  count    [n_seq] int32, at most lds (what is above counts as lds, below 0 as 0).   first [n_seq] int32 or NULL (0); a sequence whose first is
+ *           negative is passed over.
+ *  mass     [n_pages][n_heads][page_size] fp32 or NULL.
+ * Tokens whose index is outside of the sequence's pages, or whose page (read or written) is outside the cache, are not moved: what is in their
+ * place stays.  Pages that two sequences name in place hold an unspecified mix of both.  No workspace.
+ */
+kt_status kt_kv_compact(const kt_kv_cache* cache, const int32_t* pages, int64_t ldp, int64_t n_seq, const int32_t* src, int64_t lds,
+                        int32_t per_head, const int32_t* count, const int32_t* first, const int32_t* to_pages, int64_t ldt,
+                        float* mass, void* stream);
+
+/*
  * Measurement aid (not part of the method; off by default).  When enabled, the
  * library brackets its large launches with HIP events on the caller's stream so a
  * benchmark can read per-kernel durations without a profiler attached.  This is the

@@ -17,7 +17,8 @@ KT_KV_BF16, KT_KV_U8, KT_KV_U4 = 0, 1, 2
 EXPORTS = ("kt_version", "kt_last_error", "kt_workspace_bytes", "kt_kurtosis_loss_grad",
            "kt_pooled_kurtosis_loss_grad", "kt_cayley_step", "kt_cayley_adam_step", "kt_rotate_fakequant_int4", "kt_rotate_quant_metrics", "kt_hadamard_rows", "kt_fuse_rotation", "kt_quant_sensitivity", "kt_profile_enable", "kt_profile_read",
            "kt_profile_reset", "kt_cayley_step_static", "kt_build_id", "kt_add_rmsnorm_quant", "kt_kv_cache_bytes", "kt_kv_append",
-           "kt_kv_gather", "kt_paged_attention", "kt_paged_attention_bytes")
+           "kt_kv_gather", "kt_paged_attention", "kt_paged_attention_bytes", "kt_tree_attention", "kt_attention_mass", "kt_kv_select",
+           "kt_kv_compact")
 
 
 class _CacheDesc(ctypes.Structure):
@@ -111,6 +112,14 @@ def lib():
     L.kt_paged_attention.restype = i32
     L.kt_paged_attention.argtypes = [cache, vp, i64, i32, vp, vp, vp, i64, i64, i64, i64, i64, vp, i64, f32, vp, i64, vp, vp, sz, vp]
     L.kt_profile_enable.restype = i32
+    L.kt_tree_attention.argtypes = [cache, vp, i64, i32, vp, vp, vp, i64, i64, i64, i64, i64, vp, i64, vp, i64, f32, vp, i64, vp, vp, sz, vp]
+    L.kt_tree_attention.restype = i32
+    L.kt_attention_mass.argtypes = [cache, vp, i64, i32, vp, vp, vp, i64, i64, i64, i64, i64, f32, vp, f32, vp, vp]
+    L.kt_attention_mass.restype = i32
+    L.kt_kv_select.argtypes = [cache, vp, vp, vp, i64, i64, vp, i64, i64, vp, i64, vp, vp]
+    L.kt_kv_select.restype = i32
+    L.kt_kv_compact.argtypes = [cache, vp, i64, i64, vp, i64, i32, vp, vp, vp, i64, vp, vp]
+    L.kt_kv_compact.restype = i32
     L.kt_profile_enable.argtypes = [i32]
     L.kt_profile_read.restype = i32
     L.kt_profile_read.argtypes = [i32, ctypes.POINTER(ctypes.c_double), ctypes.POINTER(i32)]
@@ -492,12 +501,40 @@ def kt_paged_attention(Q, cache, pages, lens, *, q_starts=None, max_q=None, pref
                        lse=None, workspace=None, stream=None):
     """Attention of Q [n_tokens][heads][head_dim] over the cache; returns out (given or new).  scale: 1 / sqrt(head_dim).
     max_q: a bound on the queries of a sequence (rows of a longer one can be left as they were); without one, all of Q's."""
-    dev, dtype = _device(Q, "Q"), Q.dtype
+    return _attention(Q, cache, pages, lens, None, q_starts, max_q, prefix_pages, prefix_len, scale, out, lse, workspace, stream)
+
+
+def kt_tree_attention(Q, cache, pages, lens, tree, *, q_starts=None, max_q=None, prefix_pages=None, prefix_len=0, scale=None, out=None,
+                      lse=None, workspace=None, stream=None):
+    """kt_paged_attention where a query sees, of its sequence's queries, those whose bit is set in its row of `tree` [n_tokens][words] int64
+    (query d: bit d % 64 of word d / 64).  max_q: without one, as many as all of Q's or the words have bits for."""
+    if tree.dim() != 2:
+        raise ValueError(f"tree: [n_tokens, words] needed, got {tuple(tree.shape)}")
+    if max_q is None and q_starts is not None:
+        max_q = min(Q.shape[0], 64 * tree.shape[1])
+    return _attention(Q, cache, pages, lens, tree, q_starts, max_q, prefix_pages, prefix_len, scale, out, lse, workspace, stream)
+
+
+def _queries(Q, cache, dev):
+    """Sizes of Q [n_tokens][heads][head_dim], its leading dimension."""
     if Q.dim() != 3:
         raise ValueError(f"Q: [n_tokens, heads, head_dim] needed, got {tuple(Q.shape)}")
     n, hq, hd = Q.shape
     if hd != cache.head_dim:
         raise ValueError(f"Q: heads of {hd} features, {cache.head_dim} in the cache")
+    return n, hq, hd, _heads(Q, "Q", dev, Q.dtype, n, hq, hd)
+
+
+def _table(pages, name, dev, n_seq):
+    """Address and width of a table of pages."""
+    if pages.dim() != 2:
+        raise ValueError(f"{name}: [{n_seq}, pages of a sequence] needed, got {tuple(pages.shape)}")
+    return _index(pages, name, dev, torch.int32, (n_seq, pages.shape[1])), pages.shape[1]
+
+
+def _attention(Q, cache, pages, lens, tree, q_starts, max_q, prefix_pages, prefix_len, scale, out, lse, workspace, stream):
+    dev, dtype = _device(Q, "Q"), Q.dtype
+    n, hq, hd, ldq = _queries(Q, cache, dev)
     if out is None:     # (rows in no sequence are not written)
         out = _new(torch.empty if q_starts is None else torch.zeros, stream, n, hq, hd, dtype=dtype, device=Q.device)
     ws = workspace if workspace is not None else Workspace(Q.device)
@@ -505,12 +542,9 @@ def kt_paged_attention(Q, cache, pages, lens, *, q_starts=None, max_q=None, pref
     n_seq = lens.shape[0]
     if max_q is None:
         max_q = 1 if q_starts is None else n
-    ldq, ldo = _heads(Q, "Q", dev, dtype, n, hq, hd), _heads(out, "out", dev, dtype, n, hq, hd)
+    ldo = _heads(out, "out", dev, dtype, n, hq, hd)
     plens = _index(lens, "lens", dev, torch.int32, (n_seq,))
-    if pages.dim() != 2:
-        raise ValueError(f"pages: [{n_seq}, pages of a sequence] needed, got {tuple(pages.shape)}")
-    ldp = pages.shape[1]
-    ppages = _index(pages, "pages", dev, torch.int32, (n_seq, ldp))
+    ppages, ldp = _table(pages, "pages", dev, n_seq)
     pstarts = pprefix = plse = None
     if q_starts is not None:
         pstarts = _index(q_starts, "q_starts", dev, torch.int32, (n_seq + 1,))
@@ -520,14 +554,77 @@ def kt_paged_attention(Q, cache, pages, lens, *, q_starts=None, max_q=None, pref
         pprefix = _index(prefix_pages, "prefix_pages", dev, torch.int32, prefix_pages.shape)
     if lse is not None:
         plse = _index(lse, "lse", dev, torch.float32, (n, hq))
+    masks = () if tree is None else (_index(tree, "tree", dev, torch.int64, (n, tree.shape[1])), tree.shape[1])
     L = lib()
     buf = _new(ws.get, stream, L.kt_paged_attention_bytes(n, hq, hd, prefix_len))
     if buf.get_device() != dev:
         raise ValueError(f"workspace is on {buf.device}: operands have to be on the current device")
-    _check(L.kt_paged_attention(ref, Q.data_ptr(), ldq, _dtype_code(Q), pstarts, plens, ppages, ldp, n_seq, n, max_q, hq, pprefix,
-                                prefix_len, hd ** -0.5 if scale is None else scale, out.data_ptr(), ldo, plse, buf.data_ptr(), buf.numel(),
-                                _stream(stream)))
+    call = L.kt_paged_attention if tree is None else L.kt_tree_attention
+    _check(call(ref, Q.data_ptr(), ldq, _dtype_code(Q), pstarts, plens, ppages, ldp, n_seq, n, max_q, hq, *masks, pprefix, prefix_len,
+                hd ** -0.5 if scale is None else scale, out.data_ptr(), ldo, plse, buf.data_ptr(), buf.numel(), _stream(stream)))
     return out
+
+
+def _mass(mass, cache, dev):
+    return _index(mass, "mass", dev, torch.float32, (cache.n_pages, cache.n_heads, cache.page_size))
+
+
+def kt_attention_mass(Q, cache, pages, lens, lse, mass, *, q_starts=None, max_q=None, scale=None, decay=1.0, stream=None):
+    """Adds to `mass` [n_pages][heads][page_size] fp32 the attention weight that the cache's tokens receive from Q [n_tokens][heads][head_dim], whose
+    lse [n_tokens][heads] attention has written, after a product of what is there with `decay`; returns mass."""
+    dev = _device(Q, "Q")
+    n, hq, hd, ldq = _queries(Q, cache, dev)
+    ref = cache._on(dev)
+    n_seq = lens.shape[0]
+    if max_q is None:
+        max_q = 1 if q_starts is None else n
+    plens = _index(lens, "lens", dev, torch.int32, (n_seq,))
+    ppages, ldp = _table(pages, "pages", dev, n_seq)
+    pstarts = None if q_starts is None else _index(q_starts, "q_starts", dev, torch.int32, (n_seq + 1,))
+    _check(lib().kt_attention_mass(ref, Q.data_ptr(), ldq, _dtype_code(Q), pstarts, plens, ppages, ldp, n_seq, n, max_q, hq,
+                                   hd ** -0.5 if scale is None else scale, _index(lse, "lse", dev, torch.float32, (n, hq)), decay,
+                                   _mass(mass, cache, dev), _stream(stream)))
+    return mass
+
+
+def kt_kv_select(cache, mass, pages, lens, keep, *, sink=0, recent=0, kept=None, n_kept=None, stream=None):
+    """The tokens of every sequence and head that stay: (kept [n_seq][heads][most] int32, n_kept [n_seq] int32), those given or new ones.
+    keep: tokens of each sequence [n_seq] int32 (kept is needed then), or a number for all of them."""
+    dev, n_seq = _device(mass, "mass"), lens.shape[0]
+    plens = _index(lens, "lens", dev, torch.int32, (n_seq,))
+    ppages, ldp = _table(pages, "pages", dev, n_seq)
+    pmass = _mass(mass, cache, dev)
+    if not isinstance(keep, torch.Tensor):
+        most = min(int(keep), ldp * cache.page_size)
+        if most < 1:
+            raise ValueError(f"keep: a positive number needed, got {keep}")
+        keep = _new(torch.full, stream, (n_seq,), most, dtype=torch.int32, device=mass.device)
+        if kept is None:
+            kept = _new(torch.zeros, stream, n_seq, cache.n_heads, most, dtype=torch.int32, device=mass.device)
+    if kept is None or kept.dim() != 3:
+        raise ValueError("kept: [n_seq, heads, most tokens to keep] needed")
+    if n_kept is None:
+        n_kept = _new(torch.empty, stream, n_seq, dtype=torch.int32, device=mass.device)
+    _check(lib().kt_kv_select(cache.ref, pmass, plens, ppages, ldp, n_seq, _index(keep, "keep", dev, torch.int32, (n_seq,)), sink, recent,
+                              _index(kept, "kept", dev, torch.int32, (n_seq, cache.n_heads, kept.shape[2])), kept.shape[2],
+                              _index(n_kept, "n_kept", dev, torch.int32, (n_seq,)), _stream(stream)))
+    return kept, n_kept
+
+
+def kt_kv_compact(cache, pages, src, count, *, first=None, to_pages=None, mass=None, stream=None):
+    """Token src[j] of every sequence becomes its token first + j (first [n_seq] int32: 0 without), j < count [n_seq] int32, in place or in to_pages.
+    src: [n_seq][most] int32, or [n_seq][heads][most] with a list for each head."""
+    dev, n_seq = _device(pages, "pages"), count.shape[0]
+    ref = cache._on(dev)
+    ppages, ldp = _table(pages, "pages", dev, n_seq)
+    if src.dim() not in (2, 3):
+        raise ValueError(f"src: [n_seq, tokens] or [n_seq, heads, tokens] needed, got {tuple(src.shape)}")
+    lds, per_head = src.shape[-1], src.dim() == 3
+    psrc = _index(src, "src", dev, torch.int32, (n_seq, cache.n_heads, lds) if per_head else (n_seq, lds))
+    pto, ldt = (None, 0) if to_pages is None else _table(to_pages, "to_pages", dev, n_seq)
+    _check(lib().kt_kv_compact(ref, ppages, ldp, n_seq, psrc, lds, per_head, _index(count, "count", dev, torch.int32, (n_seq,)),
+                               None if first is None else _index(first, "first", dev, torch.int32, (n_seq,)), pto, ldt,
+                               None if mass is None else _mass(mass, cache, dev), _stream(stream)))
 
 
 def kt_profile_enable(max_records):

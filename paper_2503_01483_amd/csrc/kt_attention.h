@@ -43,7 +43,20 @@ struct AttendArgs {
   int4* cuts;    // [workers] the segment whose first piece a worker has while others have the rest: {first token, first row * 32 + rows, head, pieces or 0}
   float* part;   // pieces of cut segments: O [2 workers][kRows][HD], then {max in bits, sum} [2 workers][kRows]
   float* whole;  // null: whole segments go to out.  Else something is to be joined: O [n_tokens][hq][HD], then {max, sum} [n_tokens][hq]
+  const unsigned long long* tree;  // [n_tokens][ldt] bits: which queries of its sequence a query sees (kernels with TREE; else null)
+  int64_t ldt;
 };
+
+// Which of the `there` tokens of a tile a query of a tree sees, one a bit: those in front of the sequence's queries, and the queries that its row of words
+// names.  behind: the tile's first token less the sequence's first query; a tile has bits of two words.
+__device__ __forceinline__ unsigned long long tree_sees(const AttendArgs& a, int64_t token, int behind, int there) {
+  const unsigned long long all = there >= 64 ? ~0ull : (1ull << there) - 1;
+  if (behind <= -64) return all;
+  const unsigned long long* row = a.tree + token * a.ldt;
+  auto word = [&](int64_t w) { return w < 0 ? ~0ull : w < a.ldt ? row[w] : 0ull; };
+  const int w = behind >> 6, b = behind & 63;
+  return all & (b ? word(w) >> b | word(w + 1) << (64 - b) : word(w));
+}
 
 // First token and number of a sequence's queries, and its tokens in the cache.
 struct Sequence {
@@ -229,7 +242,8 @@ __device__ __forceinline__ unsigned long long any_lane(unsigned long long which)
 }
 
 // The list's order: sequences, in each its heads, in each its row tiles, in each the key tiles.
-template <int KV, int HD>
+// TREE: of its sequence's queries a row sees those that its mask names (tree_sees), not those up to its own.
+template <int KV, int HD, bool TREE>
 __global__ __launch_bounds__(256, HD == 256 ? 1 : 2) void attend_rows_kernel(AttendArgs a) {
   extern __shared__ int cum[];
   __shared__ float4 params[4][64];
@@ -262,7 +276,7 @@ __global__ __launch_bounds__(256, HD == 256 ? 1 : 2) void attend_rows_kernel(Att
     const int in_seq = (row0 + r) / a.group, qh = head * a.group + (row0 + r - in_seq * a.group);
     const bool live = in_seq < q.count;
     const int64_t token = q.first + (live ? in_seq : 0);
-    const int sees = min(max(q.len - q.count + in_seq + 1, 0), q.len), all_see = q.len - q.count + row0 / a.group + 1;
+    const int sees = min(max(q.len - q.count + in_seq + 1, 0), q.len), all_see = q.len - q.count + (TREE ? 0 : row0 / a.group + 1);
     bf16x8 qf[HD / 32];
     float qsum = 0.f;
 #pragma unroll
@@ -340,12 +354,15 @@ __global__ __launch_bounds__(256, HD == 256 ? 1 : 2) void attend_rows_kernel(Att
       if (kEarly && more) t64.load_keys(a.cache.data + block_next, lane);
       const bool masked = there < 64 || tile * 64 + 64 > all_see;
       const int seen = min(max(sees - tile * 64, 0), there);
+      unsigned long long bits = 0ull;  // TREE: of the tile's tokens, those that are seen
+      if (TREE && masked) bits = tree_sees(a, token, tile * 64 - (q.len - q.count), there);
+      auto hidden = [&](int j) { return TREE ? !(bits >> j & 1ull) : j >= seen; };
       if (masked) {
 #pragma unroll
         for (int t = 0; t < 4; ++t)
 #pragma unroll
           for (int i = 0; i < 4; ++i)
-            if (Tile64<KV, HD>::token(t, 4 * g + i) >= seen) x[t][i] = kNone;
+            if (hidden(Tile64<KV, HD>::token(t, 4 * g + i))) x[t][i] = kNone;
       }
       float most = m;
 #pragma unroll
@@ -372,7 +389,7 @@ __global__ __launch_bounds__(256, HD == 256 ? 1 : 2) void attend_rows_kernel(Att
           const int e = 4 * (t & 1) + i, at = KV == kKvU4 ? (e & 4) | (e & 1) << 1 | (e & 2) >> 1 : e;
           if constexpr (KV != kKvBf16) {
             const float vs = vp[t][i >> 1][2 * (i & 1)], vb = vp[t][i >> 1][2 * (i & 1) + 1];
-            const bool off = masked && Tile64<KV, HD>::token(t, 4 * g + i) >= seen;  // parameters of keys that are not seen may be anything
+            const bool off = masked && hidden(Tile64<KV, HD>::token(t, 4 * g + i));  // parameters of keys that are not seen may be anything
             low = off ? low : fmaf(p, fmaf(kCentre, vs, vb), low);
             p = off ? 0.f : p * vs;
             rest[t >> 1][at] = (bf16)(p - (float)(bf16)p);
@@ -398,7 +415,7 @@ __global__ __launch_bounds__(256, HD == 256 ? 1 : 2) void attend_rows_kernel(Att
 #pragma unroll
               for (int e = 0; e < 4; ++e) {
                 const float x = (float)v[(16 * i + e) * kBlockTokens + j];
-                if (j < seen && !(fabsf(x) <= kHuge)) o[i][e] += x;
+                if (!hidden(j) && !(fabsf(x) <= kHuge)) o[i][e] += x;
               }
           }
         }

@@ -62,8 +62,8 @@ __device__ __forceinline__ int64_t first_entry(const AttendArgs& a, int s, int R
 // list, in front of them, so that pieces take equally long.
 constexpr int kSegmentCost = 4;
 
-// The list of row tiles.  One workgroup of 1024.
-template <int R>
+// The list of row tiles.  One workgroup of 1024.  TREE: every row can see all of its sequence's queries.
+template <int R, bool TREE>
 __global__ __launch_bounds__(1024) void plan_tiles_kernel(TileArgs t) {
   __shared__ int wave_sum[16];
   const AttendArgs& a = t.a;
@@ -86,7 +86,7 @@ __global__ __launch_bounds__(1024) void plan_tiles_kernel(TileArgs t) {
       const int64_t rows = (int64_t)q.count * a.group;
       if (rt >= 0 && rt * R < rows) {
         const int last = (int)((min(rows, (rt + 1) * R) - 1) / a.group);
-        const int sees = min(max(q.len - q.count + last + 1, 0), q.len);
+        const int sees = TREE ? q.len : min(max(q.len - q.count + last + 1, 0), q.len);
         mine = kSegmentCost + max(1, prefix_tiles + (int)(((unsigned)sees + 63) >> 6));
       }
     }
@@ -295,8 +295,8 @@ struct TileState {
   int base;       // the sequence's first token in it; negative: of the prefix
 };
 
-// PREFIX: the rows of all tokens over the prefix alone, split over its tiles, to prefix_part; else the list.
-template <int KV, int HD, int WAVES, bool PREFIX>
+// PREFIX: the rows of all tokens over the prefix alone, split over its tiles, to prefix_part; else the list.  TREE: as in kt_attention.h.
+template <int KV, int HD, int WAVES, bool PREFIX, bool TREE>
 __global__ __launch_bounds__(64 * WAVES, HD == 256 && WAVES == 4 ? 1 : 2) void attend_tiles_kernel(TileArgs t) {
   constexpr int R = 32 * WAVES, TD = HD / 32, KS = HD / 16;
   constexpr bool Q16 = KV != kKvBf16;  // quantised: p and the values in fp16
@@ -377,7 +377,7 @@ __global__ __launch_bounds__(64 * WAVES, HD == 256 && WAVES == 4 ? 1 : 2) void a
     const int in_seq = live ? (int)(row / a.group) : 0, qh = head * a.group + (live ? (int)(row - (int64_t)in_seq * a.group) : 0);
     const int64_t token = q.first + in_seq;
     const int sees = min(max(q.len - q.count + in_seq + 1, 0), q.len);                                    // of its own tokens
-    const int all_see = q.len - q.count + 1 + (int)((int64_t)row_tile * R / a.group);                     // what every row of the workgroup sees
+    const int all_see = q.len - q.count + (TREE ? 0 : 1 + (int)((int64_t)row_tile * R / a.group));        // what every row of the workgroup sees
     bf16x8 qf[KS];
     float qsum = 0.f;
 #pragma unroll
@@ -430,6 +430,12 @@ __global__ __launch_bounds__(64 * WAVES, HD == 256 && WAVES == 4 ? 1 : 2) void a
     };
     auto masked_of = [&](const TileState& x) { return x.there < 64 || (x.base >= 0 && x.base + 64 > all_see); };
     auto seen_of = [&](const TileState& x) { return x.base >= 0 ? min(max(sees - x.base, 0), x.there) : x.there; };
+    // ... one a bit
+    auto bits_of = [&](const TileState& x) {
+      if (TREE && x.base >= 0) return tree_sees(a, token, x.base - (q.len - q.count), x.there);
+      const int seen = seen_of(x);
+      return seen >= 64 ? ~0ull : (1ull << seen) - 1;
+    };
     // operands in LDS: the exchange puts n into bits of the address that only an exclusive or reaches.  Where a lane reads is worked out anew for
     // each half tile: kept in registers, it would push others out to memory, and a wait for those is one for the copies under way
     auto key_place = [&] {
@@ -464,12 +470,16 @@ __global__ __launch_bounds__(64 * WAVES, HD == 256 && WAVES == 4 ? 1 : 2) void a
         x[k][e + 1] *= c;
       }
     };
-    auto mask = [&](f32x16(&x)[2], int seen) {
+    auto mask = [&](f32x16(&x)[2], const TileState& s) {
+      const int seen = TREE ? 0 : seen_of(s);
+      const unsigned long long bits = TREE ? bits_of(s) >> (8 * h) : 0ull;
 #pragma unroll
       for (int k = 0; k < 2; ++k)
 #pragma unroll
-        for (int e = 0; e < 16; ++e)
-          if (32 * k + 16 * (e >> 3) + 8 * h + (e & 7) >= seen) x[k][e] = kNone;
+        for (int e = 0; e < 16; ++e) {
+          const int j = 32 * k + 16 * (e >> 3) + (e & 7);
+          if (TREE ? !(bits >> j & 1ull) : j + 8 * h >= seen) x[k][e] = kNone;
+        }
     };
     auto largest = [&](const f32x16(&x)[2]) {
       float most = fmaxf(x[0][0], x[1][0]);
@@ -548,7 +558,7 @@ __global__ __launch_bounds__(64 * WAVES, HD == 256 && WAVES == 4 ? 1 : 2) void a
       }
 #pragma unroll
       for (int i = 0; i < 16; ++i) finish_scores(x, at, i);
-      if (masked_of(now)) mask(x, seen_of(now));
+      if (masked_of(now)) mask(x, now);
       float most = largest(x);
       auto of_halves = [](float v) {
         const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
@@ -631,7 +641,7 @@ __global__ __launch_bounds__(64 * WAVES, HD == 256 && WAVES == 4 ? 1 : 2) void a
       }
       if (odd) {
         const int seen = seen_of(now);
-        const unsigned long long mine = seen >= 64 ? ~0ull : (1ull << seen) - 1;
+        const unsigned long long mine = bits_of(now);
         if constexpr (Q16) {
           const float add = odd & mine ? __builtin_nanf("") : 0.f;
 #pragma unroll
@@ -646,7 +656,7 @@ __global__ __launch_bounds__(64 * WAVES, HD == 256 && WAVES == 4 ? 1 : 2) void a
 #pragma unroll
               for (int e = 0; e < 16; ++e) {
                 const float w = (float)v[(32 * i + (e & 3) + 8 * (e >> 2)) * kBlockTokens + j];
-                if (j < seen && !(fabsf(w) <= kHuge)) o[i][e] += w;
+                if ((TREE ? (mine >> j & 1ull) != 0 : j < seen) && !(fabsf(w) <= kHuge)) o[i][e] += w;
               }
           }
         }
