@@ -89,7 +89,16 @@ kt_status kt_kv_select(const kt_kv_cache* cache, const float* mass, const int32_
     return fail(KT_ERR_BAD_SHAPE, "arrays must be aligned to their type");
   const SelectArgs a{mass, lens, pages, keep, cache->n_pages, ldp, ldk, (int)cache->n_heads, log2_of(cache->page_size),
                      (int)std::min(sink, kMaxTokens), (int)std::min(recent, kMaxTokens), kept, n_kept};
-  kv_select_kernel<<<dim3((unsigned)cache->n_heads, (unsigned)n_seq), 1024, 0, static_cast<hipStream_t>(stream)>>>(a);
+  // as many rows of 64 tokens a wave as the page table has room for
+  auto go = [&](auto per) {
+    kv_select_kernel<decltype(per)::value><<<dim3((unsigned)cache->n_heads, (unsigned)n_seq), 1024, 0, static_cast<hipStream_t>(stream)>>>(a);
+  };
+  using std::integral_constant;
+  const int64_t rows = ceil_div(ldp * cache->page_size, 1024);
+  if (rows <= 2) go(integral_constant<int, 2>{});
+  else if (rows <= 4) go(integral_constant<int, 4>{});
+  else if (rows <= 16) go(integral_constant<int, 16>{});
+  else go(integral_constant<int, 64>{});
   return launch_ok() ? KT_OK : fail(KT_ERR_DEVICE, "select kernel launch failed");
 }
 

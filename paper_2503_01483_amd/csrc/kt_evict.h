@@ -12,61 +12,120 @@ struct SelectArgs {
   int *kept, *n_kept;
 };
 
-// Numbers in the order of the masses: larger is kept before smaller; -0 is 0, a NaN is below all.
+// Numbers in the order of the masses, from 1 on: larger is kept before smaller; -0 is 0, a NaN is below all.
 __device__ __forceinline__ uint32_t mass_order(float m) {
   const uint32_t b = __float_as_uint(m + 0.f);
-  return m != m ? 0u : b >> 31 ? ~b : b | 0x80000000u;
+  return m != m ? 1u : b ^ (uint32_t)((int)b >> 31 | (int)0x80000000u);
 }
 
-// One sequence and head a workgroup of 1024.  Of the tokens between the first `sink` and the last `recent` the k largest stay, the lower index of equal
-// ones: the k-th largest number is found digit by digit (11, 11 and 10 bits, counted in LDS), then every wave counts what stays in its piece of
-// the tokens, and writes it behind that of the waves in front.
+// Sum over the lanes up to this one, by row shifts and broadcasts.
+__device__ __forceinline__ int sum_up_to(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);  // row_shr 1, 2, 4, 8
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);  // row_bcast 15, 31
+  return v + __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);
+}
+
+// How many of a mask's lanes are in front of this one.
+__device__ __forceinline__ uint32_t lanes_below(unsigned long long mask) {
+  return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0u));
+}
+
+// One sequence and head a workgroup of 16 waves.  The n largest tokens stay, the lower index of equal ones, where the first `sink` and the last `recent` count
+// as the largest of all: the n-th largest number is found digit by digit (11, 11 and 10 bits, counted in LDS), then every wave counts what stays in its
+// piece of the tokens, and writes it behind that of the waves in front.
+// A wave has PER neighbouring rows of 64 tokens, whose numbers it keeps in registers: they are read once, all at the same time.  What is longer than 1024 PER tokens
+// goes through in as many parts, read again for every digit.  Digits are counted 8 times side by side, by lane: the top digit of a float is
+// its exponent, which most of a wave's lanes share, and an LDS counter takes its additions one by one.
+// Bound by a compute unit's instructions, and barriers where there are few tokens: 8 heads of 2300 tokens 10 us, 256 of up to 16384 18 us, 16 of up to 65536 33 us
+// (numbers read again for each digit and counted row by row instead: 11, 49, 157).
+template <int PER>
 __global__ __launch_bounds__(1024) void kv_select_kernel(SelectArgs a) {
-  constexpr int kBins = 2048;
-  __shared__ int bins[kBins];
+  constexpr int kBins = 2048, kCopies = 8, PART = 1024 * PER;
+  constexpr uint32_t kStays = 0xffffffffu;  // of a token that stays in any case; 0: of one that there is not
+  __shared__ int bins[kBins * kCopies];
   __shared__ int counts[2][16];
-  __shared__ int found[3];  // bin, numbers above it
-  const int s = blockIdx.y, head = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  __shared__ int found[2];  // bin, numbers above it
+  const int s = blockIdx.y, head = blockIdx.x, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int len = min(max(a.lens[s], 0), (int)(a.ldp << a.log2_page));
   const int n = min(min(max(a.keep[s], 0), len), (int)a.ldk);
-  const int recent = min(a.recent, n), sink = min(a.sink, n - recent);
-  const int first = sink, last = len - recent;  // the tokens to choose from
-  int k = n - recent - sink;
+  const int recent = min(a.recent, n), sink = min(a.sink, n - recent), last = len - recent;
   const int* pages = a.pages + s * a.ldp;
   int* kept = a.kept + ((int64_t)s * a.n_heads + head) * a.ldk;
   if (head == 0 && threadIdx.x == 0) a.n_kept[s] = n;
-  const int page_mask = (1 << a.log2_page) - 1;
-  auto number = [&](int t) {  // (of a page outside the cache: as a NaN's)
-    const int page = pages[t >> a.log2_page];
-    return page < 0 || page >= a.n_pages ? 0u : mass_order(a.mass[(((int64_t)page * a.n_heads + head) << a.log2_page) + (t & page_mask)]);
-  };
-  uint32_t limit = 0xffffffffu;  // stays: above it, and the first `ties` equal to it
-  int ties = 0;
-  if (k > 0 && k < last - first) {
-    uint32_t prefix = 0;
-    int left = k;
+  const int page_mask = (1 << a.log2_page) - 1, parts = (int)(((int64_t)len + PART - 1) / PART);
+  uint32_t v[PER];  // the lane's numbers of a part: tokens part PART + (wave PER + i) 64 + lane
+  auto row = [&](int part, int i) { return part * PART + (wave * PER + i) * 64; };
+  auto load = [&](int part) {
+    // where the rows' masses lie, one a lane
+    static_assert(PER <= 64);
+    const int mine = row(part, 0) + 64 * (lane < PER ? lane : 0);
+    const int page = pages[min(mine, len - 1) >> a.log2_page];
+    const bool there = page >= 0 && page < a.n_pages;
+    const int64_t place = there ? ((((int64_t)page * a.n_heads + head) << a.log2_page) + (mine & page_mask)) * 4 : 0;
+    const unsigned long long not_there = __ballot(!there && mine < len);
 #pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const int64_t at = (int64_t)__builtin_amdgcn_readlane((int)(place >> 32), i) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)place, i);
+      v[i] = reinterpret_cast<const uint32_t*>(reinterpret_cast<const char*>(a.mass) + at)[lane];  // (behind the last token: of its page, and not looked at)
+    }
+    const int row0 = row(part, 0);
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      v[i] = mass_order(__uint_as_float(v[i]));
+      if (row0 + 64 * i < sink || row0 + 64 * i + 64 > last) {
+        const int t = row0 + 64 * i + lane;
+        v[i] = t >= len ? 0u : t < sink || t >= last ? kStays : v[i];
+      }
+    }
+    if (not_there)
+#pragma unroll
+      for (int i = 0; i < PER; ++i)
+        if (not_there >> i & 1ull) v[i] = v[i] == 0u || v[i] == kStays ? v[i] : 1u;
+  };
+
+  uint32_t limit = 0u;  // stays: above it, and the first `ties` equal to it
+  int ties = 0;
+  if (n == 0) return;
+  if (parts == 1) load(0);
+  if (n < len) {
+    uint32_t prefix = 0;
+    int left = n;
+#pragma unroll 1
     for (int pass = 0; pass < 3; ++pass) {
-      constexpr int kShift[3] = {21, 10, 0};
-      const int shift = kShift[pass], width = pass == 2 ? 10 : 11;
-      for (int i = threadIdx.x; i < kBins; i += 1024) bins[i] = 0;
+      const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, width = pass == 2 ? 10 : 11;
+#pragma unroll
+      for (int i = 0; i < kBins * kCopies / 4096; ++i) reinterpret_cast<int4*>(bins)[threadIdx.x + 1024 * i] = int4{0, 0, 0, 0};
       __syncthreads();
-      for (int t = first + threadIdx.x; t < last; t += 1024) {
-        const uint32_t v = number(t);
-        if (pass == 0 || v >> (shift + width) == prefix) atomicAdd(&bins[v >> shift & ((1u << width) - 1)], 1);
+      for (int part = 0; part < parts; ++part) {
+        if (parts > 1) load(part);
+        if (pass == 0) {
+#pragma unroll
+          for (int i = 0; i < PER; ++i) atomicAdd(&bins[(v[i] >> 21) * kCopies + (lane & (kCopies - 1))], 1);
+        } else {
+          const uint32_t from = prefix << (shift + width);
+#pragma unroll
+          for (int i = 0; i < PER; ++i) {
+            const uint32_t x = v[i] - from;
+            if (x >> (shift + width) == 0) atomicAdd(&bins[(x >> shift) * kCopies + (lane & (kCopies - 1))], 1);
+          }
+        }
       }
       __syncthreads();
       // the bin that the left-th from the top is in: two bins a thread, the top ones first
-      const int hi = kBins - 1 - 2 * threadIdx.x, x = bins[hi], y = bins[hi - 1];
-      int upto = x + y;
-#pragma unroll
-      for (int o = 1; o < 64; o *= 2) {
-        const int v = __shfl_up(upto, o);
-        if (lane >= o) upto += v;
-      }
+      const int hi = kBins - 1 - 2 * threadIdx.x;
+      auto count = [&](int bin) {
+        const int4* b = reinterpret_cast<const int4*>(bins + bin * kCopies);
+        return b[0].x + b[0].y + b[0].z + b[0].w + b[1].x + b[1].y + b[1].z + b[1].w;
+      };
+      const int x = count(hi), y = count(hi - 1);
+      int upto = sum_up_to(x + y);
       if (lane == 63) counts[0][wave] = upto;
       __syncthreads();
-      for (int w = 0; w < wave; ++w) upto += counts[0][w];
+#pragma unroll
+      for (int w = 0; w < 16; ++w) upto += w < wave ? counts[0][w] : 0;
       const int above = upto - x - y;
       if (above < left && left <= upto) {
         const bool second = above + x < left;
@@ -79,43 +138,53 @@ __global__ __launch_bounds__(1024) void kv_select_kernel(SelectArgs a) {
     }
     limit = prefix;
     ties = left;
-  } else if (k > 0) {
-    limit = 0u;
-    ties = len;
   }
-  // pieces of whole waves
-  const int piece = ((len + 1023) >> 10) * 64, from = wave * piece, to = min(from + piece, len);
-  auto look = [&](int t, bool& stays, bool& equal) {
-    const bool in = t < to, middle = in && t >= first && t < last && k > 0;
-    const uint32_t v = middle ? number(t) : 0u;
-    stays = in && (!middle ? t < first || t >= last : v > limit);
-    equal = middle && v == limit;
-  };
-  int stay = 0, same = 0;
-  for (int t = from; t < to; t += 64) {
-    bool stays, equal;
-    look(t + lane, stays, equal);
-    stay += __popcll(__ballot(stays));
-    same += __popcll(__ballot(equal));
-  }
-  if (lane == 0) counts[0][wave] = stay, counts[1][wave] = same;
-  __syncthreads();
-  int at = 0, seen = 0;  // kept, equal ones, in front of the wave
-  for (int w = 0; w < wave; ++w) {
-    const int e = counts[1][w];
-    at += counts[0][w] + min(e, max(0, ties - seen));
-    seen += e;
-  }
-  const unsigned long long below = (1ull << lane) - 1;
-  for (int t = from; t < to; t += 64) {
-    bool stays, equal;
-    look(t + lane, stays, equal);
-    const unsigned long long equals = __ballot(equal);
-    stays = stays || (equal && seen + __popcll(equals & below) < ties);
-    const unsigned long long all = __ballot(stays);
-    if (stays) kept[at + __popcll(all & below)] = t + lane;
-    at += __popcll(all);
-    seen += __popcll(equals);
+  int at = 0, seen = 0;  // kept, equal ones, in front of the part, then of the wave
+  for (int part = 0; part < parts; ++part) {
+    if (parts > 1) load(part);
+    int stay = 0, same = 0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {  // (a lane's own: a count of lanes waits for the comparison)
+      stay += v[i] > limit;
+      same += v[i] == limit;
+    }
+    stay = sum_up_to(stay);
+    same = sum_up_to(same);
+    __syncthreads();
+    if (lane == 63) counts[0][wave] = stay, counts[1][wave] = same;
+    __syncthreads();
+    int next = at, next_seen = seen;
+#pragma unroll
+    for (int w = 0; w < 16; ++w) {
+      if (w == wave) at = next, seen = next_seen;
+      const int e = counts[1][w];
+      next += counts[0][w] + min(e, max(0, ties - next_seen));
+      next_seen += e;
+    }
+    at = __builtin_amdgcn_readfirstlane(at);
+    seen = __builtin_amdgcn_readfirstlane(seen);
+    const int row0 = row(part, 0) + lane;
+    char* to = reinterpret_cast<char*>(kept);
+    auto write = [&](int i, bool stays) {
+      const unsigned long long all = __ballot(stays);
+      if (stays) *reinterpret_cast<int*>(to + ((uint32_t)at + lanes_below(all)) * 4u) = row0 + 64 * i;
+      at += __popcll(all);
+    };
+    if (next_seen <= ties || seen >= ties) {  // all of the wave's equal ones stay (those of later waves do), or none
+      const uint32_t beyond = seen >= ties ? limit : limit - 1;  // (a limit of 0 has no ties)
+#pragma unroll
+      for (int i = 0; i < PER; ++i) write(i, v[i] > beyond);
+    } else {
+#pragma unroll
+      for (int i = 0; i < PER; ++i) {
+        const bool equal = v[i] == limit;
+        const unsigned long long equals = __ballot(equal);
+        write(i, v[i] > limit || (equal && seen + (int)lanes_below(equals) < ties));
+        seen += __popcll(equals);
+      }
+    }
+    at = next;
+    seen = next_seen;
   }
 }
 
