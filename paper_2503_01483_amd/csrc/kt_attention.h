@@ -121,11 +121,16 @@ __device__ __forceinline__ int sequence_at(const int* cum, int n_seq, int u) {
 __device__ __forceinline__ int piece_length(int total, int workers) { return max(1, (int)(((unsigned)total + workers - 1) / (unsigned)workers)); }
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
-// 8 codes of 4 bits as bf16 128 + c: elements 2 i, 2 i + 1 in dword i.
+// 8 codes of 4 bits as bf16 ZERO + c: elements 2 i, 2 i + 1 in dword i.  ZERO: 128 or 16; of sums with the smaller one less is lost when it is taken off.
+template <int ZERO = 128>
 __device__ __forceinline__ bf16x8 spread_nibbles(uint32_t x) {
+  static_assert(ZERO == 128 || ZERO == 16);
   u32x4 t;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) t[i] = (x >> (4 * i) & 0x000f000fu) | 0x43004300u;
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (ZERO == 128) t[i] = (x >> (4 * i) & 0x000f000fu) | 0x43004300u;
+    else t[i] = ((i ? x >> (4 * i - 3) : x << 3) & 0x00780078u) | 0x41804180u;
+  }
   return __builtin_bit_cast(bf16x8, t);
 }
 // 8 tokens' low or high nibbles as bf16 128 + c, in the order 0 2 1 3 4 6 5 7.
@@ -181,21 +186,23 @@ struct Tile64 {
   __device__ __forceinline__ static int token(int t, int r) {
     return KV == kKvBf16 ? 32 * (t >> 1) + 8 * (r >> 2) + 4 * (t & 1) + (r & 3) : 16 * (r >> 2) + 4 * t + (r & 3);
   }
+  // token `tok` of a block as the t-th key
+  __device__ __forceinline__ void load_key(const char* block, int tok, int t, int g) {
+    const char* row = block + tok * (kHalf / kBlockTokens);
+    if constexpr (KV == kKvBf16) {
+#pragma unroll
+      for (int w = 0; w < HD / 32; ++w) *reinterpret_cast<u32x4*>(&k[t][4 * w]) = *reinterpret_cast<const u32x4*>(row + 64 * w + 16 * g);
+    } else if constexpr (KD % 4 == 0) {
+#pragma unroll
+      for (int i = 0; i < KD; i += 4) *reinterpret_cast<u32x4*>(&k[t][i]) = *reinterpret_cast<const u32x4*>(row + 4 * KD * g + 4 * i);
+    } else {
+      *reinterpret_cast<u32x2*>(&k[t][0]) = *reinterpret_cast<const u32x2*>(row + 4 * KD * g);
+    }
+  }
   __device__ __forceinline__ void load_keys(const char* block, int lane) {
     const int r = lane & 15, g = lane >> 4;
 #pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      const char* row = block + token(t, r) * (kHalf / kBlockTokens);
-      if constexpr (KV == kKvBf16) {
-#pragma unroll
-        for (int w = 0; w < HD / 32; ++w) *reinterpret_cast<u32x4*>(&k[t][4 * w]) = *reinterpret_cast<const u32x4*>(row + 64 * w + 16 * g);
-      } else if constexpr (KD % 4 == 0) {
-#pragma unroll
-        for (int i = 0; i < KD; i += 4) *reinterpret_cast<u32x4*>(&k[t][i]) = *reinterpret_cast<const u32x4*>(row + 4 * KD * g + 4 * i);
-      } else {
-        *reinterpret_cast<u32x2*>(&k[t][0]) = *reinterpret_cast<const u32x2*>(row + 4 * KD * g);
-      }
-    }
+    for (int t = 0; t < 4; ++t) load_key(block, token(t, r), t, g);
     if constexpr (KV != kKvBf16) par = reinterpret_cast<const u32x4*>(block + 2 * kHalf)[lane];
   }
   __device__ __forceinline__ void load_values(const char* block, int lane) {
@@ -212,10 +219,11 @@ struct Tile64 {
       }
     }
   }
+  template <int ZERO = 128>
   __device__ __forceinline__ bf16x8 key(int t, int w) const {
     if constexpr (KV == kKvBf16) return __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(&k[t][4 * w]));
     else if constexpr (KV == kKvU8) return spread_bytes(k[t][2 * w], k[t][2 * w + 1]);
-    else return spread_nibbles(k[t][w]);
+    else return spread_nibbles<ZERO>(k[t][w]);
   }
   // features 16 td + r, the 8 tokens of half j
   __device__ __forceinline__ bf16x8 value(int td, int j) const {

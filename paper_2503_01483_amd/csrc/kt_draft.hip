@@ -64,15 +64,25 @@ kt_status kt_attention_mass(const kt_kv_cache* cache, const void* Q, int64_t ldq
   t.mass = mass;
   t.decay = decay;
   hipStream_t st = static_cast<hipStream_t>(stream);
-  const bool few = max_q * a.group <= 16;
-  with_cache(cache, [&](auto kv, auto h) {
+  const int64_t most = max_q * a.group;  // rows a head
+  const bool ok = with_cache(cache, [&](auto kv, auto h) {
     constexpr int KV = decltype(kv)::value, HD = decltype(h)::value;
-    const size_t lds = (size_t)(n_seq + 1) * 4;
-    const int64_t groups = n_seq * ceil_div(ldp * cache->page_size, few ? 256 : 64) * cache->n_heads;
-    const dim3 grid((unsigned)std::min<int64_t>(groups, kNumCUs * 8));
-    if (few) mass_kernel<KV, HD, 1><<<grid, 256, lds, st>>>(t);
-    else mass_kernel<KV, HD, 4><<<grid, 256, lds, st>>>(t);
+    using std::integral_constant;
+    const int64_t tokens = ldp * cache->page_size;
+    const size_t list = (size_t)(n_seq + 1) * 4;
+    auto grid = [&](int keys) { return dim3((unsigned)std::min<int64_t>(n_seq * ceil_div(tokens, keys) * cache->n_heads, kNumCUs * 8)); };
+    auto go_few = [&](auto ni) {
+      mass_few_kernel<KV, HD, decltype(ni)::value><<<grid(256), 256, list, st>>>(t);
+      return true;
+    };
+    if (most <= 4) return go_few(integral_constant<int, 1>{});
+    if (most <= 64) return go_few(integral_constant<int, 4>{});
+    auto kernel = mass_rows_kernel<KV, HD>;
+    if (!ensure_dynamic_lds(reinterpret_cast<const void*>(kernel), sizeof(MassShared<HD>) + (kMaxSequences + 1) * 4)) return false;
+    kernel<<<grid(128), 512, sizeof(MassShared<HD>) + list, st>>>(t);
+    return true;
   });
+  if (!ok) return fail(KT_ERR_DEVICE, "mass kernel needs more LDS than the device gives");
   return launch_ok() ? KT_OK : fail(KT_ERR_DEVICE, "mass kernel launch failed");
 }
 

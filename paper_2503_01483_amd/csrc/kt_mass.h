@@ -2,9 +2,12 @@
 //
 //   mass_j <- decay mass_j (0 of a token that is one of the queries) + sum_r exp(scale q_r . k_j - lse_r),  r over the rows of j's key head that see j
 //
-// A wave holds 64 keys, one block of the cache, in the registers of the 16 x 16 x 32 products' first operand (S^T = K Q^T, as in kt_attention.h) and
-// goes through the rows sixteen at a time: a lane adds up the exponentials of one row in sixteen for its 16 keys, and the 16 lanes are added
-// once at the end.  Every sum has a fixed order and one owner: nothing is atomic, no score leaves the registers.
+// A wave holds 64 keys, one block of the cache, and goes through the rows sixteen at a time, S = Q K^T in 16 x 16 x 32 products with the keys on the
+// columns: a lane has four keys and of each the scores of four rows, whose exponentials it adds up; the four quarters of the wave are added once at the
+// end.  A token's {step, minimum} are its lane's own, and neighbouring lanes write neighbouring masses.  Every sum has a fixed order and one owner: nothing
+// is atomic, no score leaves the registers.
+// With few rows, row j of sixteen is row 4 (j % 4) + j / 4 of the products, so that the first four (a token's, with four queries a head) lie in one register of
+// every quarter, and only that is exponentiated.
 #pragma once
 #include "kt_attention.h"
 
@@ -17,26 +20,25 @@ struct MassArgs {
   float decay;
 };
 
-// Sum over the 16 lanes of a row of the wave, in all of them.
-__device__ __forceinline__ float row16_sum(float v) {
-  v += lane_xor<1>(v);
-  v += lane_xor<2>(v);
-  v += lane_xor<4>(v);
-  return v + lane_xor<8>(v);
+// 16 bytes a lane from memory straight into LDS: lane l lands at lds_addr + 16 l (wave-uniform).  Waits are placed by hand (vmcnt).
+__device__ __forceinline__ void lds_copy_16(const char* base, uint32_t offset, unsigned lds_addr) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(base), "s"(lds_addr) : "memory", "m0");
 }
 
-// Groups of keys of one head in front of each sequence, `cum` [n_seq + 1] (LDS), by a workgroup of 256.
+__device__ __forceinline__ void lds_copy_4(const char* base, uint32_t offset, unsigned lds_addr) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1" ::"v"(offset), "s"(base), "s"(lds_addr) : "memory", "m0");
+}
+
+// Groups of keys of one head in front of each sequence, `cum` [n_seq + 1] (LDS), by a workgroup of THREADS.
+template <int THREADS>
 __device__ __forceinline__ void list_key_groups(const AttendArgs& a, int keys, int* cum) {
-  __shared__ int wave_sum[4];
+  __shared__ int wave_sum[THREADS / 64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   int carry = 0;
-  for (int base = 0; base < a.n_seq; base += 256) {
+  for (int base = 0; base < a.n_seq; base += THREADS) {
     const int s = base + threadIdx.x;
     int mine = 0;
-    if (s < a.n_seq) {
-      const Sequence q = sequence_of(a, s);
-      mine = (int)(((unsigned)q.len + keys - 1) / (unsigned)keys);
-    }
+    if (s < a.n_seq) mine = (int)(((unsigned)sequence_of(a, s).len + keys - 1) / (unsigned)keys);
     int upto = mine;
 #pragma unroll
     for (int o = 1; o < 64; o *= 2) {
@@ -46,125 +48,352 @@ __device__ __forceinline__ void list_key_groups(const AttendArgs& a, int keys, i
     if (lane == 63) wave_sum[wave] = upto;
     __syncthreads();
     int before = carry;
-    for (int w = 0; w < wave; ++w) before += wave_sum[w];
+#pragma unroll
+    for (int w = 0; w < THREADS / 64; ++w) {
+      if (w < wave) before += wave_sum[w];
+      carry += wave_sum[w];
+    }
     if (s < a.n_seq) cum[s] = before + upto - mine;
-    carry += wave_sum[0] + wave_sum[1] + wave_sum[2] + wave_sum[3];
     __syncthreads();
   }
   if (threadIdx.x == 0) cum[a.n_seq] = carry;
   __syncthreads();
 }
 
-// WR of a workgroup's four waves share a block's rows, 4 / WR blocks lie next to each other.
-template <int KV, int HD, int WR>
-__global__ __launch_bounds__(256, 2) void mass_kernel(MassArgs t) {
+// Few rows: a wave goes through all of them, 4 NI at a time, with queries straight from memory.  Bound by HBM: 64 tokens behind up to 16384, 32 + 8 heads of 128, 4 bits:
+// 103 us, 4.1 TB/s of keys, parameters and masses.
+template <int KV, int HD, int NI>
+__global__ __launch_bounds__(256, 2) void mass_few_kernel(MassArgs t) {
   extern __shared__ int cum[];
-  __shared__ float joined[WR > 1 ? 4 : 1][64];
-  constexpr int WK = 4 / WR;
-  constexpr float kInf = __builtin_inff();
+  constexpr int W = HD / 32, ROWS = 4 * NI;
+  constexpr float kInf = __builtin_inff(), kZero = KV == kKvU4 ? 16.f : 0.f;  // codes of 4 bits enter as 16 + c
   using Tile = Tile64<KV, HD>;
   const AttendArgs& a = t.a;
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), r = lane & 15, g = lane >> 4, heads = a.cache.n_heads;
-  const int wk = wave / WR, wr = wave % WR, page_blocks = a.cache.log2_page - 6;
+  const int page_blocks = a.cache.log2_page - 6;
   const float c = a.scale * 1.44269504f;
-  list_key_groups(a, 64 * WK, cum);
+  list_key_groups<256>(a, 256, cum);
   const int64_t total = (int64_t)cum[a.n_seq] * heads;
-  const int step_q = 16 * WR / a.group, step_r = 16 * WR - step_q * a.group;
+  const int step_q = ROWS / a.group, step_r = ROWS - step_q * a.group;
 
   for (int64_t u = blockIdx.x; u < total; u += gridDim.x) {
     const int at = (int)(u / heads), head = (int)(u - (int64_t)at * heads);
     const int s = uniform(sequence_at(cum, a.n_seq, at));
     const Sequence q = sequence_of(a, s);
-    const int tile = (at - uniform(cum[s])) * WK + wk, ahead = q.len - q.count, key0 = tile * 64;
+    const int tile = (at - uniform(cum[s])) * 4 + wave, ahead = q.len - q.count, key0 = tile * 64;
     const int there = uniform(min(q.len - key0, 64));
     int page = there > 0 ? a.pages[s * a.ldp + (tile >> page_blocks)] : -1;
     if (page >= a.cache.n_pages) page = -1;
     page = uniform(page);
-    float sum[4][4];
+    if (page < 0) continue;
+    float sum[4] = {0.f, 0.f, 0.f, 0.f}, old = 0.f;
+    float* const mass = t.mass + (((int64_t)page * heads + head) << a.cache.log2_page) + (key0 & ((1 << a.cache.log2_page) - 1)) + lane;
+    Tile k;
+    const char* block = a.cache.data + kv_block_offset<KV, HD>(a.cache, page, head, tile & ((1 << page_blocks) - 1));
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < 4; ++i) k.load_key(block, 16 * i + r, i, g);
+    [[maybe_unused]] float2 par[4];
+    if constexpr (KV != kKvBf16) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) sum[i][e] = 0.f;
-    if (page >= 0) {
-      Tile k;
-      const int64_t block = kv_block_offset<KV, HD>(a.cache, page, head, tile & ((1 << page_blocks) - 1));
-      k.load_keys(a.cache.data + block, lane);
-      [[maybe_unused]] f32x4 par[4][2];  // {step, minimum} of a lane's keys
-      if constexpr (KV != kKvBf16) {
-        const f32x4* p = reinterpret_cast<const f32x4*>(a.cache.data + block + 2 * Tile::kHalf) + 8 * g;
+      for (int i = 0; i < 4; ++i) par[i] = reinterpret_cast<const float2*>(block + 2 * Tile::kHalf)[16 * i + r];
+    }
+    if (t.decay != 0.f && key0 + lane < ahead) old = *mass;
+    // rows from the first that sees the first key on; this lane's queries are those of row j of a group of rows
+    const int j = (r >> 2) + 4 * (r & 3);
+    const int64_t rows = (int64_t)q.count * a.group;
+    int64_t row0 = max(0, key0 - ahead) * (int64_t)a.group & ~(int64_t)(ROWS - 1);
+    int in_seq = (int)((row0 + j) / a.group), rest = (int)(row0 + j - (int64_t)in_seq * a.group);
+    bf16x8 qf[W];
+    float lse = 0.f;
+    int seen = 0;  // of the block's tokens by row j; 0: it adds nothing
+    auto ask = [&] {
+      const bool live = j < ROWS && row0 + j < rows;
+      const int64_t token = q.first + (live ? in_seq : 0);
+      const int qh = head * a.group + (live ? rest : 0);
+#pragma unroll
+      for (int w = 0; w < W; ++w) qf[w] = *reinterpret_cast<const bf16x8*>(a.q + token * a.ldq + qh * HD + 32 * w + 8 * g);
+      lse = t.lse[token * a.hq + qh];
+      seen = live ? ahead + in_seq + 1 - key0 : 0;
+      in_seq += step_q;
+      rest += step_r;
+      if (rest >= a.group) rest -= a.group, ++in_seq;
+    };
+    if (row0 < rows) ask();
+    if constexpr (KV != kKvBf16) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) par[i].x *= c, par[i].y *= c;
+    }
+    while (row0 < rows) {
+      if constexpr (KV != kKvBf16) {  // (codes are expanded anew for every group of rows: kept expanded they would take the registers of other waves)
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
-          for (int h = 0; h < 2; ++h) par[i][h] = p[2 * i + h];
+          for (int w = 0; w < Tile::KD; ++w) asm volatile("" : "+v"(k.k[i][w]));
       }
-      // rows from the first that sees the first key on
-      const int64_t rows = (int64_t)q.count * a.group;
-      int64_t row = (max(0, key0 - ahead) * (int64_t)a.group & ~(int64_t)15) + 16 * wr + r;
-      int in_seq = (int)(row / a.group), rest = (int)(row - (int64_t)in_seq * a.group);
-      for (; row - r < rows; row += 16 * WR) {
-        const bool live = row < rows;
-        const int64_t token = q.first + (live ? in_seq : 0);
-        const int qh = head * a.group + (live ? rest : 0);
-        bf16x8 qf[HD / 32];
+      f32x4 x[4], qsum = {0.f, 0.f, 0.f, 0.f};
+      if constexpr (KV != kKvBf16) {
+        bf16x8 one;
 #pragma unroll
-        for (int w = 0; w < HD / 32; ++w) qf[w] = *reinterpret_cast<const bf16x8*>(a.q + token * a.ldq + qh * HD + 32 * w + 8 * g);
-        const float lse = t.lse[token * a.hq + qh];
-        const bool counts = live && fabsf(lse) <= kHuge;
-        const float base = counts ? lse * 1.44269504f : kInf;
+        for (int e = 0; e < 8; ++e) one[e] = (bf16)1.f;
+#pragma unroll
+        for (int w = 0; w < W; ++w) qsum = mfma16(qf[w], one, qsum);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        x[i] = KV == kKvU4 ? -kZero * qsum : f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < W; ++w) x[i] = mfma16(qf[w], k.template key<(int)kZero>(i, w), x[i]);
+      }
+      const bool counts = fabsf(lse) <= kHuge;
+      const float mine = counts ? lse * -1.44269504f : -kInf;
+      const int mine_seen = counts ? seen : 0;
+      const bool edge = __any(mine_seen < 64);
+      float base[NI];
+      [[maybe_unused]] int sees[NI];
+#pragma unroll
+      for (int e = 0; e < NI; ++e) base[e] = __shfl(mine, 4 * g + e);
+      if (edge)
+#pragma unroll
+        for (int e = 0; e < NI; ++e) sees[e] = __shfl(mine_seen, 4 * g + e);
+      row0 += ROWS;
+      if (row0 < rows) ask();
+#pragma unroll
+      for (int e = 0; e < NI; ++e)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          float y;
+          if constexpr (KV == kKvBf16) y = fmaf(x[i][e], c, base[e]);
+          else y = fmaf(x[i][e], par[i].x, fmaf(par[i].y, qsum[e], base[e]));
+          x[i][e] = __builtin_amdgcn_exp2f(y);
+        }
+      if (edge)
+#pragma unroll
+        for (int e = 0; e < NI; ++e)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) x[i][e] = 16 * i + r < sees[e] ? x[i][e] : 0.f;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float add = x[i][0];
+#pragma unroll
+        for (int e = 1; e < NI; ++e) add += x[i][e];
+        sum[i] += add;
+      }
+    }
+    // lane l has key l
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sum[i] = quarters_sum(sum[i]);
+    const float mine = g == 0 ? sum[0] : g == 1 ? sum[1] : g == 2 ? sum[2] : sum[3];
+    if (lane < there) *mass = fmaf(t.decay, old, mine);
+  }
+}
+
+// Many rows: queries go through LDS, 64 rows at a time, double buffered, straight from memory, by lanes that read neighbouring bytes (an operand's
+// own lanes read sixteen rows at once, of which the first-level cache finds one a cycle: 690 us instead of 440 for prompts of up to 2 x 8192, 32 + 8 heads of 128, bf16).  Four of the eight waves share a block and
+// take sixteen of the rows each, the two blocks lie next to each other.  Rows go from the last one down to the first that sees the first key:
+// workgroups that begin together find each other's queries in the caches.
+// Bound by the vector ALU (an exponential, two more instructions a score) and by the workgroup with the most rows, alone on its compute unit at the
+// end: 770 TFLOP/s of Q K^T for those prompts.
+template <int HD>
+struct MassShared {
+  char q[2][64 * HD * 2];  // 16-byte chunks of a row exchanged by its number, so that eight rows' are in all banks
+  float lse[2][64];        // as it comes
+  float base[2][64];       // -lse in bits; -inf: the row adds nothing
+  int sees[2][64];         // tokens of the sequence that a row sees; 0 of one that adds nothing
+  int least[2];            // the least of these
+};
+
+template <int KV, int HD>
+__global__ __launch_bounds__(512, HD == 256 ? 2 : 4) void mass_rows_kernel(MassArgs t) {
+  extern __shared__ __align__(16) char lds[];
+  using Shared = MassShared<HD>;
+  Shared& sh = *reinterpret_cast<Shared*>(lds);
+  int* const cum = reinterpret_cast<int*>(lds + sizeof(Shared));
+  __shared__ float joined[8][64];
+  constexpr int WK = 2, WR = 4, W = HD / 32, ROWB = HD * 2, PIECES = HD / 64;  // KiB of a wave
+  constexpr float kInf = __builtin_inff(), kZero = KV == kKvU4 ? 16.f : 0.f;
+  using Tile = Tile64<KV, HD>;
+  const AttendArgs& a = t.a;
+  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), r = lane & 15, g = lane >> 4, heads = a.cache.n_heads;
+  const int wk = wave / WR, wr = wave % WR, page_blocks = a.cache.log2_page - 6;
+  const float c = a.scale * 1.44269504f, per_group = 1.f / (float)a.group;
+  const int step_q = 64 / a.group, step_r = 64 - step_q * a.group;
+  list_key_groups<512>(a, 64 * WK, cum);
+  const int64_t total = (int64_t)cum[a.n_seq] * heads;
+
+  for (int64_t u = blockIdx.x; u < total; u += gridDim.x) {
+    const int at = (int)(u / heads), head = (int)(u - (int64_t)at * heads);
+    const int s = uniform(sequence_at(cum, a.n_seq, at));
+    const Sequence q = sequence_of(a, s);
+    // a sequence's groups of keys: the first half in order, then from the last one back, so that two on a compute unit have as many rows together
+    const int groups = uniform(cum[s + 1] - cum[s]), n = at - uniform(cum[s]), group = n < (groups + 1) / 2 ? n : groups - 1 - (n - (groups + 1) / 2);
+    const int tile = group * WK + wk, ahead = q.len - q.count, key0 = tile * 64;
+    const int there = uniform(min(q.len - key0, 64));
+    int page = there > 0 ? a.pages[s * a.ldp + (tile >> page_blocks)] : -1;
+    if (page >= a.cache.n_pages) page = -1;
+    page = uniform(page);
+    float sum[4] = {0.f, 0.f, 0.f, 0.f}, old = 0.f;
+    float* const mass = t.mass + (((int64_t)max(page, 0) * heads + head) << a.cache.log2_page) + (key0 & ((1 << a.cache.log2_page) - 1)) + lane;
+    Tile k;
+    const char* block = a.cache.data + (page < 0 ? 0 : kv_block_offset<KV, HD>(a.cache, page, head, tile & ((1 << page_blocks) - 1)));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) k.load_key(block, 16 * i + r, i, g);
+    [[maybe_unused]] float2 par[4];
+    if constexpr (KV != kKvBf16) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) par[i] = reinterpret_cast<const float2*>(block + 2 * Tile::kHalf)[16 * i + r];
+    }
+    if (page >= 0 && wr == 0 && t.decay != 0.f && key0 + lane < ahead) old = *mass;
+    const int64_t rows = (int64_t)q.count * a.group;
+    const int64_t first = max(0, group * WK * 64 - ahead) * (int64_t)a.group >> 6;  // tile of 64 rows
+    int64_t rt = ((rows + 63) >> 6) - 1;
+    int base_q = (int)(rt * 64 / a.group), base_r = (int)(rt * 64 - (int64_t)base_q * a.group);  // the first row of the tile that is asked for next
+    int sees = 0;  // by row `lane` of the tile that was asked for last
+    // Row `row` of that tile: its query and head.  (Numbers of less than 2^17: the product is off by one at most.)
+    auto find = [&](int row, int& in_seq, int& rest) {
+      const int x = base_r + row;
+      in_seq = (int)((float)x * per_group);
+      rest = x - in_seq * a.group;
+      if (rest < 0) rest += a.group, --in_seq;
+      if (rest >= a.group) rest -= a.group, ++in_seq;
+      in_seq += base_q;
+    };
+    // The i-th piece that this wave fetches of a tile: this lane's part lies `offset` behind the first row of the tile's first query and of the head.
+    const char* const heads_lse = reinterpret_cast<const char*>(t.lse + (int64_t)q.first * a.hq + head * a.group);
+    const char* const heads_q = reinterpret_cast<const char*>(a.q) + ((int64_t)q.first * a.ldq + head * a.group * HD) * 2;
+    auto offset_of = [&](int i, int lane, int64_t left) {
+      const int byte = (wave * PIECES + i) * 1024 + lane * 16, row = byte / ROWB, chunk = byte % ROWB / 16 ^ (row & 7);
+      int in_seq, rest;
+      find(row, in_seq, rest);
+      const bool live = row < left;  // (rows behind the last one: some row of the first query that is there)
+      return (live ? (uint32_t)(in_seq - base_q) * (uint32_t)(a.ldq * 2) + (uint32_t)(rest * ROWB) : 0u) + (uint32_t)(chunk * 16);
+    };
+    auto send = [&](const char* base, uint32_t offset, int i, int at) { lds_copy_16(base, offset, uniform((int)(uintptr_t)sh.q[at] + (wave * PIECES + i) * 1024)); };
+    auto fetch = [&](int64_t rt, int at) {
+      int tid = threadIdx.x;
+      asm volatile("" : "+v"(tid));  // (places are worked out anew: kept, they would push the keys out to memory)
+      const char* base = heads_q + (int64_t)base_q * a.ldq * 2;
+#pragma unroll
+      for (int i = 0; i < PIECES; ++i) send(base, offset_of(i, tid & 63, rows - rt * 64), i, at);
+      if (wave == 0) {
+        int in_seq, rest;
+        find(tid, in_seq, rest);
+        lds_copy_4(heads_lse + (int64_t)base_q * a.hq * 4, rt * 64 + tid < rows ? ((uint32_t)(in_seq - base_q) * (uint32_t)a.hq + (uint32_t)rest) * 4u : 0u,
+                   uniform((int)(uintptr_t)sh.lse[at]));
+        sees = ahead + in_seq + 1;
+      }
+      base_q -= step_q;
+      base_r -= step_r;
+      if (base_r < 0) base_r += a.group, --base_q;
+    };
+    // Where the query heads of a key head divide 64, rows of neighbouring tiles are whole queries apart: places are those of the tile before.
+    const bool even = step_r == 0;
+    uint32_t offsets[PIECES] = {}, offset_lse = 0;
+    auto place_next = [&] {
+#pragma unroll
+      for (int i = 0; i < PIECES; ++i) offsets[i] = offset_of(i, lane, 64);
+      int in_seq, rest;
+      find(lane, in_seq, rest);
+      offset_lse = ((uint32_t)(in_seq - base_q) * (uint32_t)a.hq + (uint32_t)rest) * 4u;
+    };
+    auto fetch_even = [&](int at) {
+      const char* base = heads_q + (int64_t)base_q * a.ldq * 2;
+#pragma unroll
+      for (int i = 0; i < PIECES; ++i) send(base, offsets[i], i, at);
+      if (wave == 0) lds_copy_4(heads_lse + (int64_t)base_q * a.hq * 4, offset_lse, uniform((int)(uintptr_t)sh.lse[at]));
+      sees -= step_q;
+      base_q -= step_q;
+    };
+    auto put = [&](int64_t rt, int at) {
+      if (wave == 0) {
+        const float lse = sh.lse[at][lane];
+        const bool counts = fabsf(lse) <= kHuge && rt * 64 + lane < rows;
+        const int mine = counts ? sees : 0;
+        sh.base[at][lane] = counts ? lse * -1.44269504f : -kInf;
+        sh.sees[at][lane] = mine;
+        const int least = -wave_max(-mine);
+        if (lane == 0) sh.least[at] = least;
+      }
+    };
+    bf16x8 kf[4][W];
+    __syncthreads();  // the buffers are free
+    if (rt >= first) {
+      fetch(rt, rt & 1);
+      if (even && rt > first) place_next();
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int w = 0; w < W; ++w) kf[i][w] = k.template key<(int)kZero>(i, w);
+    if constexpr (KV != kKvBf16) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) par[i].x *= c, par[i].y *= c;
+    }
+    // keys have arrived before the loop: a wait for them in it would be one for the queries that are on their way
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int w = 0; w < W; ++w) asm volatile("" : "+v"(kf[i][w]));
+    for (; rt >= first; --rt) {
+      const int at = rt & 1;
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // this wave's part has arrived
+      put(rt, at);
+      __syncthreads();
+      if (rt > first) {
+        if (even) fetch_even(at ^ 1);
+        else fetch(rt - 1, at ^ 1);
+      }
+      const bool edge = uniform(sh.least[at]) < key0 + 64;
+      {
+        const int row0 = 16 * wr;
+        bf16x8 qf[W];
+#pragma unroll
+        for (int w = 0; w < W; ++w) qf[w] = *reinterpret_cast<const bf16x8*>(sh.q[at] + (row0 + r) * ROWB + (((4 * w + g) ^ (r & 7)) << 4));
+        const f32x4 base = *reinterpret_cast<const f32x4*>(&sh.base[at][row0 + 4 * g]);
         f32x4 x[4], qsum = {0.f, 0.f, 0.f, 0.f};
         if constexpr (KV != kKvBf16) {
           bf16x8 one;
 #pragma unroll
           for (int e = 0; e < 8; ++e) one[e] = (bf16)1.f;
 #pragma unroll
-          for (int w = 0; w < HD / 32; ++w) qsum = mfma16(one, qf[w], qsum);
+          for (int w = 0; w < W; ++w) qsum = mfma16(qf[w], one, qsum);
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          x[i] = KV == kKvU4 ? -128.f * qsum : f32x4{0.f, 0.f, 0.f, 0.f};
+          x[i] = KV == kKvU4 ? -kZero * qsum : f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int w = 0; w < HD / 32; ++w) x[i] = mfma16(k.key(i, w), qf[w], x[i]);
-          if constexpr (KV != kKvBf16) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) x[i][e] = fmaf(x[i][e], par[i][e >> 1][2 * (e & 1)], par[i][e >> 1][2 * (e & 1) + 1] * qsum[e]);
-          }
+          for (int w = 0; w < W; ++w) x[i] = mfma16(qf[w], kf[i][w], x[i]);
         }
-        const int seen = counts ? ahead + in_seq + 1 - key0 : 0;  // of the block's tokens
-        const bool edge = __any(seen < 64);
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int e = 0; e < 4; ++e)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float p = __builtin_amdgcn_exp2f(fmaf(x[i][e], c, -base));
-            sum[i][e] += edge && Tile::token(i, 4 * g + e) >= seen ? 0.f : p;
+          for (int i = 0; i < 4; ++i) {
+            float y;
+            if constexpr (KV == kKvBf16) y = fmaf(x[i][e], c, base[e]);
+            else y = fmaf(x[i][e], par[i].x, fmaf(par[i].y, qsum[e], base[e]));
+            x[i][e] = __builtin_amdgcn_exp2f(y);
           }
-        in_seq += step_q;
-        rest += step_r;
-        if (rest >= a.group) rest -= a.group, ++in_seq;
+        if (edge) {
+          const int4 seen = *reinterpret_cast<const int4*>(&sh.sees[at][row0 + 4 * g]);
+          const int see[4] = {seen.x, seen.y, seen.z, seen.w};
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[i][e] = key0 + 16 * i + r < see[e] ? x[i][e] : 0.f;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum[i] += (x[i][0] + x[i][1]) + (x[i][2] + x[i][3]);
       }
     }
+    // lane l has key l
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) sum[i][e] = row16_sum(sum[i][e]);
-    // lane r of a quarter keeps its r-th key
-    float mine = 0.f;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) mine = r == i ? sum[i >> 2][i & 3] : mine;
-    const int j = Tile::token(r >> 2, 4 * g + (r & 3));
-    if constexpr (WR > 1) {
-      __syncthreads();
-      joined[wave][lane] = mine;
-      __syncthreads();
-      if (wr != 0) continue;
-      mine = 0.f;
+    for (int i = 0; i < 4; ++i) sum[i] = quarters_sum(sum[i]);
+    joined[wave][lane] = g == 0 ? sum[0] : g == 1 ? sum[1] : g == 2 ? sum[2] : sum[3];
+    __syncthreads();
+    if (wr == 0 && page >= 0 && lane < there) {
+      float mine = 0.f;
 #pragma unroll
       for (int w = 0; w < WR; ++w) mine += joined[wk * WR + w][lane];
-    }
-    if (page >= 0 && j < there) {
-      float* to = t.mass + (((int64_t)page * heads + head) << a.cache.log2_page) + ((key0 + j) & ((1 << a.cache.log2_page) - 1));
-      if (key0 + j < ahead && t.decay != 0.f) mine = fmaf(t.decay, *to, mine);
-      *to = mine;
+      *mass = fmaf(t.decay, old, mine);
     }
   }
 }
