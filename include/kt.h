@@ -482,9 +482,9 @@ size_t kt_paged_attention_bytes(int64_t n_tokens, int64_t n_q_heads, int64_t hea
  *  tree     [n_tokens][ldt] uint64: bit d % 64 of word d / 64 of a query's row says whether it sees query d of its sequence (usually its ancestors and
  *           itself).  Bits of queries that the sequence does not have are passed over.  ldt at least ceil(max_q / 64), 8-byte aligned.
  *  q_starts NULL: one query a sequence, whose bit 0 says whether it sees itself.
- * A query without tokens in front and with no bit set gives 0, and -inf in lse.  Everything else, the prefix, the workspace (kt_paged_attention_bytes)
- * and how results are rounded among it, is as kt_paged_attention says.  Queries whose masks name all queries up to their own are chunks; the
- * order of sums can be another than kt_paged_attention's.
+ * A query without tokens in front and with no bit set gives 0, and -inf in lse.  Everything else, the prefix and the workspace (kt_paged_attention_bytes)
+ * among it, is as kt_paged_attention says, but for which calls round p times the value's step to 16 bits: those with max_q * n_q_heads / n_heads
+ * <= 64 (KT_KV_U4) or 32 (KT_KV_U8).  Queries whose masks name all queries up to their own are a chunk of kt_paged_attention; the order of sums can be another.
  */
 kt_status kt_tree_attention(const kt_kv_cache* cache, const void* Q, int64_t ldq, kt_dtype dtype, const int32_t* q_starts,
                             const int32_t* lens, const int32_t* pages, int64_t ldp, int64_t n_seq, int64_t n_tokens,

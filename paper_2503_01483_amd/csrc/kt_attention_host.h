@@ -29,6 +29,16 @@ static int64_t most_few_rows(const kt_kv_cache* c) {
   return c->format == KT_KV_U8 && c->head_dim == 256 ? 32 : 64;
 }
 
+// Trees: their workgroups of kt_attention_tiles.h have 128 rows and leave out waves without any (bf16, more than 128 rows: 256).  By the rows of a sequence and
+// head, us with waves / with tiles, 64 sequences of up to 4096 tokens (4 of 30000), 8 heads:
+//   bf16  64 features   8 rows 72 / 78 (38 / 40), 32 rows 101 / 83;            128 features  8 rows 155 / 146 (68 / 62), 32 rows 213 / 156;
+//         256 features  8 rows (of 2048) 181 / 200 (164 / 150), 32 rows 229 / 203
+//   u8    64 features   32 rows 73 / 96 (49 / 49), 64 rows 114 / 110;          128 features  32 rows 108 / 126 (71 / 66), 64 rows 173 / 153 (106 / 78);
+//         256 features  32 rows 232 / 317 (146 / 143), 64 rows 360 / 334
+//   u4    64 features   64 rows 100 / 113 (60 / 60), 128 rows 169 / 138;       128 features  64 rows 125 / 141 (81 / 76), 128 rows 223 / 171;
+//         256 features  64 rows 282 / 317 (175 / 148), 128 rows 494 / 348
+static int64_t most_few_tree_rows(const kt_kv_cache* c) { return c->format == KT_KV_BF16 ? 0 : c->format == KT_KV_U8 ? 32 : 64; }
+
 // Tiles of a prefix that single tokens share are split until the launch fills the card (96 tokens, 8192 in front: 16 splits).
 static int64_t prefix_splits(int64_t n_tokens, int64_t hq, int64_t n_heads, int64_t hd, int64_t prefix_len) {
   const int64_t items = ceil_div(n_tokens * (hq / n_heads), tile_rows(hd)) * n_heads;
@@ -61,12 +71,12 @@ static AttendPlan plan_attention(int64_t n_tokens, int64_t hq, int64_t hd, int64
   return p;
 }
 
-template <int KV, int HD, bool PREFIX, bool TREE>
+template <int KV, int HD, int WAVES, bool PREFIX, bool TREE>
 static bool launch_tiles(const TileArgs& t, int64_t wgs, hipStream_t st) {
-  constexpr size_t lds = sizeof(TileShared<KV, HD, tile_waves(HD)>);
-  auto kernel = attend_tiles_kernel<KV, HD, tile_waves(HD), PREFIX, TREE>;
-  if (!ensure_dynamic_lds(reinterpret_cast<const void*>(kernel), lds)) return false;
-  kernel<<<dim3((unsigned)wgs), 64 * tile_waves(HD), lds, st>>>(t);
+  const size_t lds = tiles_lds<KV, HD, WAVES, TREE>() + (TREE ? (size_t)(t.a.n_seq + 1) * 4 : 0);
+  auto kernel = attend_tiles_kernel<KV, HD, WAVES, PREFIX, TREE>;
+  if (!ensure_dynamic_lds(reinterpret_cast<const void*>(kernel), tiles_lds<KV, HD, WAVES, TREE>() + (TREE ? (kMaxSequences + 1) * 4 : 0))) return false;
+  kernel<<<dim3((unsigned)wgs), 64 * WAVES, lds, st>>>(t);
   return true;
 }
 
@@ -103,10 +113,10 @@ static kt_status attend(const kt_kv_cache* cache, const void* Q, int64_t ldq, kt
     return fail(KT_ERR_BAD_SHAPE, "index arrays and lse must be aligned to their type");
 
   const int64_t group = n_q_heads / cache->n_heads;
-  const int64_t most = most_few_rows(cache);
+  const int64_t most = TREE ? most_few_tree_rows(cache) : most_few_rows(cache);
   const bool few = max_q <= most && max_q * group <= most;
   const int64_t row_tiles = few ? ceil_div(max_q * group, kRows) : 0;
-  const int64_t entries = few ? n_seq * row_tiles : n_tokens * group / tile_rows(hd) + n_seq;
+  const int64_t entries = few ? n_seq * row_tiles : n_tokens * group / (TREE ? 128 : tile_rows(hd)) + n_seq;
   if (entries > INT32_MAX / 2 / cache->n_heads / (ceil_div(ldp * cache->page_size, 64) + (few ? 0 : ceil_div(prefix_len, 64) + kSegmentCost)))
     return fail(KT_ERR_NOT_SUPPORTED, "too many tiles of 64 keys for one call: hand in a narrower page table or fewer tokens");
 
@@ -152,16 +162,33 @@ static kt_status attend(const kt_kv_cache* cache, const void* Q, int64_t ldq, kt
   const bool ok = with_cache(cache, [&](auto kv, auto h) {
     constexpr int KV = decltype(kv)::value, HD = decltype(h)::value, kRowsOf = 1024 / HD, ROWS = tile_rows(HD);  // (rows of a workgroup that joins)
     if (!few) {
-      plan_tiles_kernel<ROWS, TREE><<<1, 1024, 0, st>>>(t);
-      if (!launch_tiles<KV, HD, false, TREE>(t, t.workers, st)) return false;
-      join_tiles_kernel<HD, ROWS><<<dim3((unsigned)t.workers, ROWS / kRowsOf), 256, 0, st>>>(t);
-      return true;
+      auto go = [&](auto waves) {
+        constexpr int WAVES = decltype(waves)::value, R = 32 * WAVES;
+        if constexpr (TREE) {
+          t.workers = kTileWorkers * ROWS / R;
+          a.row_tiles = (int)ceil_div(max_q * group, R);
+        } else {
+          plan_tiles_kernel<R><<<1, 1024, 0, st>>>(t);
+        }
+        if (!launch_tiles<KV, HD, WAVES, false, TREE>(t, t.workers, st)) return false;
+        join_tiles_kernel<HD, R, TREE><<<dim3((unsigned)t.workers, R / kRowsOf), 256, 0, st>>>(t);
+        return true;
+      };
+      if constexpr (TREE && KV != kKvBf16) {
+        return go(std::integral_constant<int, 4>{});
+      } else {
+        if (TREE && max_q * group <= 128) return go(std::integral_constant<int, 4>{});
+        return go(std::integral_constant<int, tile_waves(HD)>{});
+      }
     }
-    if (prefix_len && !launch_tiles<KV, HD, true, TREE>(t, ceil_div(n_tokens * group, ROWS) * cache->n_heads * t.splits, st)) return false;
+    if constexpr (TREE && KV == kKvBf16) return false;  // (no tree takes this)
+    else {
+    if (prefix_len && !launch_tiles<KV, HD, tile_waves(HD), true, false>(t, ceil_div(n_tokens * group, ROWS) * cache->n_heads * t.splits, st)) return false;
     attend_rows_kernel<KV, HD, TREE><<<dim3(kWaveWorkers / 4), 256, (size_t)(n_seq + 1) * 4, st>>>(a);
     if (prefix_len) join_prefix_kernel<HD><<<dim3((unsigned)ceil_div(n_tokens * n_q_heads, kRowsOf)), 256, 0, st>>>(t);
     else attend_join_kernel<HD><<<dim3(kWaveWorkers, 4), 256, 0, st>>>(a);
     return true;
+    }
   });
   if (!ok) return fail(KT_ERR_DEVICE, "attention kernel needs more LDS than the device gives");
   return launch_ok() ? KT_OK : fail(KT_ERR_DEVICE, "attention kernel launch failed");

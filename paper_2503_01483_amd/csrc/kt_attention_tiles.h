@@ -38,7 +38,7 @@ struct TileArgs {
   int workers;           // workgroups; a multiple of 8
   int entries;           // row tiles of one head, gaps among them
   int4* list;            // [entries + 1] {tiles of the keys (and cost) in front, sequence, row tile, tiles and cost}
-  int4* cuts;            // [workers] {entry, head, pieces or 0}
+  int4* cuts;            // [workers] {entry, head, pieces or 0}; of trees {first token, first row, pieces * 512 + rows or 0, head}
   float* part;           // pieces of cut segments: O [2 workers][R][HD], then {max in bits, sum}
   int splits;            // of a prefix of its own (kt_attention.h takes the rest)
   float* prefix_part;    // [splits][n_tokens][hq][HD], then {max in bits, sum}
@@ -62,8 +62,51 @@ __device__ __forceinline__ int64_t first_entry(const AttendArgs& a, int s, int R
 // list, in front of them, so that pieces take equally long.
 constexpr int kSegmentCost = 4;
 
-// The list of row tiles.  One workgroup of 1024.  TREE: every row can see all of its sequence's queries.
-template <int R, bool TREE>
+// Trees: every row tile of a sequence goes through all of its tokens, so that the list is one number a sequence, which each workgroup works out for itself.
+__device__ __forceinline__ int tree_units(const TileArgs& t, const Sequence& q) {
+  return kSegmentCost + max(1, (int)(((unsigned)t.prefix_len + 63) >> 6) + (int)(((unsigned)q.len + 63) >> 6));
+}
+template <int R>
+__device__ __forceinline__ int tree_row_tiles(const AttendArgs& a, const Sequence& q) {
+  return (int)min(((int64_t)q.count * a.group + R - 1) / R, (int64_t)a.row_tiles);
+}
+// Units in front of each sequence, `cum` [n_seq + 1] (LDS), by a workgroup of THREADS.
+template <int R, int THREADS>
+__device__ __forceinline__ void list_trees(const TileArgs& t, int* cum) {
+  __shared__ int wave_sum[THREADS / 64];
+  const AttendArgs& a = t.a;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int carry = 0;
+  for (int base = 0; base < a.n_seq; base += THREADS) {
+    const int s = base + threadIdx.x;
+    int mine = 0;
+    if (s < a.n_seq) {
+      const Sequence q = sequence_of(a, s);
+      mine = tree_row_tiles<R>(a, q) * tree_units(t, q);
+    }
+    int upto = mine;
+#pragma unroll
+    for (int o = 1; o < 64; o *= 2) {
+      const int v = __shfl_up(upto, o);
+      if (lane >= o) upto += v;
+    }
+    if (lane == 63) wave_sum[wave] = upto;
+    __syncthreads();
+    int before = carry;
+#pragma unroll
+    for (int w = 0; w < THREADS / 64; ++w) {
+      if (w < wave) before += wave_sum[w];
+      carry += wave_sum[w];
+    }
+    if (s < a.n_seq) cum[s] = before + upto - mine;
+    __syncthreads();
+  }
+  if (threadIdx.x == 0) cum[a.n_seq] = carry;
+  __syncthreads();
+}
+
+// The list of row tiles.  One workgroup of 1024.
+template <int R>
 __global__ __launch_bounds__(1024) void plan_tiles_kernel(TileArgs t) {
   __shared__ int wave_sum[16];
   const AttendArgs& a = t.a;
@@ -86,7 +129,7 @@ __global__ __launch_bounds__(1024) void plan_tiles_kernel(TileArgs t) {
       const int64_t rows = (int64_t)q.count * a.group;
       if (rt >= 0 && rt * R < rows) {
         const int last = (int)((min(rows, (rt + 1) * R) - 1) / a.group);
-        const int sees = TREE ? q.len : min(max(q.len - q.count + last + 1, 0), q.len);
+        const int sees = min(max(q.len - q.count + last + 1, 0), q.len);
         mine = kSegmentCost + max(1, prefix_tiles + (int)(((unsigned)sees + 63) >> 6));
       }
     }
@@ -111,22 +154,39 @@ __global__ __launch_bounds__(1024) void plan_tiles_kernel(TileArgs t) {
   if (threadIdx.x == 0) t.list[t.entries] = int4{carry, 0, 0, 0};
 }
 
-template <int KV, int HD, int WAVES>
+template <int KV, int HD, int WAVES, int BUFFERS>
 struct TileShared {
   static constexpr int kTile = kBlockTokens * HD * 2;
   // 16-byte chunks exchanged within a row (swizzled)
-  char keys[2][kTile];          // [64][HD]
-  char values[2][kTile];        // [HD][64]
-  float2 par[2][64];            // {step, minimum} of the keys, times the factor of the exponentials
-  _Float16 expand[WAVES][2][64];  // steps of the values that are being expanded, and what their middle code stands for
-  float power[2][64];             // exponents of the tokens' values, where each has its own
-  unsigned long long odd[2][WAVES];  // bf16: tokens of a masked tile with values that are not finite, those in the pieces of each wave
+  char keys[BUFFERS][kTile];          // [64][HD]
+  char values[BUFFERS][kTile];        // [HD][64]
+  float2 par[BUFFERS][64];            // {step, minimum} of the keys, times the factor of the exponentials
+  _Float16 expand[WAVES][2][64];      // steps of the values that are being expanded, and what their middle code stands for
+  float power[BUFFERS][64];           // exponents of the tokens' values, where each has its own
+  unsigned long long odd[BUFFERS][WAVES];  // bf16: tokens of a masked tile with values that are not finite, those in the pieces of each wave
 };
 
+// Blocks of a quantised cache that a workgroup of a tree has in LDS or on their way there, as they are.
+template <int KV, int HD>
+constexpr int ring_blocks() { return KV == kKvU4 ? 4 : 2; }
+// What one wave finds out about such a block for all of them.  Eight tokens are in the order 0 2 1 3 4 6 5 7, that of their codes' bytes in `expand_values`.
+struct TileParams {
+  _Float16 step[64], middle[64];  // of the values, scaled
+  float power[64];                // exponents of the tokens' values, where each has its own
+  float2 par[64];                 // {step, minimum} of the keys, times the factor of the exponentials
+  int v_exp, each, odd[2];        // as in attend_tiles_kernel
+};
+// LDS of a workgroup in front of the list of trees.
+template <int KV, int HD, int WAVES, bool TREE>
+constexpr size_t tiles_lds() {
+  if (TREE && KV != kKvBf16) return sizeof(TileShared<KV, HD, WAVES, 1>) + 2 * sizeof(TileParams) + ring_blocks<KV, HD>() * kv_block_bytes<KV, HD>();
+  return sizeof(TileShared<KV, HD, WAVES, 2>);
+}
+
 // Moves tiles of keys and of values into LDS.
-template <int KV, int HD, int WAVES>
+template <int KV, int HD, int WAVES, int BUFFERS>
 struct TileLoader {
-  using Shared = TileShared<KV, HD, WAVES>;
+  using Shared = TileShared<KV, HD, WAVES, BUFFERS>;
   static constexpr int THREADS = 64 * WAVES, kHalf = kv_half_bytes<KV, HD>(), ROWB = HD * 2;
   // The chunks of key row `row` are exchanged with this: eight lanes that read together, rows 0 .. 3 and 8 .. 11 or the like, take eight
   // different ones of the eight places that 32 banks have.  Linear: of rows without a common bit it is that of each, exclusive or.
@@ -260,6 +320,81 @@ struct TileLoader {
     }
     __builtin_amdgcn_wave_barrier();
   }
+
+  // Trees: codes of a block in LDS, expanded; what its values are scaled by is known.
+  __device__ __forceinline__ static void expand_keys(Shared& sh, const char* block) {
+    const int tid = thread(), token = tid >> 2, g = tid & 3;
+    const u32x4* from = reinterpret_cast<const u32x4*>(block + tid * (KW * 4));
+    uint32_t d[KW];
+    if constexpr (KW % 4 == 0) {
+#pragma unroll
+      for (int j = 0; j < KW; j += 4) *reinterpret_cast<u32x4*>(&d[j]) = from[j / 4];
+    } else {
+      *reinterpret_cast<u32x2*>(&d[0]) = *reinterpret_cast<const u32x2*>(block + tid * (KW * 4));
+    }
+    char* to = sh.keys[0] + token * ROWB;
+#pragma unroll
+    for (int w = 0; w < HD / 32; ++w) {
+      bf16x8 out;
+      if constexpr (KV == kKvU4) out = spread_nibbles<16>(d[w]);
+      else out = spread_bytes(d[2 * w], d[2 * w + 1]);
+      *reinterpret_cast<bf16x8*>(to + (((4 * w + g) ^ exchange(token)) << 4)) = out;
+    }
+  }
+  __device__ __forceinline__ static void expand_values(Shared& sh, const char* block, const TileParams& p) {
+    const int tid = thread();
+    constexpr float centre = KV == kKvU4 ? 8.f : 128.f;
+    const f16x2 bias = {(_Float16)(-1024.f - centre), (_Float16)(-1024.f - centre)};  // (1024 + c - 1024 - centre: exact)
+    auto half2 = [](uint32_t x) { return __builtin_bit_cast(f16x2, x); };
+    const int g = tid & 3;  // (a thread's pieces are of the same tokens)
+    u32x4 d[VP], s8[2], b8[2];
+#pragma unroll
+    for (int i = 0; i < VP; ++i)
+      if ((i + 1) * THREADS <= VROWS * 4 || tid + i * THREADS < VROWS * 4) d[i] = *reinterpret_cast<const u32x4*>(block + kHalf + (tid + i * THREADS) * 16);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      s8[h] = reinterpret_cast<const u32x4*>(&p.step[16 * g])[h];
+      b8[h] = reinterpret_cast<const u32x4*>(&p.middle[16 * g])[h];
+    }
+#pragma unroll
+    for (int i = 0; i < VP; ++i) {
+      if ((i + 1) * THREADS > VROWS * 4 && tid + i * THREADS >= VROWS * 4) break;
+      const int row = (tid + i * THREADS) >> 2;
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int n = 0; n < (KV == kKvU4 ? 2 : 1); ++n) {
+          u32x4 out;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {  // of four tokens in a dword, the first and third, then the others
+            constexpr uint32_t kMask = KV == kKvU4 ? 0x000f000fu : 0x00ff00ffu;
+            const uint32_t x = (d[i][2 * h + (j >> 1)] >> (8 * (j & 1) + 4 * n) & kMask) | 0x64006400u;  // fp16 1024 + c
+            out[j] = __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(half2(x) + bias, half2(s8[h][j]), half2(b8[h][j])));
+          }
+          const int f = KV == kKvU4 ? (row >> 4) * 32 + 16 * n + (row & 15) : row;
+          *reinterpret_cast<u32x4*>(sh.values[0] + f * 128 + (((2 * g + h) ^ (f & 7)) << 4)) = out;
+        }
+    }
+  }
+  // By one wave: the parameters of a block in LDS.  each: as asked for; there, c: as in put_keys.
+  __device__ __forceinline__ void find_params(TileParams& p, const char* block, int there, bool each, float c) {
+    const int lane = thread() & 63, at = (lane & ~3) | (lane & 1) << 1 | (lane & 2) >> 1;
+    constexpr float centre = KV == kKvU4 ? 8.f : 128.f;
+    kp = reinterpret_cast<const float2*>(block + 2 * kHalf)[lane];
+    vp = reinterpret_cast<const float2*>(block + 2 * kHalf)[kBlockTokens + lane];
+    p.par[lane] = lane < there ? make_float2(kp.x * c, kp.y * c) : make_float2(0.f, 0.f);
+    bool bad;
+    const float most = largest_value(lane, there, bad);
+    const unsigned long long odd = __ballot(bad);
+    const float vs = bad || lane >= there ? 0.f : vp.x, vb = bad || lane >= there ? 0.f : vp.y;
+    const int mine = power_of(most), largest = wave_max(mine);
+    each = each || __any(most > 0.f && mine + 6 < largest);
+    if (each) p.power[lane] = (float)mine;
+    const float f = __uint_as_float((unsigned)(253 - (each ? mine : largest)) << 23);
+    p.step[at] = (_Float16)(vs * f);
+    p.middle[at] = (_Float16)(fmaf(centre, vs, vb) * f);
+    if (lane == 0) *reinterpret_cast<int4*>(&p.v_exp) = int4{each ? 0 : largest, each, (int)(uint32_t)odd, (int)(uint32_t)(odd >> 32)};
+  }
 };
 
 // N products in order, `product(n, operand)`, each with an operand from LDS, `read(n)`, that is asked for kAhead products earlier: left to itself
@@ -295,21 +430,26 @@ struct TileState {
   int base;       // the sequence's first token in it; negative: of the prefix
 };
 
-// PREFIX: the rows of all tokens over the prefix alone, split over its tiles, to prefix_part; else the list.  TREE: as in kt_attention.h.
+// PREFIX: the rows of all tokens over the prefix alone, split over its tiles, to prefix_part; else the list.  TREE: as in kt_attention.h; a tree
+// has as many rows as it has, so that waves without any leave the products to the others.
 template <int KV, int HD, int WAVES, bool PREFIX, bool TREE>
 __global__ __launch_bounds__(64 * WAVES, HD == 256 && WAVES == 4 ? 1 : 2) void attend_tiles_kernel(TileArgs t) {
   constexpr int R = 32 * WAVES, TD = HD / 32, KS = HD / 16;
   constexpr bool Q16 = KV != kKvBf16;  // quantised: p and the values in fp16
   constexpr int kUp = Q16 ? 7 : 0;     // p enters times 2^kUp: at most 2^15
   using frag = std::conditional_t<Q16, f16x8, bf16x8>;
-  using Loader = TileLoader<KV, HD, WAVES>;
+  constexpr bool RING = TREE && Q16;   // blocks go to LDS as they are, several ahead, and are expanded from there between two barriers
+  using Loader = TileLoader<KV, HD, WAVES, RING ? 1 : 2>;
   using Shared = typename Loader::Shared;
   extern __shared__ __align__(16) char lds[];
   Shared& sh = *reinterpret_cast<Shared*>(lds);
+  [[maybe_unused]] TileParams* const params = reinterpret_cast<TileParams*>(lds + sizeof(Shared));  // RING: of the tile at hand and of the next
+  [[maybe_unused]] int* const cum = reinterpret_cast<int*>(lds + tiles_lds<KV, HD, WAVES, TREE>());  // TREE
   constexpr float kNone = -__builtin_inff();
   const AttendArgs& a = t.a;
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), r = lane & 31, h = lane >> 5, heads = a.cache.n_heads;
   const int page_blocks = a.cache.log2_page - 6, prefix_tiles = (int)(((unsigned)t.prefix_len + 63) >> 6);
+  const int rows0 = 32 * wave;
   const float c = a.scale * 1.44269504f;
 
   int me, begin, end, per = 0, one = 0;
@@ -319,8 +459,14 @@ __global__ __launch_bounds__(64 * WAVES, HD == 256 && WAVES == 4 ? 1 : 2) void a
     end = 1;
   } else {
     me = (blockIdx.x & 7) * (t.workers >> 3) + (blockIdx.x >> 3);
-    one = t.list[t.entries].x;
+    if constexpr (TREE) {
+      list_trees<R, 64 * WAVES>(t, cum);
+      one = uniform(cum[a.n_seq]);
+    } else {
+      one = t.list[t.entries].x;
+    }
     per = piece_length(one * heads, t.workers);
+    if constexpr (TREE) per = max(per, 3);  // (joined pieces of a tile each cost more than they save)
     begin = me * per;
     end = min(begin + per, one * heads);
   }
@@ -344,6 +490,15 @@ __global__ __launch_bounds__(64 * WAVES, HD == 256 && WAVES == 4 ? 1 : 2) void a
     } else {
       head = (int)((unsigned)u / (unsigned)one);
       in = u - head * one;
+      int s, at, all;
+      if constexpr (TREE) {
+        s = uniform(sequence_at(cum, a.n_seq, in));
+        const Sequence mine = sequence_of(a, s);
+        all = uniform(tree_units(t, mine));
+        row_tile = uniform((int)((unsigned)(in - uniform(cum[s])) / (unsigned)all));
+        at = uniform(cum[s]) + row_tile * all;
+        entry = s;
+      } else {
       // the entry that place `in` of a head's list is in: looked for once, then the next ones in turn
       if (entry < 0) {
         int lo = 0, hi = t.entries - 1;
@@ -357,8 +512,9 @@ __global__ __launch_bounds__(64 * WAVES, HD == 256 && WAVES == 4 ? 1 : 2) void a
       int4 item = t.list[entry];
       while (item.x + item.w <= in) item = t.list[++entry];
       entry = uniform(entry);
-      const int s = uniform(item.y), at = uniform(item.x), all = uniform(item.w);
+      s = uniform(item.y), at = uniform(item.x), all = uniform(item.w);
       row_tile = uniform(item.z);
+      }
       q = sequence_of(a, s);
       pages = a.pages + s * a.ldp;
       tiles = all - kSegmentCost;
@@ -372,7 +528,7 @@ __global__ __launch_bounds__(64 * WAVES, HD == 256 && WAVES == 4 ? 1 : 2) void a
       }
     }
     // this lane's row
-    const int64_t row = (int64_t)row_tile * R + 32 * wave + r;
+    const int64_t row = (int64_t)row_tile * R + rows0 + r;
     const bool live = row < (int64_t)q.count * a.group;
     const int in_seq = live ? (int)(row / a.group) : 0, qh = head * a.group + (live ? (int)(row - (int64_t)in_seq * a.group) : 0);
     const int64_t token = q.first + in_seq;
@@ -456,13 +612,14 @@ __global__ __launch_bounds__(64 * WAVES, HD == 256 && WAVES == 4 ? 1 : 2) void a
 #pragma unroll
       for (int k = 0; k < 2; ++k)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) x[k][e] = KV == kKvU4 ? -128.f * qsum : 0.f;  // (codes of 4 bits enter as 128 + c)
+        for (int e = 0; e < 16; ++e) x[k][e] = KV == kKvU4 ? (RING ? -16.f : -128.f) * qsum : 0.f;  // (codes of 4 bits enter as 128 + c, or 16 + c)
     };
     // scores 2 i, 2 i + 1, in bits, from products
     auto finish_scores = [&](f32x16(&x)[2], int at, int i) {
       const int k = i >> 3, e = 2 * (i & 7);
       if constexpr (Q16) {
-        const float4 p = *reinterpret_cast<const float4*>(&sh.par[at][32 * k + 16 * (e >> 3) + 8 * h + (e & 7)]);
+        const float2* par = RING ? params[at].par : sh.par[at];
+        const float4 p = *reinterpret_cast<const float4*>(&par[32 * k + 16 * (e >> 3) + 8 * h + (e & 7)]);
         x[k][e] = fmaf(x[k][e], p.x, p.y * qsum);
         x[k][e + 1] = fmaf(x[k][e + 1], p.z, p.w * qsum);
       } else {
@@ -490,7 +647,8 @@ __global__ __launch_bounds__(64 * WAVES, HD == 256 && WAVES == 4 ? 1 : 2) void a
 
     // bf16: the i-th of 2 STEPS pieces that a wave copies of a tile, keys first
     const int copy_at = uniform(wave * Loader::STEPS * 1024);
-    auto copy = [&](int64_t block, int at, int i) {
+    auto copy = [&](int64_t block, int at, int i, bool more = true) {
+      if (TREE && !more) return;
       const bool key = i < Loader::STEPS;
       const int j = key ? i : i - Loader::STEPS, from = key ? Loader::key_source() ^ Loader::key_turn(j) : Loader::value_source();
       to_lds_16(from + 1024 * j, a.cache.data + block, uniform((int)(uintptr_t)(key ? sh.keys[at] : sh.values[at]) + copy_at + 1024 * j));
@@ -512,8 +670,50 @@ __global__ __launch_bounds__(64 * WAVES, HD == 256 && WAVES == 4 ? 1 : 2) void a
       if (lane == 0) sh.odd[at][wave] = all;
     };
 
-    TileState now = state_of(first);
+    const bool idle = TREE && (int64_t)row_tile * R + rows0 >= (int64_t)q.count * a.group;  // (of the wave)
+
+    // RING: a block comes in pieces of a KiB, every fourth of them a wave's
+    constexpr int AHEAD = ring_blocks<KV, HD>(), PIECES = kv_block_bytes<KV, HD>() / 1024;
+    [[maybe_unused]] TileState queue[AHEAD];  // the tiles from the next on
+    auto slot = [&](int tile) { return lds + sizeof(Shared) + 2 * sizeof(TileParams) + ((tile - first) & (AHEAD - 1)) * kv_block_bytes<KV, HD>(); };
+    auto fetch = [&](const TileState& x, int tile) {
+      const unsigned to = (unsigned)(uintptr_t)slot(tile);
+#pragma unroll
+      for (int i = 0; i < (PIECES + WAVES - 1) / WAVES; ++i) {
+        const int piece = PIECES - WAVES + wave - WAVES * i;  // (the last one, the parameters, is the last wave's)
+        if (piece >= 0) to_lds_16((Loader::thread() & 63) * 16 + piece * 1024, a.cache.data + x.block, uniform((int)(to + piece * 1024)));
+      }
+    };
+    // waits for a tile's block: those behind it may still be under way
+    auto arrived = [&](int tile) {
+      if (tile + AHEAD <= last) {
+        constexpr int LESS = PIECES / WAVES, MORE = LESS + 1;
+        if (wave >= WAVES - PIECES % WAVES) asm volatile("s_waitcnt vmcnt(%0)" ::"n"((AHEAD - 1) * MORE) : "memory");
+        else asm volatile("s_waitcnt vmcnt(%0)" ::"n"((AHEAD - 1) * LESS) : "memory");
+      } else {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      }
+    };
+
+    TileState now = state_of(first), next = now;
+    if constexpr (RING) {
+#pragma unroll
+      for (int i = 0; i + 1 < AHEAD; ++i) queue[i] = first + 1 + i < last ? state_of(first + 1 + i) : now;
+    }
     __syncthreads();  // the buffers are free (the last segment's tiles were read)
+    if constexpr (RING) {
+      // (queries first, so that a wait for them is none for the blocks)
+#pragma unroll
+      for (int w = 0; w < KS; ++w) asm volatile("" : "+v"(qf[w]));
+      fetch(now, first);
+#pragma unroll
+      for (int i = 0; i + 1 < AHEAD; ++i)
+        if (first + 1 + i < last) fetch(queue[i], first + 1 + i);
+      if (wave == WAVES - 1) {
+        arrived(first);
+        ld.find_params(params[first & 1], slot(first), now.there, masked_of(now), c);
+      }
+    } else {
     if constexpr (Q16) {
       ld.ask_keys(a.cache.data + now.block);
       ld.ask_values(a.cache.data + now.block);
@@ -531,16 +731,45 @@ __global__ __launch_bounds__(64 * WAVES, HD == 256 && WAVES == 4 ? 1 : 2) void a
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     if (!Q16 && masked_of(now)) clean(now, 0);
     __syncthreads();
+    }
 
     for (int tile = first; tile < last; ++tile) {
-      const int at = tile - first & 1;
-      const TileState next = state_of(tile + 1);
-      if constexpr (Q16) {
+      const int at = RING ? 0 : tile - first & 1;
+      if constexpr (RING) {
+        arrived(tile);
+        __syncthreads();  // ... at every wave; the tile before is used up
+        const TileParams& p = params[tile & 1];
+        const int4 found = *reinterpret_cast<const int4*>(&p.v_exp);
+        Loader::expand_keys(sh, slot(tile));
+        Loader::expand_values(sh, slot(tile), p);
+        v_exp = uniform(found.x);
+        each = uniform(found.y) != 0;
+        odd = (unsigned long long)(uint32_t)uniform(found.w) << 32 | (uint32_t)uniform(found.z);
+        __syncthreads();
+        queue[AHEAD - 1] = now;
+        if (tile + AHEAD < last) {
+          queue[AHEAD - 1] = state_of(tile + AHEAD);
+          fetch(queue[AHEAD - 1], tile + AHEAD);
+        }
+        if (wave == WAVES - 1 && tile + 1 < last) {
+          arrived(tile + 1);
+          ld.find_params(params[tile + 1 & 1], slot(tile + 1), queue[0].there, masked_of(queue[0]), c);
+        }
+      } else {
+        next = state_of(tile + 1);
+      }
+      if constexpr (Q16 && !RING) {
         ld.ask_keys(a.cache.data + next.block);
         ld.ask_values(a.cache.data + next.block);
       }
       [[maybe_unused]] int v_next = 0;
       [[maybe_unused]] bool each_next = false;
+      if (idle) {
+        if constexpr (!Q16) {
+#pragma unroll
+          for (int i = 0; i < 2 * Loader::STEPS; ++i) copy(next.block, at ^ 1, i, tile + 1 < last);
+        }
+      } else {
       f32x16 x[2];
       clear(x);
       {
@@ -549,15 +778,15 @@ __global__ __launch_bounds__(64 * WAVES, HD == 256 && WAVES == 4 ? 1 : 2) void a
                           [&](int n) {
                             if constexpr (!Q16) {
                               constexpr int EVERY = KS / Loader::STEPS;
-                              if (n % EVERY == 0) copy(next.block, at ^ 1, n / EVERY);
-                            } else if (n == 2 * KS - 5) {  // (the chunk: 290 us four products from the end, 280 five, 282 six, 285 eight)
+                              if (n % EVERY == 0) copy(next.block, at ^ 1, n / EVERY, tile + 1 < last);
+                            } else if (!RING && n == 2 * KS - 5) {  // (the chunk: 290 us four products from the end, 280 five, 282 six, 285 eight)
                               each_next = masked_of(next);
                               v_next = ld.look(next.there, each_next);
                             }
                           });
       }
 #pragma unroll
-      for (int i = 0; i < 16; ++i) finish_scores(x, at, i);
+      for (int i = 0; i < 16; ++i) finish_scores(x, RING ? tile & 1 : at, i);
       if (masked_of(now)) mask(x, now);
       float most = largest(x);
       auto of_halves = [](float v) {
@@ -573,7 +802,7 @@ __global__ __launch_bounds__(64 * WAVES, HD == 256 && WAVES == 4 ? 1 : 2) void a
         const float up = most - m;  // not a number where nothing has been seen yet
         float size = (float)v_exp, alone = 0.f;
         if (each) {  // p alone for its sum, and with the token's exponent
-          const float* power = &sh.power[at][8 * h];
+          const float* power = (RING ? params[tile & 1].power : sh.power[at]) + 8 * h;
           const float base = most == kNone ? 0.f : most;
           size = kNone;
 #pragma unroll
@@ -610,7 +839,7 @@ __global__ __launch_bounds__(64 * WAVES, HD == 256 && WAVES == 4 ? 1 : 2) void a
       float sum[2] = {0.f, 0.f}, even = 0.f;
       auto exponential = [&](int i) {
         const int k = i >> 4, e = i & 15;
-        const float v = __builtin_amdgcn_exp2f(x[k][e] - mb);
+        const float v = __builtin_amdgcn_exp2f(x[k][RING ? (e & ~3) | (e & 1) << 1 | (e & 2) >> 1 : e] - mb);
         sum[e & 1] += v;
         if constexpr (!Q16) pf[2 * k + (e >> 3)][e & 7] = (bf16)v;
         else if (e & 1) put_pair(pf[2 * k + (e >> 3)], e & 6, even, v);
@@ -631,6 +860,7 @@ __global__ __launch_bounds__(64 * WAVES, HD == 256 && WAVES == 4 ? 1 : 2) void a
       const float all = sum[0] + sum[1];
       if constexpr (!Q16) l += all;
       else if (!each) l += ldexpf(all, -shift);
+      }
       if constexpr (!Q16) {
         odd = 0ull;
         if (masked_of(now)) {
@@ -661,6 +891,11 @@ __global__ __launch_bounds__(64 * WAVES, HD == 256 && WAVES == 4 ? 1 : 2) void a
           }
         }
       }
+      if constexpr (RING) {
+        now = queue[0];
+#pragma unroll
+        for (int i = 0; i + 1 < AHEAD; ++i) queue[i] = queue[i + 1];
+      } else {
       if constexpr (Q16) {
         ld.put_keys(sh, at ^ 1, next.there, c);
         each = each_next;
@@ -668,9 +903,10 @@ __global__ __launch_bounds__(64 * WAVES, HD == 256 && WAVES == 4 ? 1 : 2) void a
         ld.put_values(sh, at ^ 1, next.there, v_exp, each, odd);
       }
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-      if (!Q16 && masked_of(next)) clean(next, at ^ 1);
+      if (!Q16 && (!TREE || tile + 1 < last) && masked_of(next)) clean(next, at ^ 1);
       __syncthreads();
       now = next;
+      }
     }
 
     l += __shfl_xor(l, 32);
@@ -699,7 +935,7 @@ __global__ __launch_bounds__(64 * WAVES, HD == 256 && WAVES == 4 ? 1 : 2) void a
           }
         if (a.lse && h == 0) a.lse[token * a.hq + qh] = l == 0.f ? kNone : (m + __log2f(l)) * 0.693147181f;
       } else {
-        const int64_t slot = PREFIX ? (split * (int64_t)a.n_tokens + token) * a.hq + qh : (int64_t)(2 * me + (first ? 0 : 1)) * R + 32 * wave + r;
+        const int64_t slot = PREFIX ? (split * (int64_t)a.n_tokens + token) * a.hq + qh : (int64_t)(2 * me + (first ? 0 : 1)) * R + rows0 + r;
         float* to = (PREFIX ? t.prefix_part : t.part) + slot * HD + 4 * h;
 #pragma unroll
         for (int i = 0; i < TD; ++i)
@@ -710,7 +946,11 @@ __global__ __launch_bounds__(64 * WAVES, HD == 256 && WAVES == 4 ? 1 : 2) void a
       }
     }
     if constexpr (PREFIX) break;
-    if (first == 0 && !whole) cut = int4{entry, head, (int)((unsigned)(u + (tiles - first) + (units - (last - first)) - 1) / (unsigned)per) - me + 1, 0};
+    if (first == 0 && !whole)
+    {
+      const int pieces = (int)((unsigned)(u + (tiles - first) + (units - (last - first)) - 1) / (unsigned)per) - me + 1;
+      cut = TREE ? int4{q.first, row_tile * R, pieces << 9 | (int)min((int64_t)q.count * a.group - (int64_t)row_tile * R, (int64_t)R), head} : int4{entry, head, pieces, 0};
+    }
     u += units;
     if (in + units == one) entry = 0;
   }
@@ -739,26 +979,44 @@ struct Joined {
 };
 
 // The cut segments of the list: HD / 4 threads a row, grid (workers, R HD / 1024).
-template <int HD, int R>
+template <int HD, int R, bool TREE>
 __global__ __launch_bounds__(256) void join_tiles_kernel(TileArgs t) {
   constexpr int TR = HD / 4;
   const int me = blockIdx.x;
   const int4 cut = t.cuts[me];
   if (cut.z == 0) return;
   const AttendArgs& a = t.a;
-  const int4 entry = t.list[cut.x];
-  const Sequence q = sequence_of(a, entry.y);
   const int r = blockIdx.y * (256 / TR) + threadIdx.x / TR, lane4 = 4 * (threadIdx.x % TR);
-  const int64_t row = (int64_t)entry.z * R + r;
-  if (row >= (int64_t)q.count * a.group) return;
+  int first, head, pieces;
+  int64_t row;
+  if constexpr (TREE) {
+    first = cut.x, head = cut.w, pieces = cut.z >> 9, row = (int64_t)cut.y + r;
+    if (r >= (cut.z & 511)) return;
+  } else {
+    const int4 entry = t.list[cut.x];
+    const Sequence q = sequence_of(a, entry.y);
+    first = q.first, head = cut.y, pieces = cut.z, row = (int64_t)entry.z * R + r;
+    if (row >= (int64_t)q.count * a.group) return;
+  }
   const float2* ml = reinterpret_cast<const float2*>(t.part + (int64_t)2 * t.workers * R * HD);
+  constexpr int kAtOnce = 4;  // pieces that are asked for together
   Joined j;
-  for (int k = 0; k < cut.z; ++k) {
-    const int64_t slot = (2 * ((int64_t)me + k) + (k ? 0 : 1)) * R + r;
-    j.add(ml[slot], *reinterpret_cast<const f32x4*>(t.part + slot * HD + lane4));
+  for (int k = 0; k < pieces; k += kAtOnce) {
+    float2 d[kAtOnce];
+    f32x4 v[kAtOnce];
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i) {
+      const int piece = min(k + i, pieces - 1);
+      const int64_t slot = (2 * ((int64_t)me + piece) + (piece ? 0 : 1)) * R + r;
+      d[i] = ml[slot];
+      v[i] = *reinterpret_cast<const f32x4*>(t.part + slot * HD + lane4);
+    }
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i)
+      if (k + i < pieces) j.add(d[i], v[i]);
   }
   const int in_seq = (int)(row / a.group);
-  j.store(a, q.first + in_seq, cut.y * a.group + (int)(row - (int64_t)in_seq * a.group), HD, lane4);
+  j.store(a, first + in_seq, head * a.group + (int)(row - (int64_t)in_seq * a.group), HD, lane4);
 }
 
 // Every row of a batch of single tokens behind a prefix: its own pieces (kt_attention.h) and those over the prefix.  HD / 4 threads a row.

@@ -5,7 +5,6 @@ import numpy as np
 import torch
 
 import paper_2503_01483_amd as kt
-from attention_bounds import few
 from serving_util import TOP
 
 FORMATS = [kt.KT_KV_BF16, kt.KT_KV_U8, kt.KT_KV_U4]
@@ -14,6 +13,11 @@ NAMES = {kt.KT_KV_BF16: "bf16", kt.KT_KV_U8: "u8", kt.KT_KV_U4: "u4"}
 
 def ints(v):
     return torch.as_tensor(np.asarray(v), dtype=torch.int32).cuda()
+
+
+def few(b, max_q):
+    """Whether trees of up to max_q queries are computed by waves (p times the step to 16 bits) or as many rows are."""
+    return max_q * (b.hq // b.hkv) <= {kt.KT_KV_BF16: 0, kt.KT_KV_U8: 32, kt.KT_KV_U4: 64}[b.fmt]
 
 
 def random_tree(count, rng, wide=7):
