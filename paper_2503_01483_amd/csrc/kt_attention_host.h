@@ -102,7 +102,7 @@ static kt_status attend(const kt_kv_cache* cache, const void* Q, int64_t ldq, kt
   if (prefix_len < 0 || prefix_len > kMaxTokens || (prefix_len && !prefix_pages))
     return fail(KT_ERR_INVALID_ARG, "prefix_len must be in [0, 2^30], with prefix_pages");
   if (TREE && !tree) return fail(KT_ERR_INVALID_ARG, "tree must not be null");
-  if (TREE && (ldt < ceil_div(max_q, 64) || ldt > ((int64_t)1 << 24) || misaligned(tree, 8)))
+  if (TREE && (ldt < 1 || ldt > ((int64_t)1 << 24) || max_q > 64 * ldt || misaligned(tree, 8)))
     return fail(KT_ERR_BAD_SHAPE, "ldt must be in [ceil(max_q / 64), 2^24], tree 8-byte aligned");
   if (!(scale > 0.f) || !(scale <= kHuge)) return fail(KT_ERR_INVALID_ARG, "scale must be positive and finite");
   const size_t need = kt_paged_attention_bytes(n_tokens, n_q_heads, hd, prefix_len);
@@ -161,34 +161,31 @@ static kt_status attend(const kt_kv_cache* cache, const void* Q, int64_t ldq, kt
   hipStream_t st = static_cast<hipStream_t>(stream);
   const bool ok = with_cache(cache, [&](auto kv, auto h) {
     constexpr int KV = decltype(kv)::value, HD = decltype(h)::value, kRowsOf = 1024 / HD, ROWS = tile_rows(HD);  // (rows of a workgroup that joins)
-    if (!few) {
-      auto go = [&](auto waves) {
-        constexpr int WAVES = decltype(waves)::value, R = 32 * WAVES;
-        if constexpr (TREE) {
-          t.workers = kTileWorkers * ROWS / R;
-          a.row_tiles = (int)ceil_div(max_q * group, R);
-        } else {
-          plan_tiles_kernel<R><<<1, 1024, 0, st>>>(t);
-        }
-        if (!launch_tiles<KV, HD, WAVES, false, TREE>(t, t.workers, st)) return false;
-        join_tiles_kernel<HD, R, TREE><<<dim3((unsigned)t.workers, R / kRowsOf), 256, 0, st>>>(t);
+    if constexpr (!TREE || KV != kKvBf16) {  // (no tree over bf16 has few rows)
+      if (few) {
+        if (prefix_len && !launch_tiles<KV, HD, tile_waves(HD), true, false>(t, ceil_div(n_tokens * group, ROWS) * cache->n_heads * t.splits, st)) return false;
+        attend_rows_kernel<KV, HD, TREE><<<dim3(kWaveWorkers / 4), 256, (size_t)(n_seq + 1) * 4, st>>>(a);
+        if (prefix_len) join_prefix_kernel<HD><<<dim3((unsigned)ceil_div(n_tokens * n_q_heads, kRowsOf)), 256, 0, st>>>(t);
+        else attend_join_kernel<HD><<<dim3(kWaveWorkers, 4), 256, 0, st>>>(a);
         return true;
-      };
-      if constexpr (TREE && KV != kKvBf16) {
-        return go(std::integral_constant<int, 4>{});
-      } else {
-        if (TREE && max_q * group <= 128) return go(std::integral_constant<int, 4>{});
-        return go(std::integral_constant<int, tile_waves(HD)>{});
       }
     }
-    if constexpr (TREE && KV == kKvBf16) return false;  // (no tree takes this)
-    else {
-    if (prefix_len && !launch_tiles<KV, HD, tile_waves(HD), true, false>(t, ceil_div(n_tokens * group, ROWS) * cache->n_heads * t.splits, st)) return false;
-    attend_rows_kernel<KV, HD, TREE><<<dim3(kWaveWorkers / 4), 256, (size_t)(n_seq + 1) * 4, st>>>(a);
-    if (prefix_len) join_prefix_kernel<HD><<<dim3((unsigned)ceil_div(n_tokens * n_q_heads, kRowsOf)), 256, 0, st>>>(t);
-    else attend_join_kernel<HD><<<dim3(kWaveWorkers, 4), 256, 0, st>>>(a);
-    return true;
-    }
+    auto go = [&](auto waves) {
+      constexpr int WAVES = decltype(waves)::value, R = 32 * WAVES;
+      if constexpr (TREE) {
+        t.workers = kTileWorkers * ROWS / R;
+        a.row_tiles = (int)std::min<int64_t>(ceil_div(max_q * group, R), INT32_MAX);
+      } else {
+        plan_tiles_kernel<R><<<1, 1024, 0, st>>>(t);
+      }
+      if (!launch_tiles<KV, HD, WAVES, false, TREE>(t, t.workers, st)) return false;
+      join_tiles_kernel<HD, R, TREE><<<dim3((unsigned)t.workers, R / kRowsOf), 256, 0, st>>>(t);
+      return true;
+    };
+    using std::integral_constant;
+    if constexpr (TREE && KV != kKvBf16) return go(integral_constant<int, 4>{});
+    else if constexpr (TREE) return max_q * group <= 128 ? go(integral_constant<int, 4>{}) : go(integral_constant<int, tile_waves(HD)>{});
+    else return go(integral_constant<int, tile_waves(HD)>{});
   });
   if (!ok) return fail(KT_ERR_DEVICE, "attention kernel needs more LDS than the device gives");
   return launch_ok() ? KT_OK : fail(KT_ERR_DEVICE, "attention kernel launch failed");

@@ -22,6 +22,12 @@
 // once they are passed by 2^8 (p, and p times the power of two, stay below 256).  In fp16 p goes in times 2^7: it is rounded to 2^-31 of the row's largest
 // p |v| at worst, and a million tokens of it do not show in a result.
 //
+// Trees (TREE) have few rows a sequence, all of which go through all of its tokens.  Their workgroups have four waves (bf16, many rows: eight), two of
+// them to a compute unit; a wave without rows copies and expands for the others.  Quantised blocks go to LDS as they are, two (u8) or four (u4) on their
+// way, and are expanded from there between two barriers, in place of a second buffer; one wave finds the parameters of the next block while the others compute.  The
+// list is worked out by every workgroup for itself.  32 trees of up to 64 drafts behind 8192, 32 + 2 x 8 heads of 128, 4 bits: 254 us, 430 TFLOP/s, of which a
+// wave spends 19 % on expanding, 34 % on exponentials and the products of the values, 25 % in front of barriers; 4 of 16 behind 65536, 8 bits: 158 us, 2.6 TB/s.
+//
 // All key tiles of all row tiles form one list, heads outermost; each workgroup takes an equal piece, neighbouring pieces on one XCD, whose
 // L2 then holds the keys of few heads.  Segments that are cut are joined by a second launch.
 #pragma once
@@ -499,21 +505,21 @@ __global__ __launch_bounds__(64 * WAVES, HD == 256 && WAVES == 4 ? 1 : 2) void a
         at = uniform(cum[s]) + row_tile * all;
         entry = s;
       } else {
-      // the entry that place `in` of a head's list is in: looked for once, then the next ones in turn
-      if (entry < 0) {
-        int lo = 0, hi = t.entries - 1;
-        while (lo < hi) {
-          const int mid = (lo + hi + 1) >> 1;
-          if (t.list[mid].x <= in) lo = mid;
-          else hi = mid - 1;
+        // the entry that place `in` of a head's list is in: looked for once, then the next ones in turn
+        if (entry < 0) {
+          int lo = 0, hi = t.entries - 1;
+          while (lo < hi) {
+            const int mid = (lo + hi + 1) >> 1;
+            if (t.list[mid].x <= in) lo = mid;
+            else hi = mid - 1;
+          }
+          entry = uniform(lo);
         }
-        entry = uniform(lo);
-      }
-      int4 item = t.list[entry];
-      while (item.x + item.w <= in) item = t.list[++entry];
-      entry = uniform(entry);
-      s = uniform(item.y), at = uniform(item.x), all = uniform(item.w);
-      row_tile = uniform(item.z);
+        int4 item = t.list[entry];
+        while (item.x + item.w <= in) item = t.list[++entry];
+        entry = uniform(entry);
+        s = uniform(item.y), at = uniform(item.x), all = uniform(item.w);
+        row_tile = uniform(item.z);
       }
       q = sequence_of(a, s);
       pages = a.pages + s * a.ldp;
@@ -714,23 +720,23 @@ __global__ __launch_bounds__(64 * WAVES, HD == 256 && WAVES == 4 ? 1 : 2) void a
         ld.find_params(params[first & 1], slot(first), now.there, masked_of(now), c);
       }
     } else {
-    if constexpr (Q16) {
-      ld.ask_keys(a.cache.data + now.block);
-      ld.ask_values(a.cache.data + now.block);
-      ld.put_keys(sh, 0, now.there, c);
-      each = masked_of(now);
-      v_exp = ld.look(now.there, each);
-      ld.put_values(sh, 0, now.there, v_exp, each, odd);
-    } else {
+      if constexpr (Q16) {
+        ld.ask_keys(a.cache.data + now.block);
+        ld.ask_values(a.cache.data + now.block);
+        ld.put_keys(sh, 0, now.there, c);
+        each = masked_of(now);
+        v_exp = ld.look(now.there, each);
+        ld.put_values(sh, 0, now.there, v_exp, each, odd);
+      } else {
 #pragma unroll
-      for (int i = 0; i < 2 * Loader::STEPS; ++i) copy(now.block, 0, i);
-    }
-    // queries arrived before the loop: a wait for them in it would wait for the tiles that are on their way to LDS as well
+        for (int i = 0; i < 2 * Loader::STEPS; ++i) copy(now.block, 0, i);
+      }
+      // queries arrived before the loop: a wait for them in it would wait for the tiles that are on their way to LDS as well
 #pragma unroll
-    for (int w = 0; w < KS; ++w) asm volatile("" : "+v"(qf[w]));
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    if (!Q16 && masked_of(now)) clean(now, 0);
-    __syncthreads();
+      for (int w = 0; w < KS; ++w) asm volatile("" : "+v"(qf[w]));
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      if (!Q16 && masked_of(now)) clean(now, 0);
+      __syncthreads();
     }
 
     for (int tile = first; tile < last; ++tile) {
@@ -770,96 +776,96 @@ __global__ __launch_bounds__(64 * WAVES, HD == 256 && WAVES == 4 ? 1 : 2) void a
           for (int i = 0; i < 2 * Loader::STEPS; ++i) copy(next.block, at ^ 1, i, tile + 1 < last);
         }
       } else {
-      f32x16 x[2];
-      clear(x);
-      {
-        const int place = key_place();
-        pipelined<2 * KS>([&](int n) { return key_operand(place, at, n); }, [&](int n, bf16x8 f) { x[n & 1] = mfma32(f, qf[n >> 1], x[n & 1]); },
-                          [&](int n) {
-                            if constexpr (!Q16) {
-                              constexpr int EVERY = KS / Loader::STEPS;
-                              if (n % EVERY == 0) copy(next.block, at ^ 1, n / EVERY, tile + 1 < last);
-                            } else if (!RING && n == 2 * KS - 5) {  // (the chunk: 290 us four products from the end, 280 five, 282 six, 285 eight)
-                              each_next = masked_of(next);
-                              v_next = ld.look(next.there, each_next);
-                            }
-                          });
-      }
-#pragma unroll
-      for (int i = 0; i < 16; ++i) finish_scores(x, RING ? tile & 1 : at, i);
-      if (masked_of(now)) mask(x, now);
-      float most = largest(x);
-      auto of_halves = [](float v) {
-        const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-        return fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1]));
-      };
-      most = of_halves(most);
-      int shift = 0;
-      if constexpr (Q16) {
-        // O is held relative to 2^(m + v_run), the largest p |v| of the row so far, so that a large value of little weight takes no bits off the
-        // others; both parts of it are raised by the row's own scores alone.
-        // (In differences of scores throughout: a large score added to an exponent would swallow it.)
-        const float up = most - m;  // not a number where nothing has been seen yet
-        float size = (float)v_exp, alone = 0.f;
-        if (each) {  // p alone for its sum, and with the token's exponent
-          const float* power = (RING ? params[tile & 1].power : sh.power[at]) + 8 * h;
-          const float base = most == kNone ? 0.f : most;
-          size = kNone;
-#pragma unroll
-          for (int i = 0; i < 32; ++i) {
-            const float s = x[i >> 4][i & 15] - base, with = s + power[32 * (i >> 4) + 16 * (i >> 3 & 1) + (i & 7)];
-            alone += __builtin_amdgcn_exp2f(s);
-            size = fmaxf(size, with);
-            x[i >> 4][i & 15] = with;
-          }
-          size = of_halves(size);
+        f32x16 x[2];
+        clear(x);
+        {
+          const int place = key_place();
+          pipelined<2 * KS>([&](int n) { return key_operand(place, at, n); }, [&](int n, bf16x8 f) { x[n & 1] = mfma32(f, qf[n >> 1], x[n & 1]); },
+                            [&](int n) {
+                              if constexpr (!Q16) {
+                                constexpr int EVERY = KS / Loader::STEPS;
+                                if (n % EVERY == 0) copy(next.block, at ^ 1, n / EVERY, tile + 1 < last);
+                              } else if (!RING && n == 2 * KS - 5) {  // (the chunk: 290 us four products from the end, 280 five, 282 six, 285 eight)
+                                each_next = masked_of(next);
+                                v_next = ld.look(next.there, each_next);
+                              }
+                            });
         }
-        const bool higher = up > 8.f, raise = higher || size + up > (float)v_run + 8.f;
-        if (__any(raise)) {
-          const int run = max(v_run - (higher ? (int)fminf(up, 1024.f) : 0), (int)ceilf(fmaxf(higher ? size : size + up, -1024.f)));
-          const float shrink = raise ? __builtin_amdgcn_exp2f((float)(v_run - run) - (higher ? up : 0.f)) : 1.f;
-          l *= higher ? __builtin_amdgcn_exp2f(-up) : 1.f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) finish_scores(x, RING ? tile & 1 : at, i);
+        if (masked_of(now)) mask(x, now);
+        float most = largest(x);
+        auto of_halves = [](float v) {
+          const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+          return fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1]));
+        };
+        most = of_halves(most);
+        int shift = 0;
+        if constexpr (Q16) {
+          // O is held relative to 2^(m + v_run), the largest p |v| of the row so far, so that a large value of little weight takes no bits off the
+          // others; both parts of it are raised by the row's own scores alone.
+          // (In differences of scores throughout: a large score added to an exponent would swallow it.)
+          const float up = most - m;  // not a number where nothing has been seen yet
+          float size = (float)v_exp, alone = 0.f;
+          if (each) {  // p alone for its sum, and with the token's exponent
+            const float* power = (RING ? params[tile & 1].power : sh.power[at]) + 8 * h;
+            const float base = most == kNone ? 0.f : most;
+            size = kNone;
+#pragma unroll
+            for (int i = 0; i < 32; ++i) {
+              const float s = x[i >> 4][i & 15] - base, with = s + power[32 * (i >> 4) + 16 * (i >> 3 & 1) + (i & 7)];
+              alone += __builtin_amdgcn_exp2f(s);
+              size = fmaxf(size, with);
+              x[i >> 4][i & 15] = with;
+            }
+            size = of_halves(size);
+          }
+          const bool higher = up > 8.f, raise = higher || size + up > (float)v_run + 8.f;
+          if (__any(raise)) {
+            const int run = max(v_run - (higher ? (int)fminf(up, 1024.f) : 0), (int)ceilf(fmaxf(higher ? size : size + up, -1024.f)));
+            const float shrink = raise ? __builtin_amdgcn_exp2f((float)(v_run - run) - (higher ? up : 0.f)) : 1.f;
+            l *= higher ? __builtin_amdgcn_exp2f(-up) : 1.f;
+#pragma unroll
+            for (int i = 0; i < TD; ++i) o[i] *= shrink;
+            if (higher) m = most;
+            if (raise) v_run = run;
+          }
+          shift = max(v_exp - v_run, each ? -1000 : -60);  // (p is nothing in fp16 from 2^-60 on)
+          if (each) l += alone * (m == kNone ? 1.f : __builtin_amdgcn_exp2f(most - m + (float)kUp));
+        } else if (__any(most > m + 8.f)) {
+          const bool raise = most > m + 8.f;  // (of a row by its own scores alone)
+          const float shrink = raise ? __builtin_amdgcn_exp2f(m - most) : 1.f;
+          l *= shrink;
 #pragma unroll
           for (int i = 0; i < TD; ++i) o[i] *= shrink;
-          if (higher) m = most;
-          if (raise) v_run = run;
+          if (raise) m = most;
         }
-        shift = max(v_exp - v_run, each ? -1000 : -60);  // (p is nothing in fp16 from 2^-60 on)
-        if (each) l += alone * (m == kNone ? 1.f : __builtin_amdgcn_exp2f(most - m + (float)kUp));
-      } else if (__any(most > m + 8.f)) {
-        const bool raise = most > m + 8.f;  // (of a row by its own scores alone)
-        const float shrink = raise ? __builtin_amdgcn_exp2f(m - most) : 1.f;
-        l *= shrink;
+        const float mb = (m == kNone ? 0.f : Q16 && each ? m - most : m) - (float)(shift + kUp);
+        frag pf[4];
+        float sum[2] = {0.f, 0.f}, even = 0.f;
+        auto exponential = [&](int i) {
+          const int k = i >> 4, e = i & 15;
+          const float v = __builtin_amdgcn_exp2f(x[k][RING ? (e & ~3) | (e & 1) << 1 | (e & 2) >> 1 : e] - mb);
+          sum[e & 1] += v;
+          if constexpr (!Q16) pf[2 * k + (e >> 3)][e & 7] = (bf16)v;
+          else if (e & 1) put_pair(pf[2 * k + (e >> 3)], e & 6, even, v);
+          else even = v;
+        };
 #pragma unroll
-        for (int i = 0; i < TD; ++i) o[i] *= shrink;
-        if (raise) m = most;
-      }
-      const float mb = (m == kNone ? 0.f : Q16 && each ? m - most : m) - (float)(shift + kUp);
-      frag pf[4];
-      float sum[2] = {0.f, 0.f}, even = 0.f;
-      auto exponential = [&](int i) {
-        const int k = i >> 4, e = i & 15;
-        const float v = __builtin_amdgcn_exp2f(x[k][RING ? (e & ~3) | (e & 1) << 1 | (e & 2) >> 1 : e] - mb);
-        sum[e & 1] += v;
-        if constexpr (!Q16) pf[2 * k + (e >> 3)][e & 7] = (bf16)v;
-        else if (e & 1) put_pair(pf[2 * k + (e >> 3)], e & 6, even, v);
-        else even = v;
-      };
+        for (int i = 0; i < 8; ++i) exponential(i);
+        {
+          const int place = value_place();
+          pipelined<4 * TD>([&](int n) { return value_operand(place, at, n); }, [&](int n, frag f) { o[n % TD] = mfma32(f, pf[n / TD], o[n % TD]); },
+                            [&](int n) {  // for the next sixteen keys
+                              if (n < 3 * TD) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) exponential(i);
-      {
-        const int place = value_place();
-        pipelined<4 * TD>([&](int n) { return value_operand(place, at, n); }, [&](int n, frag f) { o[n % TD] = mfma32(f, pf[n / TD], o[n % TD]); },
-                          [&](int n) {  // for the next sixteen keys
-                            if (n < 3 * TD) {
-#pragma unroll
-                              for (int i = 8 + 8 * n / TD; i < 8 + 8 * (n + 1) / TD; ++i) exponential(i);
-                            }
-                          });
-      }
-      const float all = sum[0] + sum[1];
-      if constexpr (!Q16) l += all;
-      else if (!each) l += ldexpf(all, -shift);
+                                for (int i = 8 + 8 * n / TD; i < 8 + 8 * (n + 1) / TD; ++i) exponential(i);
+                              }
+                            });
+        }
+        const float all = sum[0] + sum[1];
+        if constexpr (!Q16) l += all;
+        else if (!each) l += ldexpf(all, -shift);
       }
       if constexpr (!Q16) {
         odd = 0ull;
@@ -896,16 +902,16 @@ __global__ __launch_bounds__(64 * WAVES, HD == 256 && WAVES == 4 ? 1 : 2) void a
 #pragma unroll
         for (int i = 0; i + 1 < AHEAD; ++i) queue[i] = queue[i + 1];
       } else {
-      if constexpr (Q16) {
-        ld.put_keys(sh, at ^ 1, next.there, c);
-        each = each_next;
-        v_exp = v_next;
-        ld.put_values(sh, at ^ 1, next.there, v_exp, each, odd);
-      }
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-      if (!Q16 && (!TREE || tile + 1 < last) && masked_of(next)) clean(next, at ^ 1);
-      __syncthreads();
-      now = next;
+        if constexpr (Q16) {
+          ld.put_keys(sh, at ^ 1, next.there, c);
+          each = each_next;
+          v_exp = v_next;
+          ld.put_values(sh, at ^ 1, next.there, v_exp, each, odd);
+        }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        if (!Q16 && (!TREE || tile + 1 < last) && masked_of(next)) clean(next, at ^ 1);
+        __syncthreads();
+        now = next;
       }
     }
 
@@ -946,8 +952,7 @@ __global__ __launch_bounds__(64 * WAVES, HD == 256 && WAVES == 4 ? 1 : 2) void a
       }
     }
     if constexpr (PREFIX) break;
-    if (first == 0 && !whole)
-    {
+    if (first == 0 && !whole) {
       const int pieces = (int)((unsigned)(u + (tiles - first) + (units - (last - first)) - 1) / (unsigned)per) - me + 1;
       cut = TREE ? int4{q.first, row_tile * R, pieces << 9 | (int)min((int64_t)q.count * a.group - (int64_t)row_tile * R, (int64_t)R), head} : int4{entry, head, pieces, 0};
     }

@@ -64,7 +64,7 @@ kt_status kt_attention_mass(const kt_kv_cache* cache, const void* Q, int64_t ldq
   t.mass = mass;
   t.decay = decay;
   hipStream_t st = static_cast<hipStream_t>(stream);
-  const int64_t most = max_q * a.group;  // rows a head
+  const int64_t most = std::min(max_q, n_tokens) * a.group;  // rows a head
   const bool ok = with_cache(cache, [&](auto kv, auto h) {
     constexpr int KV = decltype(kv)::value, HD = decltype(h)::value;
     using std::integral_constant;

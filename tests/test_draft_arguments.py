@@ -25,7 +25,7 @@ def _tree(cache=None, Q=FAKE, ldq=512, dt=1, starts=FAKE, lens=FAKE, pages=FAKE,
 
 
 @pytest.mark.parametrize("bad,status,text", [
-    (dict(tree=None), 1, "tree"), (dict(ldt=0), 2, "ldt"), (dict(max_q=65), 2, "ldt"), (dict(max_q=129, ldt=2), 2, "ldt"), (dict(tree=FAKE + 4), 2, "tree"),
+    (dict(tree=None), 1, "tree"), (dict(ldt=0), 2, "ldt"), (dict(max_q=65), 2, "ldt"), (dict(max_q=129, ldt=2), 2, "ldt"), (dict(max_q=(1 << 63) - 1), 2, "ldt"), (dict(max_q=(1 << 62), ldt=1 << 24), 2, "ldt"), (dict(tree=FAKE + 4), 2, "tree"),
     (dict(ldt=(1 << 24) + 1), 2, "ldt"), (dict(Q=None), 1, "null"), (dict(lens=None), 1, "null"), (dict(pages=None), 1, "null"), (dict(O=None), 1, "null"),
     (dict(dt=0), 3, "dtype"), (dict(n_seq=0), 1, "positive"), (dict(n=0), 1, "positive"), (dict(max_q=0), 1, "positive"), (dict(n_seq=4097), 6, "sequences"),
     (dict(starts=None), 1, "q_starts"), (dict(hq=3), 2, "n_q_heads"), (dict(ldq=504), 2, "leading"), (dict(ldo=500), 2, "leading"), (dict(ldp=0), 2, "ldp"),

@@ -1,0 +1,133 @@
+"""Calls of the operators for drafted tokens and budgets that the documentation allows: pages far away, streams, random sizes, the same arrays twice."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2503_01483_amd as kt
+from draft_util import FORMATS, NAMES, Held, ints, mass_check, random_tree, select_expected, tree_check, words_of
+from serving_util import Batch
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("fmt", FORMATS, ids=NAMES.get)
+def test_pages_beyond_32_bits(fmt):
+    """A cache of more than 4 GiB: the same tokens in its first and in its last pages give the same bits."""
+    heads, hd, page = 8, 256, 1024
+    bytes_of = {kt.KT_KV_BF16: 1024, kt.KT_KV_U8: 528, kt.KT_KV_U4: 272}[fmt]
+    n_pages = (1 << 32) // (page * heads * bytes_of) + 8
+    cache = kt.KVCache(n_pages, page, heads, hd, fmt)
+    assert cache.nbytes > 1 << 32
+    g = torch.Generator().manual_seed(1)
+    t, count = 1100, 9
+    k, v = (torch.randn(t, heads, hd, generator=g).cuda() for _ in range(2))
+    q = torch.randn(count, heads, hd, generator=g).to(torch.bfloat16).cuda()
+    mass = torch.zeros(n_pages, heads, page, device="cuda")
+    tree = words_of([random_tree(count, np.random.default_rng(2))], count, 1)
+    results = []
+    for table, into in (([0, 1], [2]), ([n_pages - 1, n_pages - 2], [n_pages - 3])):
+        pages, lens, starts = ints([table]), ints([t]), ints([0, count])
+        slots = torch.tensor(table, device="cuda")[torch.arange(t, device="cuda") // page] * page + torch.arange(t, device="cuda") % page
+        kt.kt_kv_append(cache, k, v, slots)
+        lse = torch.empty(count, heads, device="cuda")
+        out = kt.kt_tree_attention(q, cache, pages, lens, tree, q_starts=starts, max_q=count, lse=lse)
+        kt.kt_attention_mass(q, cache, pages, lens, lse, mass, q_starts=starts, max_q=count)
+        kept, n = kt.kt_kv_select(cache, mass, pages, lens, 300, sink=1, recent=7)
+        kt.kt_kv_compact(cache, pages, kept, n, to_pages=ints([into]), mass=mass)
+        moved = kt.kt_kv_gather(cache, into[0] * page + torch.arange(300, device="cuda"), dtype=torch.float32)
+        results.append((out, lse, mass[table].clone(), kept, *moved, mass[into].clone()))
+    for a, b in zip(*results):
+        assert torch.equal(a, b)
+    assert bool((results[0][2].sum((0, 2)) - count * 1.0 < 1).all()) and results[0][3].unique().numel() > 300
+
+
+@pytest.mark.parametrize("seed", range(18))
+def test_random_sizes(seed):
+    rng = np.random.default_rng(seed)
+    fmt, hd = FORMATS[seed % 3], [64, 128, 256][seed // 3 % 3]
+    hkv, group = int(rng.integers(1, 4)), int(rng.choice([1, 2, 3, 4, 5, 7, 8]))
+    n_seq, most = int(rng.integers(1, 6)), int(rng.choice([3, 17, 40, 90]))
+    counts = [int(c) for c in rng.integers(0, most + 1, n_seq)]
+    lens = [c + int(x) for c, x in zip(counts, rng.integers(0, int(rng.choice([5, 100, 400])), n_seq))]
+    print(seed, NAMES[fmt], hd, hkv, group, lens, counts, flush=True)
+    b = Batch(fmt, hd, hkv, group, lens, counts, page=int(rng.choice([64, 128])), seed=seed, prefix=int(rng.choice([0, 0, 70])))
+    if b.n == 0:
+        return
+    masks = [random_tree(c, rng) if rng.random() < 0.7 else rng.random((c, c)) < 0.5 for c in counts]
+    words = -(-max(1, max(counts)) // 64)
+    lse = torch.full((b.n, b.hq), 7.0, device="cuda")
+    more = dict(prefix_pages=b.prefix_pages, prefix_len=b.prefix) if b.prefix else {}
+    out = kt.kt_tree_attention(b.q.cuda(), b.cache, b.pages, ints(lens), words_of(masks, b.n, words), q_starts=ints(b.starts), max_q=max(1, max(counts)), lse=lse, **more)
+    tree_check(b, out, lse, masks)
+    z = b.expected()[1].float()
+    before = torch.rand(b.cache.n_pages, hkv, b.page)
+    got = kt.kt_attention_mass(b.q.cuda(), b.cache, b.pages, ints(lens), z.cuda(), before.cuda(), q_starts=ints(b.starts), max_q=max(1, max(counts)), decay=0.9)
+    mass_check(b, got, z, before, 0.9)
+
+
+@pytest.mark.parametrize("handle", [False, True], ids=["stream", "handle"])
+def test_a_stream_that_is_handed_in(handle):
+    """What the binding makes for a call is made on its stream, also while the current one is busy."""
+    h = Held(kt.KT_KV_U8, 64, 2, 12, 64, seed=6)
+    pages, into, lens = ints(np.arange(8).reshape(1, 8)), ints([[8, 9, 10, 11]]), ints([500])
+    want, n = kt.kt_kv_select(h.cache, h.mass, pages, lens, 200, sink=3, recent=9)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    stream = side.cuda_stream if handle else side
+    a = torch.ones(4096, 4096, device="cuda")
+    for _ in range(3):
+        for _ in range(10):
+            a = a @ a * 2.0 ** -12
+        kept, m = kt.kt_kv_select(h.cache, h.mass, pages, lens, 200, sink=3, recent=9, stream=stream)
+        kt.kt_kv_compact(h.cache, pages, kept, m, to_pages=into, stream=stream)
+        side.synchronize()
+        assert torch.equal(kept, want) and torch.equal(m, n)
+    torch.cuda.synchronize()
+    now = h.now()
+    for head in range(2):
+        src = want[0, head].cpu()
+        assert torch.equal(now[512:712, head, :128], now[src.long(), head, :128])
+
+
+def test_the_same_mass_twice_and_two_calls_side_by_side():
+    """Two batches on two streams, with a cache, pages and masses of their own: as one after the other."""
+    batches = [Batch(fmt, 128, 2, 4, [400, 170], [90, 3], seed=30 + i) for i, fmt in enumerate((kt.KT_KV_U4, kt.KT_KV_BF16))]
+    masks = [[random_tree(c, np.random.default_rng(3)) for c in b.counts] for b in batches]
+    args = [(b.q.cuda(), b.cache, b.pages, ints(b.lens), words_of(m, b.n, 2), ints(b.starts)) for b, m in zip(batches, masks)]
+
+    def run(i, stream, lse, mass, out, ws):
+        q, cache, pages, lens, tree, starts = args[i]
+        kt.kt_tree_attention(q, cache, pages, lens, tree, q_starts=starts, max_q=90, out=out, lse=lse, workspace=ws, stream=stream)
+        kt.kt_attention_mass(q, cache, pages, lens, lse, mass, q_starts=starts, max_q=90, decay=0.5, stream=stream)
+
+    made = lambda b: (torch.empty(b.n, b.hq, device="cuda"), torch.zeros(b.cache.n_pages, 2, b.page, device="cuda"), torch.empty(b.n, b.hq, 128, dtype=torch.bfloat16, device="cuda"), kt.Workspace())  # noqa: E731
+    one, two = [made(b) for b in batches], [made(b) for b in batches]
+    for i in range(2):
+        for _ in range(3):
+            run(i, None, *one[i])
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for _ in range(3):
+        for i in range(2):
+            run(i, streams[i], *two[i])
+    torch.cuda.synchronize()
+    for a, b in zip(one, two):
+        assert all(torch.equal(x, y) for x, y in zip(a[:3], b[:3]))
+
+
+def test_masses_that_are_not_numbers_are_moved_as_they_are():
+    h = Held(kt.KT_KV_BF16, 64, 1, 4, 64, seed=8)
+    h.mass[0, 0, :8] = torch.tensor([math.nan, math.inf, -math.inf, -0.0, 0.0, 1e-45, -1.0, 3e38])
+    before = h.mass.clone()
+    kt.kt_kv_compact(h.cache, ints([[0, 1]]), ints([[0, 1, 2, 3, 4, 5, 6, 7]]), ints([8]), to_pages=ints([[3]]), mass=h.mass)
+    assert torch.equal(h.mass[3, 0, :8].view(torch.int32), before[0, 0, :8].view(torch.int32))
+
+
+def test_no_sink_and_no_mass_to_choose_by():
+    """All masses equal: the first ones stay, behind them the last `recent`."""
+    cache = kt.KVCache(40, 64, 1, 64, kt.KT_KV_U4)
+    kept, n = kt.kt_kv_select(cache, torch.zeros(40, 1, 64, device="cuda"), ints([np.arange(40)]), ints([2560]), 1000, recent=64)
+    want = select_expected([[np.zeros(2560)]], [2560], [1000], 0, 64, 1000)[0][0]
+    assert n.item() == 1000 and np.array_equal(kept[0, 0].cpu().numpy(), want)
