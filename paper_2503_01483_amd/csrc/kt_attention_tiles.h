@@ -90,12 +90,7 @@ __device__ __forceinline__ void list_trees(const TileArgs& t, int* cum) {
       const Sequence q = sequence_of(a, s);
       mine = tree_row_tiles<R>(a, q) * tree_units(t, q);
     }
-    int upto = mine;
-#pragma unroll
-    for (int o = 1; o < 64; o *= 2) {
-      const int v = __shfl_up(upto, o);
-      if (lane >= o) upto += v;
-    }
+    const int upto = sum_up_to(mine);
     if (lane == 63) wave_sum[wave] = upto;
     __syncthreads();
     int before = carry;

@@ -18,16 +18,6 @@ __device__ __forceinline__ uint32_t mass_order(float m) {
   return m != m ? 1u : b ^ (uint32_t)((int)b >> 31 | (int)0x80000000u);
 }
 
-// Sum over the lanes up to this one, by row shifts and broadcasts.
-__device__ __forceinline__ int sum_up_to(int v) {
-  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);  // row_shr 1, 2, 4, 8
-  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
-  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
-  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
-  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);  // row_bcast 15, 31
-  return v + __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);
-}
-
 // How many of a mask's lanes are in front of this one.
 __device__ __forceinline__ uint32_t lanes_below(unsigned long long mask) {
   return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0u));
@@ -37,15 +27,15 @@ __device__ __forceinline__ uint32_t lanes_below(unsigned long long mask) {
 // as the largest of all: the n-th largest number is found digit by digit (11, 11 and 10 bits, counted in LDS), then every wave counts what stays in its
 // piece of the tokens, and writes it behind that of the waves in front.
 // A wave has PER neighbouring rows of 64 tokens, whose numbers it keeps in registers: they are read once, all at the same time.  What is longer than 1024 PER tokens
-// goes through in as many parts, read again for every digit.  Digits are counted 8 times side by side, by lane: the top digit of a float is
+// goes through in as many parts, read again for every digit.  Digits are counted 8 times side by side (few tokens: twice), by lane: the top digit of a float is
 // its exponent, which most of a wave's lanes share, and an LDS counter takes its additions one by one.
 // Bound by a compute unit's instructions, and barriers where there are few tokens: 8 heads of 2300 tokens 10 us, 256 of up to 16384 18 us, 16 of up to 65536 33 us
 // (numbers read again for each digit and counted row by row instead: 11, 49, 157).
 template <int PER>
 __global__ __launch_bounds__(1024) void kv_select_kernel(SelectArgs a) {
-  constexpr int kBins = 2048, kCopies = 8, PART = 1024 * PER;
+  constexpr int kBins = 2048, kCopies = PER < 16 ? 2 : 8, PART = 1024 * PER;
   constexpr uint32_t kStays = 0xffffffffu;  // of a token that stays in any case; 0: of one that there is not
-  __shared__ int bins[kBins * kCopies];
+  __shared__ __align__(16) int bins[kBins * kCopies];
   __shared__ int counts[2][16];
   __shared__ int found[2];  // bin, numbers above it
   const int s = blockIdx.y, head = blockIdx.x, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -117,8 +107,13 @@ __global__ __launch_bounds__(1024) void kv_select_kernel(SelectArgs a) {
       // the bin that the left-th from the top is in: two bins a thread, the top ones first
       const int hi = kBins - 1 - 2 * threadIdx.x;
       auto count = [&](int bin) {
-        const int4* b = reinterpret_cast<const int4*>(bins + bin * kCopies);
-        return b[0].x + b[0].y + b[0].z + b[0].w + b[1].x + b[1].y + b[1].z + b[1].w;
+        if constexpr (kCopies == 2) {
+          const int2 b = *reinterpret_cast<const int2*>(bins + bin * kCopies);
+          return b.x + b.y;
+        } else {
+          const int4* b = reinterpret_cast<const int4*>(bins + bin * kCopies);
+          return b[0].x + b[0].y + b[0].z + b[0].w + b[1].x + b[1].y + b[1].z + b[1].w;
+        }
       };
       const int x = count(hi), y = count(hi - 1);
       int upto = sum_up_to(x + y);

@@ -39,12 +39,7 @@ __device__ __forceinline__ void list_key_groups(const AttendArgs& a, int keys, i
     const int s = base + threadIdx.x;
     int mine = 0;
     if (s < a.n_seq) mine = (int)(((unsigned)sequence_of(a, s).len + keys - 1) / (unsigned)keys);
-    int upto = mine;
-#pragma unroll
-    for (int o = 1; o < 64; o *= 2) {
-      const int t = __shfl_up(upto, o);
-      if (lane >= o) upto += t;
-    }
+    const int upto = sum_up_to(mine);
     if (lane == 63) wave_sum[wave] = upto;
     __syncthreads();
     int before = carry;
