@@ -153,10 +153,11 @@ def _dtype_code(t):
     raise TypeError(f"unsupported dtype {t.dtype}")
 
 
-def _stream(stream):
+def _stream(stream, dev=None):
+    """Handle of a stream (a stream, a handle, or None: the current one), of device `dev` where the current device is known."""
     if stream is None:
         # torch.cuda.current_stream().cuda_stream without the stream object (of a call of 8 us it took 1.5)
-        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device() if dev is None else dev)
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else stream
 
 
@@ -342,7 +343,7 @@ def kt_quant_sensitivity(Y, alphas, *, bits=4, workspace=None, stream=None):
 def _device(t, name):
     """The current device, which `t` has to be on (a kernel is launched there)."""
     dev = t.get_device()
-    if dev < 0 or dev != torch.cuda.current_device():
+    if dev < 0 or dev != torch._C._cuda_getDevice():     # (torch.cuda.current_device(), which first asks whether there is a device: a tensor is on one)
         raise ValueError(f"{name} is on {t.device}: operands have to be on the current device")
     return dev
 
@@ -425,6 +426,7 @@ class KVCache:
         self.nbytes = lib().kt_kv_cache_bytes(self.ref)
         if self.nbytes == 0:
             raise KtError(2, kt_last_error() or "bad cache sizes")
+        self._mass_shape = (self.n_pages, self.n_heads, self.page_size)
         self.data = torch.empty(self.nbytes, dtype=torch.uint8, device=device) if data is None else data
 
     # the sizes that a call checks its operands against are those that the kernels go by
@@ -561,12 +563,12 @@ def _attention(Q, cache, pages, lens, tree, q_starts, max_q, prefix_pages, prefi
         raise ValueError(f"workspace is on {buf.device}: operands have to be on the current device")
     call = L.kt_paged_attention if tree is None else L.kt_tree_attention
     _check(call(ref, Q.data_ptr(), ldq, _dtype_code(Q), pstarts, plens, ppages, ldp, n_seq, n, max_q, hq, *masks, pprefix, prefix_len,
-                hd ** -0.5 if scale is None else scale, out.data_ptr(), ldo, plse, buf.data_ptr(), buf.numel(), _stream(stream)))
+                hd ** -0.5 if scale is None else scale, out.data_ptr(), ldo, plse, buf.data_ptr(), buf.numel(), _stream(stream, dev)))
     return out
 
 
 def _mass(mass, cache, dev):
-    return _index(mass, "mass", dev, torch.float32, (cache.n_pages, cache.n_heads, cache.page_size))
+    return _index(mass, "mass", dev, torch.float32, cache._mass_shape)
 
 
 def kt_attention_mass(Q, cache, pages, lens, lse, mass, *, q_starts=None, max_q=None, scale=None, decay=1.0, stream=None):
@@ -583,7 +585,7 @@ def kt_attention_mass(Q, cache, pages, lens, lse, mass, *, q_starts=None, max_q=
     pstarts = None if q_starts is None else _index(q_starts, "q_starts", dev, torch.int32, (n_seq + 1,))
     _check(lib().kt_attention_mass(ref, Q.data_ptr(), ldq, _dtype_code(Q), pstarts, plens, ppages, ldp, n_seq, n, max_q, hq,
                                    hd ** -0.5 if scale is None else scale, _index(lse, "lse", dev, torch.float32, (n, hq)), decay,
-                                   _mass(mass, cache, dev), _stream(stream)))
+                                   _mass(mass, cache, dev), _stream(stream, dev)))
     return mass
 
 
@@ -606,8 +608,8 @@ def kt_kv_select(cache, mass, pages, lens, keep, *, sink=0, recent=0, kept=None,
     if n_kept is None:
         n_kept = _new(torch.empty, stream, n_seq, dtype=torch.int32, device=mass.device)
     _check(lib().kt_kv_select(cache.ref, pmass, plens, ppages, ldp, n_seq, _index(keep, "keep", dev, torch.int32, (n_seq,)), sink, recent,
-                              _index(kept, "kept", dev, torch.int32, (n_seq, cache.n_heads, kept.shape[2])), kept.shape[2],
-                              _index(n_kept, "n_kept", dev, torch.int32, (n_seq,)), _stream(stream)))
+                              _index(kept, "kept", dev, torch.int32, (n_seq, cache._mass_shape[1], kept.shape[2])), kept.shape[2],
+                              _index(n_kept, "n_kept", dev, torch.int32, (n_seq,)), _stream(stream, dev)))
     return kept, n_kept
 
 
@@ -620,11 +622,11 @@ def kt_kv_compact(cache, pages, src, count, *, first=None, to_pages=None, mass=N
     if src.dim() not in (2, 3):
         raise ValueError(f"src: [n_seq, tokens] or [n_seq, heads, tokens] needed, got {tuple(src.shape)}")
     lds, per_head = src.shape[-1], src.dim() == 3
-    psrc = _index(src, "src", dev, torch.int32, (n_seq, cache.n_heads, lds) if per_head else (n_seq, lds))
+    psrc = _index(src, "src", dev, torch.int32, (n_seq, cache._mass_shape[1], lds) if per_head else (n_seq, lds))
     pto, ldt = (None, 0) if to_pages is None else _table(to_pages, "to_pages", dev, n_seq)
     _check(lib().kt_kv_compact(ref, ppages, ldp, n_seq, psrc, lds, per_head, _index(count, "count", dev, torch.int32, (n_seq,)),
                                None if first is None else _index(first, "first", dev, torch.int32, (n_seq,)), pto, ldt,
-                               None if mass is None else _mass(mass, cache, dev), _stream(stream)))
+                               None if mass is None else _mass(mass, cache, dev), _stream(stream, dev)))
 
 
 def kt_profile_enable(max_records):

@@ -84,8 +84,7 @@ def test_bad_caches(bad, status):
         assert call(cache=ctypes.POINTER(binding._CacheDesc)()) == 1, call
 
 
-def test_the_binding_refuses_what_is_not_on_the_current_device(monkeypatch):
-    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+def test_the_binding_refuses_what_is_not_on_the_current_device():
     cache = kt.KVCache(4, 64, 2, 64, kt.KT_KV_U4, device="cpu")
     q, i, m = torch.zeros(2, 4, 64, dtype=torch.bfloat16), torch.zeros(2, dtype=torch.int32), torch.zeros(4, 2, 64)
     table = torch.zeros(2, 3, dtype=torch.int32)
