@@ -259,6 +259,7 @@ __global__ __launch_bounds__(256, HD == 256 ? 1 : 2) void attend_rows_kernel(Att
   // The next tile asked for as registers come free, where it needs no more of them: decode of 64 behind 16384, 4 bits, 172 -> 166 us.  With 8 bits
   // registers spill (4 behind 131072: 138 -> 165), and bf16 tiles take as many as there are.
   constexpr bool kEarly = KV == kKvU4 && HD <= 128;
+  constexpr int kZero = TREE ? 16 : 128;  // what codes of 4 bits of keys enter with
   constexpr float kOffset = KV == kKvU4 ? 136.f : 128.f, kCentre = KV == kKvU4 ? 8.f : 128.f;
   constexpr float kNone = -__builtin_inff();
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, g = lane >> 4, heads = a.cache.n_heads;
@@ -335,10 +336,10 @@ __global__ __launch_bounds__(256, HD == 256 ? 1 : 2) void attend_rows_kernel(Att
       f32x4 x[4];
 #pragma unroll
       for (int t = 0; t < 4; ++t) {
-        const float x0 = KV == kKvU4 ? -128.f * qsum : 0.f;
+        const float x0 = KV == kKvU4 ? -(float)kZero * qsum : 0.f;
         x[t] = f32x4{x0, x0, x0, x0};
 #pragma unroll
-        for (int w = 0; w < HD / 32; ++w) x[t] = mfma16(t64.key(t, w), qf[w], x[t]);
+        for (int w = 0; w < HD / 32; ++w) x[t] = mfma16(t64.template key<kZero>(t, w), qf[w], x[t]);
       }
       // a lane's 16 keys: their {step, minimum}, keys' and values'
       f32x4 vp[4][2];
