@@ -131,3 +131,45 @@ def test_no_sink_and_no_mass_to_choose_by():
     kept, n = kt.kt_kv_select(cache, torch.zeros(40, 1, 64, device="cuda"), ints([np.arange(40)]), ints([2560]), 1000, recent=64)
     want = select_expected([[np.zeros(2560)]], [2560], [1000], 0, 64, 1000)[0][0]
     assert n.item() == 1000 and np.array_equal(kept[0, 0].cpu().numpy(), want)
+
+
+@pytest.mark.parametrize("fmt", FORMATS, ids=NAMES.get)
+@pytest.mark.parametrize("hd", [64, 256])
+def test_as_many_sequences_as_a_call_takes(fmt, hd):
+    """4096 sequences of up to 70 tokens, empty ones among them: single tokens attended as kt_paged_attention does, weights that add up, all cut down to 20."""
+    n_seq, heads, group = 4096, 1, 2
+    g = torch.Generator().manual_seed(hd)
+    lens = torch.randint(0, 71, (n_seq,), generator=g)
+    lens[0], lens[-1] = 0, 70
+    pages = torch.randperm(2 * n_seq, generator=g).reshape(n_seq, 2)
+    cache = kt.KVCache(2 * n_seq + n_seq, 64, heads, hd, fmt)
+    seq = torch.repeat_interleave(torch.arange(n_seq), lens)
+    t = torch.arange(len(seq)) - torch.repeat_interleave(torch.cumsum(lens, 0) - lens, lens)
+    slots = pages[seq, t // 64] * 64 + t % 64
+    k, v = (torch.randn(len(seq), heads, hd, generator=g).cuda() for _ in range(2))
+    kt.kt_kv_append(cache, k, v, slots.cuda())
+    q = torch.randn(n_seq, heads * group, hd, generator=g).to(torch.bfloat16).cuda()
+    lse, want_lse = torch.empty(n_seq, heads * group, device="cuda"), torch.empty(n_seq, heads * group, device="cuda")
+    table, length = ints(pages), ints(lens)
+    out = kt.kt_tree_attention(q, cache, table, length, torch.ones(n_seq, 1, dtype=torch.int64, device="cuda"), lse=lse)
+    want = kt.kt_paged_attention(q, cache, table, length, lse=want_lse)
+    some = lens.cuda() > 0
+    # (both round p, and the result, to bf16: 2^-8 of |v| at most each, twice; values are within 5.5 of 0)
+    assert bool(((out.float() - want.float()).abs() <= 4 * 2.0 ** -8 * 5.5).all()) and bool((out[~some] == 0).all())
+    assert bool(((lse - want_lse).abs()[some] <= 2.0 ** -14).all()) and bool((lse[~some] == -math.inf).all())
+    mass = torch.full((3 * n_seq, heads, 64), math.nan, device="cuda")
+    kt.kt_attention_mass(q, cache, table, length, lse, mass, decay=0.0)
+    per_seq = torch.zeros(n_seq, device="cuda").index_add_(0, seq.cuda(), mass.reshape(-1)[slots.cuda()])
+    assert bool(((per_seq - group * some.float()).abs() <= 2.0 ** -13).all())
+    kept, n = kt.kt_kv_select(cache, mass, table, length, 20, sink=1, recent=3)
+    assert torch.equal(n.cpu(), lens.clamp(max=20).int())
+    into = ints(2 * n_seq + torch.arange(n_seq).reshape(-1, 1))
+    kt.kt_kv_compact(cache, table, kept, n, to_pages=into, mass=mass)
+    j = torch.arange(20)
+    live = j[None] < n.cpu()[:, None]
+    src = kept[:, 0].cpu().long()
+    a = torch.gather(pages, 1, torch.where(live, src // 64, 0)) * 64 + src % 64
+    b = (2 * n_seq + torch.arange(n_seq))[:, None] * 64 + j[None]
+    x, y = kt.kt_kv_gather(cache, a[live].cuda(), dtype=torch.float32), kt.kt_kv_gather(cache, b[live].cuda(), dtype=torch.float32)
+    assert torch.equal(x[0], y[0]) and torch.equal(x[1], y[1])
+    assert torch.equal(mass.reshape(-1)[a[live].cuda()], mass.reshape(-1)[b[live].cuda()])
