@@ -501,7 +501,9 @@ kt_status kt_tree_attention(const kt_kv_cache* cache, const void* Q, int64_t ldq
  * the query heads that read the head.  A token that is itself one of the queries starts from 0: mass needs no initialisation where every
  * token has been a query once, nor with decay = 0, which does not read it.
  *  mass     [n_pages][n_heads][page_size] fp32, read and written: token t of a sequence has the place that it has in the cache's pages.  Of
- *           places that no sequence's tokens lie in nothing is read or written.  A page that several sequences name gets the sum of one of them.
+ *           places that no sequence's tokens lie in nothing is read or written.  Where sequences share pages (a prompt that they begin with: the same page in
+ *           front, and the shared one at the same place), a token's mass is that of the first sequence of the call that has the token; the queries of
+ *           the others add nothing to it.  Of a page that sequences name at other places, or twice, the masses are unspecified.
  *  lse      [n_tokens][n_q_heads] fp32, as kt_paged_attention writes it (with a prefix: over both; the prefix's own tokens get no mass here).  Rows whose
  *           lse is not finite add nothing.
  *  max_q    a bound on the queries of a sequence, by which the launch is laid out; the rows of a longer one are added all the same.

@@ -69,7 +69,7 @@ kt_status kt_attention_mass(const kt_kv_cache* cache, const void* Q, int64_t ldq
     constexpr int KV = decltype(kv)::value, HD = decltype(h)::value;
     using std::integral_constant;
     const int64_t tokens = ldp * cache->page_size;
-    const size_t list = (size_t)(n_seq + 1) * 4;
+    const size_t list = mass_lists(n_seq);
     auto grid = [&](int keys) { return dim3((unsigned)std::min<int64_t>(n_seq * ceil_div(tokens, keys) * cache->n_heads, kNumCUs * 8)); };
     auto go_few = [&](auto ni) {
       mass_few_kernel<KV, HD, decltype(ni)::value><<<grid(256), 256, list, st>>>(t);
@@ -78,7 +78,7 @@ kt_status kt_attention_mass(const kt_kv_cache* cache, const void* Q, int64_t ldq
     if (most <= 4) return go_few(integral_constant<int, 1>{});
     if (most <= 64) return go_few(integral_constant<int, 4>{});
     auto kernel = mass_rows_kernel<KV, HD>;
-    if (!ensure_dynamic_lds(reinterpret_cast<const void*>(kernel), sizeof(MassShared<HD>) + (kMaxSequences + 1) * 4)) return false;
+    if (!ensure_dynamic_lds(reinterpret_cast<const void*>(kernel), sizeof(MassShared<HD>) + mass_lists(kMaxSequences))) return false;
     kernel<<<grid(128), 512, sizeof(MassShared<HD>) + list, st>>>(t);
     return true;
   });

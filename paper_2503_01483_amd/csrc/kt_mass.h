@@ -5,7 +5,7 @@
 // A wave holds 64 keys, one block of the cache, and goes through the rows sixteen at a time, S = Q K^T in 16 x 16 x 32 products with the keys on the
 // columns: a lane has four keys and of each the scores of four rows, whose exponentials it adds up; the four quarters of the wave are added once at the
 // end.  A token's {step, minimum} are its lane's own, and neighbouring lanes write neighbouring masses.  Every sum has a fixed order and one owner: nothing
-// is atomic, no score leaves the registers.
+// is atomic, no score leaves the registers.  Of a page that sequences share, the first of them that has a token owns its mass (owned_in_front).
 // With few rows, row j of sixteen is row 4 (j % 4) + j / 4 of the products, so that the first four (a token's, with four queries a head) lie in one register of
 // every quarter, and only that is exponentiated.
 #pragma once
@@ -29,16 +29,25 @@ __device__ __forceinline__ void lds_copy_4(const char* base, uint32_t offset, un
   asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1" ::"v"(offset), "s"(base), "s"(lds_addr) : "memory", "m0");
 }
 
-// Groups of keys of one head in front of each sequence, `cum` [n_seq + 1] (LDS), by a workgroup of THREADS.
+// Lists of sequences (LDS): a tag of the page that each begins with [n_seq, rounded up], groups of keys of one head in front of each [n_seq + 1].
+constexpr int kTagsAtOnce = 512;  // a wave's 16-byte loads
+__host__ __device__ constexpr int64_t mass_tags_bytes(int64_t n_seq) { return (n_seq + kTagsAtOnce - 1) / kTagsAtOnce * kTagsAtOnce * 2; }
+constexpr size_t mass_lists(int64_t n_seq) { return (size_t)(mass_tags_bytes(n_seq) + (n_seq + 1) * 4); }
+__device__ __forceinline__ uint16_t page_tag(int page) { return (uint16_t)((uint32_t)page * 2654435761u >> 16); }  // (2^32 / golden ratio)
+
+// By a workgroup of THREADS.
 template <int THREADS>
-__device__ __forceinline__ void list_key_groups(const AttendArgs& a, int keys, int* cum) {
+__device__ __forceinline__ void list_key_groups(const AttendArgs& a, int keys, int* cum, uint16_t* tags) {
   __shared__ int wave_sum[THREADS / 64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   int carry = 0;
   for (int base = 0; base < a.n_seq; base += THREADS) {
     const int s = base + threadIdx.x;
     int mine = 0;
-    if (s < a.n_seq) mine = (int)(((unsigned)sequence_of(a, s).len + keys - 1) / (unsigned)keys);
+    if (s < a.n_seq) {
+      mine = (int)(((unsigned)sequence_of(a, s).len + keys - 1) / (unsigned)keys);
+      tags[s] = page_tag(a.pages[s * a.ldp]);  // (of an empty one whatever it is: it owns no token)
+    }
     const int upto = sum_up_to(mine);
     if (lane == 63) wave_sum[wave] = upto;
     __syncthreads();
@@ -55,11 +64,40 @@ __device__ __forceinline__ void list_key_groups(const AttendArgs& a, int keys, i
   __syncthreads();
 }
 
+// How many of sequence s' tokens, as far as they lie in `page`, place `place` of its table, belong to sequences in front of it, which share the page: they
+// begin with the same page as s and have this one at the same place.  Whoever else names a page is not looked for: each pair of places would have to be compared.
+// No more than `enough` are looked for.  All lanes take part; uniform, as the arguments are.
+// Beside the loads of keys it costs nothing up to 64 sequences (64 behind up to 16384, 4 bits: 105 to 115 us with and without); 256 behind up to 2000 take 48 us
+// (without it 47), 1024 behind 500 63 (59), 4096 behind 70 133 (106); 256 that share the first half of their pages 62.
+__device__ __forceinline__ int owned_in_front(const AttendArgs& a, const uint16_t* tags, int s, int place, int page, int enough) {
+  const int lane = threadIdx.x & 63;
+  const uint32_t both = tags[s] * 0x10001u;
+  int most = 0;
+  for (int base = 0; base < s; base += kTagsAtOnce) {
+    const u32x4 d = reinterpret_cast<const u32x4*>(tags + base)[lane];
+    uint32_t same = 0;  // bit i: sequence 2 i of the lane's eight, bit 16 + i: 2 i + 1 (and maybe one behind a match: the tables say)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t x = d[i] ^ both;
+      same |= ((x - 0x10001u) & ~x & 0x80008000u) >> (15 - i);
+    }
+    for (; same && most < enough; same &= same - 1) {
+      const int at = __builtin_ctz(same), o = base + 8 * lane + 2 * (at & 15) + (at >> 4);
+      if (o >= s) continue;
+      const int64_t row = o * a.ldp;
+      const int first = a.pages[row], its = a.pages[row + place], len = sequence_of(a, o).len;  // (asked for together)
+      if (first == a.pages[s * a.ldp] && its == page) most = max(most, len);
+    }
+    if (__any(most >= enough)) return enough;
+  }
+  return wave_max(most);
+}
+
 // Few rows: a wave goes through all of them, 4 NI at a time, with queries straight from memory.  Bound by HBM: 64 tokens behind up to 16384, 32 + 8 heads of 128, 4 bits:
 // 103 us, 4.1 TB/s of keys, parameters and masses.
 template <int KV, int HD, int NI>
 __global__ __launch_bounds__(256, 2) void mass_few_kernel(MassArgs t) {
-  extern __shared__ int cum[];
+  extern __shared__ __align__(16) char lds[];
   constexpr int W = HD / 32, ROWS = 4 * NI;
   constexpr float kInf = __builtin_inff(), kZero = KV == kKvU4 ? 16.f : 0.f;  // codes of 4 bits enter as 16 + c
   using Tile = Tile64<KV, HD>;
@@ -67,7 +105,9 @@ __global__ __launch_bounds__(256, 2) void mass_few_kernel(MassArgs t) {
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), r = lane & 15, g = lane >> 4, heads = a.cache.n_heads;
   const int page_blocks = a.cache.log2_page - 6;
   const float c = a.scale * 1.44269504f;
-  list_key_groups<256>(a, 256, cum);
+  uint16_t* const tags = reinterpret_cast<uint16_t*>(lds);
+  int* const cum = reinterpret_cast<int*>(lds + mass_tags_bytes(a.n_seq));
+  list_key_groups<256>(a, 256, cum, tags);
   const int64_t total = (int64_t)cum[a.n_seq] * heads;
   const int step_q = ROWS / a.group, step_r = ROWS - step_q * a.group;
 
@@ -114,6 +154,9 @@ __global__ __launch_bounds__(256, 2) void mass_few_kernel(MassArgs t) {
       if (rest >= a.group) rest -= a.group, ++in_seq;
     };
     if (row0 < rows) ask();
+    // (beside the loads that are under way, that of `old` among them: of a token that another sequence owns it is not used)
+    const int in_front = owned_in_front(a, tags, s, tile >> page_blocks, page, key0 + there);
+    const bool own = lane < there && key0 + lane >= in_front;
     if constexpr (KV != kKvBf16) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) par[i].x *= c, par[i].y *= c;
@@ -178,7 +221,7 @@ __global__ __launch_bounds__(256, 2) void mass_few_kernel(MassArgs t) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) sum[i] = quarters_sum(sum[i]);
     const float mine = g == 0 ? sum[0] : g == 1 ? sum[1] : g == 2 ? sum[2] : sum[3];
-    if (lane < there) *mass = fmaf(t.decay, old, mine);
+    if (own) *mass = fmaf(t.decay, old, mine);
   }
 }
 
@@ -189,7 +232,7 @@ __global__ __launch_bounds__(256, 2) void mass_few_kernel(MassArgs t) {
 // Bound by the vector ALU (an exponential, two more instructions a score) and by the workgroup with the most rows, alone on its compute unit at the
 // end: 770 TFLOP/s of Q K^T for those prompts.
 template <int HD>
-struct MassShared {
+struct alignas(16) MassShared {
   char q[2][64 * HD * 2];  // 16-byte chunks of a row exchanged by its number, so that eight rows' are in all banks
   float lse[2][64];        // as it comes
   float base[2][64];       // -lse in bits; -inf: the row adds nothing
@@ -202,7 +245,6 @@ __global__ __launch_bounds__(512, HD == 256 ? 2 : 4) void mass_rows_kernel(MassA
   extern __shared__ __align__(16) char lds[];
   using Shared = MassShared<HD>;
   Shared& sh = *reinterpret_cast<Shared*>(lds);
-  int* const cum = reinterpret_cast<int*>(lds + sizeof(Shared));
   __shared__ float joined[8][64];
   constexpr int WK = 2, WR = 4, W = HD / 32, ROWB = HD * 2, PIECES = HD / 64;  // KiB of a wave
   constexpr float kInf = __builtin_inff(), kZero = KV == kKvU4 ? 16.f : 0.f;
@@ -212,7 +254,9 @@ __global__ __launch_bounds__(512, HD == 256 ? 2 : 4) void mass_rows_kernel(MassA
   const int wk = wave / WR, wr = wave % WR, page_blocks = a.cache.log2_page - 6;
   const float c = a.scale * 1.44269504f, per_group = 1.f / (float)a.group;
   const int step_q = 64 / a.group, step_r = 64 - step_q * a.group;
-  list_key_groups<512>(a, 64 * WK, cum);
+  uint16_t* const tags = reinterpret_cast<uint16_t*>(lds + sizeof(Shared));
+  int* const cum = reinterpret_cast<int*>(lds + sizeof(Shared) + mass_tags_bytes(a.n_seq));
+  list_key_groups<512>(a, 64 * WK, cum, tags);
   const int64_t total = (int64_t)cum[a.n_seq] * heads;
 
   for (int64_t u = blockIdx.x; u < total; u += gridDim.x) {
@@ -238,6 +282,8 @@ __global__ __launch_bounds__(512, HD == 256 ? 2 : 4) void mass_rows_kernel(MassA
       for (int i = 0; i < 4; ++i) par[i] = reinterpret_cast<const float2*>(block + 2 * Tile::kHalf)[16 * i + r];
     }
     if (page >= 0 && wr == 0 && t.decay != 0.f && key0 + lane < ahead) old = *mass;
+    const int in_front = page >= 0 && wr == 0 ? owned_in_front(a, tags, s, tile >> page_blocks, page, key0 + there) : 0;
+    const bool own = page >= 0 && wr == 0 && lane < there && key0 + lane >= in_front;
     const int64_t rows = (int64_t)q.count * a.group;
     const int64_t first = max(0, group * WK * 64 - ahead) * (int64_t)a.group >> 6;  // tile of 64 rows
     int64_t rt = ((rows + 63) >> 6) - 1;
@@ -384,7 +430,7 @@ __global__ __launch_bounds__(512, HD == 256 ? 2 : 4) void mass_rows_kernel(MassA
     for (int i = 0; i < 4; ++i) sum[i] = quarters_sum(sum[i]);
     joined[wave][lane] = g == 0 ? sum[0] : g == 1 ? sum[1] : g == 2 ? sum[2] : sum[3];
     __syncthreads();
-    if (wr == 0 && page >= 0 && lane < there) {
+    if (own) {
       float mine = 0.f;
 #pragma unroll
       for (int w = 0; w < WR; ++w) mine += joined[wk * WR + w][lane];
