@@ -480,7 +480,8 @@ size_t kt_paged_attention_bytes(int64_t n_tokens, int64_t n_q_heads, int64_t hea
  * Attention of the tokens of a drafted tree over the cache: kt_paged_attention, where a query sees, of its sequence's tokens, those in front of the
  * sequence's queries and the queries that its mask names, whatever their order.  All queries are appended first, as in kt_paged_attention.
  *  tree     [n_tokens][ldt] uint64: bit d % 64 of word d / 64 of a query's row says whether it sees query d of its sequence (usually its ancestors and
- *           itself).  Bits of queries that the sequence does not have are passed over.  ldt at least ceil(max_q / 64), 8-byte aligned.
+ *           itself).  Bits of queries that the sequence does not have are passed over, queries that the words have no bit for (of a sequence with
+ *           more than max_q) are seen by none.  ldt at least ceil(max_q / 64), 8-byte aligned.
  *  q_starts NULL: one query a sequence, whose bit 0 says whether it sees itself.
  * A query without tokens in front and with no bit set gives 0, and -inf in lse.  Everything else, the prefix and the workspace (kt_paged_attention_bytes)
  * among it, is as kt_paged_attention says, but for which calls round p times the value's step to 16 bits: those with max_q * n_q_heads / n_heads

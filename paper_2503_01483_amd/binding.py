@@ -509,11 +509,12 @@ def kt_paged_attention(Q, cache, pages, lens, *, q_starts=None, max_q=None, pref
 def kt_tree_attention(Q, cache, pages, lens, tree, *, q_starts=None, max_q=None, prefix_pages=None, prefix_len=0, scale=None, out=None,
                       lse=None, workspace=None, stream=None):
     """kt_paged_attention where a query sees, of its sequence's queries, those whose bit is set in its row of `tree` [n_tokens][words] int64
-    (query d: bit d % 64 of word d / 64).  max_q: without one, as many as all of Q's or the words have bits for."""
+    (query d: bit d % 64 of word d / 64).  max_q: without one, all of Q's, for which the words need bits; a sequence with more queries than a bound that is
+    given has wrong rows (queries behind the last bit are seen by none)."""
     if tree.dim() != 2:
         raise ValueError(f"tree: [n_tokens, words] needed, got {tuple(tree.shape)}")
-    if max_q is None and q_starts is not None:
-        max_q = min(Q.shape[0], 64 * tree.shape[1])
+    if max_q is None and q_starts is not None and Q.shape[0] > 64 * tree.shape[1]:
+        raise ValueError(f"max_q: needed where Q has more rows ({Q.shape[0]}) than words of tree have bits ({64 * tree.shape[1]})")
     return _attention(Q, cache, pages, lens, tree, q_starts, max_q, prefix_pages, prefix_len, scale, out, lse, workspace, stream)
 
 
