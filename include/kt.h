@@ -508,8 +508,10 @@ kt_status kt_tree_attention(const kt_kv_cache* cache, const void* Q, int64_t ldq
  *  lse      [n_tokens][n_q_heads] fp32, as kt_paged_attention writes it (with a prefix: over both; the prefix's own tokens get no mass here).  Rows whose
  *           lse is not finite add nothing.
  *  max_q    a bound on the queries of a sequence, by which the launch is laid out; the rows of a longer one are added all the same.
- * The other arguments are those of kt_paged_attention.  Scores, exponentials and sums are fp32, in a fixed order: scores and lse are off by a few 2^-24 of
- * sum |q k| scale + |lse|, and so is, relatively, each term.  decay >= 0.  Tokens of a page outside the cache are passed over.  No workspace.
+ * The other arguments are those of kt_paged_attention.  Scores, exponentials and sums are fp32, in a fixed order.  A term is off, relatively, by up to 2^-20 of
+ * scale * sum |q| * (max |k| + n steps of the key) + 1 and 2^-22 of |scale q . k| + |lse|; n is 0 (KT_KV_BF16), 255 (KT_KV_U8) or 31 (KT_KV_U4): codes are what is
+ * multiplied, those of 4 bits as 16 + code, so that small keys of wide steps are as far off as large ones.  decay >= 0.  Tokens of a page outside the cache are
+ * passed over.  No workspace.
  */
 kt_status kt_attention_mass(const kt_kv_cache* cache, const void* Q, int64_t ldq, kt_dtype dtype, const int32_t* q_starts,
                             const int32_t* lens, const int32_t* pages, int64_t ldp, int64_t n_seq, int64_t n_tokens,
