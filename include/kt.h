@@ -512,6 +512,8 @@ kt_status kt_tree_attention(const kt_kv_cache* cache, const void* Q, int64_t ldq
  * scale * sum |q| * (max |k| + n steps of the key) + 1 and 2^-22 of |scale q . k| + |lse|; n is 0 (KT_KV_BF16), 255 (KT_KV_U8) or 31 (KT_KV_U4): codes are what is
  * multiplied, those of 4 bits as 16 + code, so that small keys of wide steps are as far off as large ones.  decay >= 0.  Tokens of a page outside the cache are
  * passed over.  No workspace.
+ * Queries see the tokens up to their own here, whatever they saw in kt_tree_attention: of a drafted tree the accepted path is moved together first
+ * (kt_kv_compact), and goes in as a chunk of its queries with the rows of lse that belong to them.
  */
 kt_status kt_attention_mass(const kt_kv_cache* cache, const void* Q, int64_t ldq, kt_dtype dtype, const int32_t* q_starts,
                             const int32_t* lens, const int32_t* pages, int64_t ldp, int64_t n_seq, int64_t n_tokens,
