@@ -77,33 +77,41 @@ template <int R>
 __device__ __forceinline__ int tree_row_tiles(const AttendArgs& a, const Sequence& q) {
   return (int)min(((int64_t)q.count * a.group + R - 1) / R, (int64_t)a.row_tiles);
 }
-// Units in front of each sequence, `cum` [n_seq + 1] (LDS), by a workgroup of THREADS.
+// Units in front of each sequence, `cum` [n_seq + 1] (LDS), by a workgroup of THREADS.  Of sequences that share queries (q_starts that descend, which the host does not
+// see) they can be more than 2^31, over all heads: then there are none, and nothing is computed.  (The host bounds those of others by 2^30.)
 template <int R, int THREADS>
 __device__ __forceinline__ void list_trees(const TileArgs& t, int* cum) {
   __shared__ int wave_sum[THREADS / 64];
   const AttendArgs& a = t.a;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  int carry = 0;
+  int64_t carry = 0;
   for (int base = 0; base < a.n_seq; base += THREADS) {
     const int s = base + threadIdx.x;
-    int mine = 0;
+    int64_t mine = 0;
     if (s < a.n_seq) {
       const Sequence q = sequence_of(a, s);
-      mine = tree_row_tiles<R>(a, q) * tree_units(t, q);
+      mine = (int64_t)tree_row_tiles<R>(a, q) * tree_units(t, q);
     }
-    const int upto = sum_up_to(mine);
-    if (lane == 63) wave_sum[wave] = upto;
+    const int upto = sum_up_to((int)mine);
+    bool beyond = false;
+    if (__any(mine > 1 << 24)) {  // (else the wave's sum is at most 2^30)
+      float all = (float)mine;
+#pragma unroll
+      for (int o = 1; o < 64; o *= 2) all += __shfl_xor(all, o);
+      beyond = all > 1.5f * (1 << 30);
+    }
+    if (lane == 63) wave_sum[wave] = beyond ? INT32_MAX : upto;
     __syncthreads();
-    int before = carry;
+    int64_t before = carry;
 #pragma unroll
     for (int w = 0; w < THREADS / 64; ++w) {
       if (w < wave) before += wave_sum[w];
       carry += wave_sum[w];
     }
-    if (s < a.n_seq) cum[s] = before + upto - mine;
+    if (s < a.n_seq) cum[s] = (int)(before + upto - mine);
     __syncthreads();
   }
-  if (threadIdx.x == 0) cum[a.n_seq] = carry;
+  if (threadIdx.x == 0) cum[a.n_seq] = carry * a.cache.n_heads < INT32_MAX ? (int)carry : 0;
   __syncthreads();
 }
 
