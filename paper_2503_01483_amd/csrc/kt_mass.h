@@ -185,7 +185,7 @@ __global__ __launch_bounds__(256, 2) void mass_few_kernel(MassArgs t) {
       const bool counts = fabsf(lse) <= kHuge;
       const float mine = counts ? lse * -1.44269504f : -kInf;
       const int mine_seen = counts ? seen : 0;
-      const bool edge = __any(mine_seen < 64);
+      const bool edge = __any(j < ROWS && mine_seen < 64);  // (lanes behind the last row have none)
       float base[NI];
       [[maybe_unused]] int sees[NI];
 #pragma unroll
