@@ -122,7 +122,7 @@ __global__ __launch_bounds__(256, 2) void mass_few_kernel(MassArgs t) {
     page = uniform(page);
     if (page < 0) continue;
     float sum[4] = {0.f, 0.f, 0.f, 0.f}, old = 0.f;
-    float* const mass = t.mass + (((int64_t)page * heads + head) << a.cache.log2_page) + (key0 & ((1 << a.cache.log2_page) - 1)) + lane;
+    float* const mass = t.mass + (((int64_t)page * heads + head) << a.cache.log2_page) + (key0 & ((1 << a.cache.log2_page) - 1));
     Tile k;
     const char* block = a.cache.data + kv_block_offset<KV, HD>(a.cache, page, head, tile & ((1 << page_blocks) - 1));
 #pragma unroll
@@ -132,7 +132,7 @@ __global__ __launch_bounds__(256, 2) void mass_few_kernel(MassArgs t) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) par[i] = reinterpret_cast<const float2*>(block + 2 * Tile::kHalf)[16 * i + r];
     }
-    if (t.decay != 0.f && key0 + lane < ahead) old = *mass;
+    if (t.decay != 0.f && key0 + lane < ahead) old = mass[lane];
     // rows from the first that sees the first key on; this lane's queries are those of row j of a group of rows
     const int j = (r >> 2) + 4 * (r & 3);
     const int64_t rows = (int64_t)q.count * a.group;
@@ -156,7 +156,6 @@ __global__ __launch_bounds__(256, 2) void mass_few_kernel(MassArgs t) {
     if (row0 < rows) ask();
     // (beside the loads that are under way, that of `old` among them: of a token that another sequence owns it is not used)
     const int in_front = owned_in_front(a, tags, s, tile >> page_blocks, page, key0 + there);
-    const bool own = lane < there && key0 + lane >= in_front;
     if constexpr (KV != kKvBf16) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) par[i].x *= c, par[i].y *= c;
@@ -221,7 +220,7 @@ __global__ __launch_bounds__(256, 2) void mass_few_kernel(MassArgs t) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) sum[i] = quarters_sum(sum[i]);
     const float mine = g == 0 ? sum[0] : g == 1 ? sum[1] : g == 2 ? sum[2] : sum[3];
-    if (own) *mass = fmaf(t.decay, old, mine);
+    if (lane < there && key0 + lane >= in_front) mass[lane] = fmaf(t.decay, old, mine);
   }
 }
 
@@ -240,12 +239,18 @@ struct alignas(16) MassShared {
   int least[2];            // the least of these
 };
 
+// What is asked for again behind the rows of a block of keys (LDS: in registers, full of keys, it would push others out to memory).
+struct MassBlock {
+  int s, tile, page, there, head;
+};
+
 template <int KV, int HD>
 __global__ __launch_bounds__(512, HD == 256 ? 2 : 4) void mass_rows_kernel(MassArgs t) {
   extern __shared__ __align__(16) char lds[];
   using Shared = MassShared<HD>;
   Shared& sh = *reinterpret_cast<Shared*>(lds);
   __shared__ float joined[8][64];
+  __shared__ MassBlock blocks[2];
   constexpr int WK = 2, WR = 4, W = HD / 32, ROWB = HD * 2, PIECES = HD / 64;  // KiB of a wave
   constexpr float kInf = __builtin_inff(), kZero = KV == kKvU4 ? 16.f : 0.f;
   using Tile = Tile64<KV, HD>;
@@ -259,6 +264,10 @@ __global__ __launch_bounds__(512, HD == 256 ? 2 : 4) void mass_rows_kernel(MassA
   list_key_groups<512>(a, 64 * WK, cum, tags);
   const int64_t total = (int64_t)cum[a.n_seq] * heads;
 
+  auto mass_of = [&](int page, int head, int tile) {
+    return t.mass + (((int64_t)page * heads + head) << a.cache.log2_page) + (tile * 64 & ((1 << a.cache.log2_page) - 1)) + lane;
+  };
+
   for (int64_t u = blockIdx.x; u < total; u += gridDim.x) {
     const int at = (int)(u / heads), head = (int)(u - (int64_t)at * heads);
     const int s = uniform(sequence_at(cum, a.n_seq, at));
@@ -271,7 +280,7 @@ __global__ __launch_bounds__(512, HD == 256 ? 2 : 4) void mass_rows_kernel(MassA
     if (page >= a.cache.n_pages) page = -1;
     page = uniform(page);
     float sum[4] = {0.f, 0.f, 0.f, 0.f}, old = 0.f;
-    float* const mass = t.mass + (((int64_t)max(page, 0) * heads + head) << a.cache.log2_page) + (key0 & ((1 << a.cache.log2_page) - 1)) + lane;
+    if (wr == 0 && lane == 0) blocks[wk] = MassBlock{s, tile, page, there, head};
     Tile k;
     const char* block = a.cache.data + (page < 0 ? 0 : kv_block_offset<KV, HD>(a.cache, page, head, tile & ((1 << page_blocks) - 1)));
 #pragma unroll
@@ -281,9 +290,7 @@ __global__ __launch_bounds__(512, HD == 256 ? 2 : 4) void mass_rows_kernel(MassA
 #pragma unroll
       for (int i = 0; i < 4; ++i) par[i] = reinterpret_cast<const float2*>(block + 2 * Tile::kHalf)[16 * i + r];
     }
-    if (page >= 0 && wr == 0 && t.decay != 0.f && key0 + lane < ahead) old = *mass;
-    const int in_front = page >= 0 && wr == 0 ? owned_in_front(a, tags, s, tile >> page_blocks, page, key0 + there) : 0;
-    const bool own = page >= 0 && wr == 0 && lane < there && key0 + lane >= in_front;
+    if (page >= 0 && wr == 0 && t.decay != 0.f && key0 + lane < ahead) old = *mass_of(page, head, tile);
     const int64_t rows = (int64_t)q.count * a.group;
     const int64_t first = max(0, group * WK * 64 - ahead) * (int64_t)a.group >> 6;  // tile of 64 rows
     int64_t rt = ((rows + 63) >> 6) - 1;
@@ -430,11 +437,18 @@ __global__ __launch_bounds__(512, HD == 256 ? 2 : 4) void mass_rows_kernel(MassA
     for (int i = 0; i < 4; ++i) sum[i] = quarters_sum(sum[i]);
     joined[wave][lane] = g == 0 ? sum[0] : g == 1 ? sum[1] : g == 2 ? sum[2] : sum[3];
     __syncthreads();
-    if (own) {
-      float mine = 0.f;
+    if (wr == 0) {
+      const MassBlock b = blocks[wk];
+      const int page = uniform(b.page), tile = uniform(b.tile), there = uniform(b.there);
+      if (page >= 0) {
+        const int in_front = owned_in_front(a, tags, uniform(b.s), tile >> page_blocks, page, tile * 64 + there);
+        if (lane < there && tile * 64 + lane >= in_front) {
+          float mine = 0.f;
 #pragma unroll
-      for (int w = 0; w < WR; ++w) mine += joined[wk * WR + w][lane];
-      *mass = fmaf(t.decay, old, mine);
+          for (int w = 0; w < WR; ++w) mine += joined[wk * WR + w][lane];
+          *mass_of(page, b.head, tile) = fmaf(t.decay, old, mine);
+        }
+      }
     }
   }
 }
