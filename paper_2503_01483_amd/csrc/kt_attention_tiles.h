@@ -51,12 +51,6 @@ struct TileArgs {
   float* prefix_part;    // [splits][n_tokens][hq][HD], then {max in bits, sum}
 };
 
-// 16 bytes a lane from memory straight into LDS: lane l lands at lds_addr + 16 l (wave-uniform).  Assembly, so that LDS reads of other buffers
-// do not wait for them: waits are placed by hand (vmcnt).
-__device__ __forceinline__ void to_lds_16(uint32_t voffset, const char* base, unsigned lds_addr) {
-  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(voffset), "s"(base), "s"(lds_addr) : "memory", "m0");
-}
-
 __device__ __forceinline__ f32x16 mfma32(bf16x8 a, bf16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
 __device__ __forceinline__ f32x16 mfma32(f16x8 a, f16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
 

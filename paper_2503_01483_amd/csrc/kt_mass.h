@@ -20,13 +20,9 @@ struct MassArgs {
   float decay;
 };
 
-// 16 bytes a lane from memory straight into LDS: lane l lands at lds_addr + 16 l (wave-uniform).  Waits are placed by hand (vmcnt).
-__device__ __forceinline__ void lds_copy_16(const char* base, uint32_t offset, unsigned lds_addr) {
-  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(base), "s"(lds_addr) : "memory", "m0");
-}
-
-__device__ __forceinline__ void lds_copy_4(const char* base, uint32_t offset, unsigned lds_addr) {
-  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1" ::"v"(offset), "s"(base), "s"(lds_addr) : "memory", "m0");
+// As to_lds_16, 4 bytes a lane.
+__device__ __forceinline__ void to_lds_4(uint32_t voffset, const char* base, unsigned lds_addr) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1" ::"v"(voffset), "s"(base), "s"(lds_addr) : "memory", "m0");
 }
 
 // Lists of sequences (LDS): a tag of the page that each begins with [n_seq, rounded up], groups of keys of one head in front of each [n_seq + 1].
@@ -315,7 +311,7 @@ __global__ __launch_bounds__(512, HD == 256 ? 2 : 4) void mass_rows_kernel(MassA
       const bool live = row < left;  // (rows behind the last one: some row of the first query that is there)
       return (live ? (uint32_t)(in_seq - base_q) * (uint32_t)(a.ldq * 2) + (uint32_t)(rest * ROWB) : 0u) + (uint32_t)(chunk * 16);
     };
-    auto send = [&](const char* base, uint32_t offset, int i, int at) { lds_copy_16(base, offset, uniform((int)(uintptr_t)sh.q[at] + (wave * PIECES + i) * 1024)); };
+    auto send = [&](const char* base, uint32_t offset, int i, int at) { to_lds_16(offset, base, uniform((int)(uintptr_t)sh.q[at] + (wave * PIECES + i) * 1024)); };
     auto fetch = [&](int64_t rt, int at) {
       int tid = threadIdx.x;
       asm volatile("" : "+v"(tid));  // (places are worked out anew: kept, they would push the keys out to memory)
@@ -325,8 +321,8 @@ __global__ __launch_bounds__(512, HD == 256 ? 2 : 4) void mass_rows_kernel(MassA
       if (wave == 0) {
         int in_seq, rest;
         find(tid, in_seq, rest);
-        lds_copy_4(heads_lse + (int64_t)base_q * a.hq * 4, rt * 64 + tid < rows ? ((uint32_t)(in_seq - base_q) * (uint32_t)a.hq + (uint32_t)rest) * 4u : 0u,
-                   uniform((int)(uintptr_t)sh.lse[at]));
+        to_lds_4(rt * 64 + tid < rows ? ((uint32_t)(in_seq - base_q) * (uint32_t)a.hq + (uint32_t)rest) * 4u : 0u, heads_lse + (int64_t)base_q * a.hq * 4,
+                 uniform((int)(uintptr_t)sh.lse[at]));
         sees = ahead + in_seq + 1;
       }
       base_q -= step_q;
@@ -347,7 +343,7 @@ __global__ __launch_bounds__(512, HD == 256 ? 2 : 4) void mass_rows_kernel(MassA
       const char* base = heads_q + (int64_t)base_q * a.ldq * 2;
 #pragma unroll
       for (int i = 0; i < PIECES; ++i) send(base, offsets[i], i, at);
-      if (wave == 0) lds_copy_4(heads_lse + (int64_t)base_q * a.hq * 4, offset_lse, uniform((int)(uintptr_t)sh.lse[at]));
+      if (wave == 0) to_lds_4(offset_lse, heads_lse + (int64_t)base_q * a.hq * 4, uniform((int)(uintptr_t)sh.lse[at]));
       sees -= step_q;
       base_q -= step_q;
     };
