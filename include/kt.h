@@ -545,7 +545,7 @@ kt_status kt_kv_select(const kt_kv_cache* cache, const float* mass, const int32_
  *           negative is passed over.
  *  mass     [n_pages][n_heads][page_size] fp32 or NULL.
  * Tokens whose index is outside of the sequence's pages, or whose page (read or written) is outside the cache, are not moved: what is in their
- * place stays.  Pages that two sequences name in place hold an unspecified mix of both.  No workspace.
+ * place stays.  Pages that two sequences are written to (in place: that both name) hold an unspecified mix of both.  No workspace.
  */
 kt_status kt_kv_compact(const kt_kv_cache* cache, const int32_t* pages, int64_t ldp, int64_t n_seq, const int32_t* src, int64_t lds,
                         int32_t per_head, const int32_t* count, const int32_t* first, const int32_t* to_pages, int64_t ldt,
