@@ -25,9 +25,9 @@
 // Trees (TREE) have few rows a sequence, all of which go through all of its tokens.  Their workgroups have four waves (bf16, many rows: eight), two of
 // them to a compute unit; a wave without rows copies and expands for the others.  Quantised blocks go to LDS as they are, two (u8) or four (u4) on their
 // way, and are expanded from there between two barriers, in place of a second buffer; one wave finds the parameters of the next block while the others compute.  The
-// list is worked out by every workgroup for itself.  32 trees of up to 64 drafts behind 8192, 32 + 2 x 8 heads of 128, 4 bits: 250 to 254 us, 430 TFLOP/s, of which a
-// wave spends 19 % on expanding, 34 % on exponentials and the products of the values, 15 to 24 % in front of barriers; 4 of 16 behind 65536, 8 bits: 154 to 158 us,
-// 2.6 TB/s.
+// list is worked out by every workgroup for itself.  32 trees of up to 64 drafts behind 8192, 32 + 2 x 8 heads of 128, 4 bits: 238 to 262 us by card and run, 420 to 460
+// TFLOP/s, of which a wave spends 19 % on expanding, 34 % on exponentials and the products of the values, 15 to 24 % in front of barriers; 4 of 16 behind 65536, 8 bits:
+// 139 to 173 us, 2.4 to 3.0 TB/s.
 //
 // All key tiles of all row tiles form one list, heads outermost; each workgroup takes an equal piece, neighbouring pieces on one XCD, whose
 // L2 then holds the keys of few heads.  Segments that are cut are joined by a second launch.

@@ -63,8 +63,8 @@ __device__ __forceinline__ void list_key_groups(const AttendArgs& a, int keys, i
 // How many of sequence s' tokens, as far as they lie in `page`, place `place` of its table, belong to sequences in front of it, which share the page: they
 // begin with the same page as s and have this one at the same place.  Whoever else names a page is not looked for: each pair of places would have to be compared.
 // No more than `enough` are looked for.  All lanes take part; uniform, as the arguments are.
-// Beside the loads of keys it costs nothing up to 64 sequences (64 behind up to 16384, 4 bits: 105 to 115 us with and without); 256 behind up to 2000 take 48 us
-// (without it 47), 1024 behind 500 63 (59), 4096 behind 70 133 (106); 256 that share the first half of their pages 62.
+// Beside the loads of keys it costs little (decode, 4 bits: 64 sequences behind up to 16384 103 to 118 us with and without, 32 behind 8000 39 us, without it 38; 256
+// behind up to 2000 48 (47), 1024 behind 500 63 (59), 4096 behind 70 134 (106)); 256 that share the first half of their pages take 62.
 __device__ __forceinline__ int owned_in_front(const AttendArgs& a, const uint16_t* tags, int s, int place, int page, int enough) {
   const int lane = threadIdx.x & 63;
   const uint32_t both = tags[s] * 0x10001u;
@@ -90,7 +90,7 @@ __device__ __forceinline__ int owned_in_front(const AttendArgs& a, const uint16_
 }
 
 // Few rows: a wave goes through all of them, 4 NI at a time, with queries straight from memory.  Bound by HBM: 64 tokens behind up to 16384, 32 + 8 heads of 128, 4 bits:
-// 103 us, 4.1 TB/s of keys, parameters and masses.
+// 101 to 104 us, 4.1 TB/s of keys, parameters and masses.
 template <int KV, int HD, int NI>
 __global__ __launch_bounds__(256, 2) void mass_few_kernel(MassArgs t) {
   extern __shared__ __align__(16) char lds[];
@@ -221,11 +221,11 @@ __global__ __launch_bounds__(256, 2) void mass_few_kernel(MassArgs t) {
 }
 
 // Many rows: queries go through LDS, 64 rows at a time, double buffered, straight from memory, by lanes that read neighbouring bytes (an operand's
-// own lanes read sixteen rows at once, of which the first-level cache finds one a cycle: 690 us instead of 440 for prompts of up to 2 x 8192, 32 + 8 heads of 128, bf16).  Four of the eight waves share a block and
+// own lanes read sixteen rows at once, of which the first-level cache finds one a cycle: 690 us instead of 440 to 450 for prompts of up to 2 x 8192, 32 + 8 heads of 128, bf16).  Four of the eight waves share a block and
 // take sixteen of the rows each, the two blocks lie next to each other.  Rows go from the last one down to the first that sees the first key:
 // workgroups that begin together find each other's queries in the caches.
 // Bound by the vector ALU (an exponential, two more instructions a score) and by the workgroup with the most rows, alone on its compute unit at the
-// end: 770 TFLOP/s of Q K^T for those prompts.
+// end: 750 to 770 TFLOP/s of Q K^T for those prompts.
 template <int HD>
 struct alignas(16) MassShared {
   char q[2][64 * HD * 2];  // 16-byte chunks of a row exchanged by its number, so that eight rows' are in all banks
