@@ -574,7 +574,8 @@ def _mass(mass, cache, dev):
 
 def kt_attention_mass(Q, cache, pages, lens, lse, mass, *, q_starts=None, max_q=None, scale=None, decay=1.0, stream=None):
     """Adds to `mass` [n_pages][heads][page_size] fp32 the attention weight that the cache's tokens receive from Q [n_tokens][heads][head_dim], whose
-    lse [n_tokens][heads] attention has written, after a product of what is there with `decay`; returns mass."""
+    lse [n_tokens][heads] attention has written, after a product of what is there with `decay`; returns mass.  Tokens of pages that sequences begin with together
+    get that of the first of them."""
     dev = _device(Q, "Q")
     n, hq, hd, ldq = _queries(Q, cache, dev)
     ref = cache._on(dev)

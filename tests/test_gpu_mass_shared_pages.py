@@ -70,6 +70,19 @@ def test_many_sequences_behind_one_page(fmt, most):
 
 
 @pytest.mark.parametrize("fmt", FORMATS, ids=NAMES.get)
+@pytest.mark.parametrize("most", [1, 30], ids=["tokens", "chunks"])
+def test_sharers_far_apart(fmt, most):
+    """1100 sequences, few of which share: a page with one hundreds of places in front, the second page alone with nobody."""
+    n = 1100
+    lens = [(37 * i) % 100 + 20 for i in range(n)]
+    tables = [[i % 97 if i % 97 < 3 else 100 + 2 * i, 101 + 2 * i] for i in range(n)]
+    counts = [1 if most == 1 else min(t, (7 * i) % 4) for i, t in enumerate(lens)]
+    if most > 1:
+        counts[1067] = 30
+    check(shared(fmt, lens, counts, tables, hd=64, hkv=1, group=3, seed=11), 0.5, single=most == 1)
+
+
+@pytest.mark.parametrize("fmt", FORMATS, ids=NAMES.get)
 def test_weights_of_a_shared_prompt_choose_the_same_tokens_every_time(fmt):
     b = shared(fmt, [320, 300, 310], [1, 1, 1], [[0, 1, 2, 3, 4], [0, 1, 2, 3, 5], [0, 1, 2, 3, 6]])
     q, lens, lse = b.q.cuda(), ints(b.lens), b.expected()[1].float().cuda()
